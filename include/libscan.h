@@ -393,6 +393,172 @@ int scan_inclusive_i32_noalloc(const int32_t* x, int32_t* y, int64_t n, void* st
  * LIBSCAN_ERANGE beyond the op's limits.  Pure host function. */
 int libscan_scratch_bytes(int op, int64_t rows, int64_t len, int64_t k, size_t* bytes);
 
+/* ------------------------------------------------------------------------
+ * Language model operators: the first-order linear recurrence of selective
+ * state space layers (a prefix scan with h_t = a_t h_{t-1} + b_t in the place
+ * of the sum, Section 2), the short causal convolution in front of it, and
+ * the logits' processing in front of topp_sample_f32 and topk_rows_f32
+ * (Section 5).  They are described by structs whose fields are all 8 bytes
+ * wide (strides in elements).  Rules shared by all of them:
+ *  - `type` is the element type of the activations; they are read as fp32,
+ *    every sum, state and statistic is fp32, and outputs are rounded once (to
+ *    nearest even).
+ *  - Inputs have unit stride over their last dimension and any strides >= 0
+ *    over the others; element alignment is enough.  Outputs are dense.
+ *    Outputs may not overlap inputs or each other (spans are compared), except
+ *    where noted.
+ *  - lengths (nullable, device, batch int32): row b has lengths[b] tokens
+ *    (taken as 0..steps); what its inputs hold past them is not read, its
+ *    outputs are 0 there, and its last state is the one after its last token.
+ *  - slots (nullable, device, batch int32): the state of row b is number
+ *    slots[b] of the pool (b when slots is NULL).  A number outside the pool
+ *    (such as -1, an idle row) reads and writes no state and gives 0.  No two
+ *    rows of a call may name the same state.
+ *  - scratch as in topp_sample_f32: needs no initialisation, carries nothing.
+ * ------------------------------------------------------------------------ */
+#define LIBSCAN_F32 0
+#define LIBSCAN_F16 1  /* IEEE binary16 */
+#define LIBSCAN_BF16 2 /* bfloat16 */
+
+/* The causal convolution y[b,t,d] = f(bias[d] + sum_{j < width} weight[d,j] *
+ * x[b, t - (width-1) + j, d]), f = silu (v / (1 + e^-v)) when silu != 0, else the
+ * identity.  x: batch x steps x dim.  Inputs before the first come from state
+ * (nullable: zeros), batch x (width-1) x dim dense, oldest first, of `type`.
+ * weight: dim x width and bias (nullable): dim, dense, of `weight_type` (type or
+ * LIBSCAN_F32).  2 <= width <= 4. */
+typedef struct {
+    int64_t type, weight_type, batch, steps, dim, width, silu;
+    const void* x;
+    int64_t x_batch, x_step;
+    const void* weight;
+    const void* bias;
+    const void* state;
+    const int32_t* lengths;
+} libscan_conv;
+
+/* y: batch x steps x dim.  state_out (nullable): batch x (width-1) x dim, the last
+ * width-1 inputs of every row (with the first state's in front of short rows). */
+int causal_conv(const libscan_conv* p, void* y, void* state_out, void* stream);
+
+/* Gradients for dy (batch x steps x dim, strides dy_batch, dy_step) and
+ * dstate_out (nullable, dense, of `type`: the gradient of state_out): dx (batch x
+ * steps x dim), dweight (dim x width, fp32), dbias (dim, fp32; nullable) and
+ * dstate (nullable: batch x (width-1) x dim, of `type`).  Sums run in a fixed
+ * order.  Scratch: what causal_conv_scratch_bytes reports (a host function). */
+int causal_conv_backward(const libscan_conv* p, const void* dy, int64_t dy_batch, int64_t dy_step,
+                         const void* dstate_out, void* dx, float* dweight, float* dbias,
+                         void* dstate, void* scratch, size_t scratch_bytes, void* stream);
+int causal_conv_scratch_bytes(const libscan_conv* p, size_t* bytes);
+
+/* One token of every row (steps = 1; p->state and p->lengths NULL): y (batch x
+ * dim) from x and the pool states (n_states x (width-1) x dim, dense), which
+ * move on by one input in place. */
+int causal_conv_step(const libscan_conv* p, void* states, int64_t n_states, const int32_t* slots,
+                     void* y, void* stream);
+
+/* The selective scan.  With delta = softplus(dt + dt_bias) (softplus != 0; else
+ * dt + dt_bias), per row b, channel d and state index i < n:
+ *   h[t,d,i] = exp(delta[t,d] A[d,i]) h[t-1,d,i] + delta[t,d] B[t,g,i] x[t,d]
+ *   y[t,d] = (sum_i C[t,g,i] h[t,d,i] + D[d] x[t,d]) * silu(z[t,d])
+ * where channel d belongs to group g = d / (dim / groups).  x, dt, z (nullable: no
+ * gate): batch x steps x dim; B, C: batch x steps x groups x n; A: dim x n, D
+ * and dt_bias (nullable): dim, dense fp32; state (nullable: zeros): batch x dim x
+ * n, dense fp32.  1 <= n <= 64, dim a multiple of groups. */
+typedef struct {
+    int64_t type, batch, steps, dim, n, groups, softplus;
+    const void* x;
+    int64_t x_batch, x_step;
+    const void* dt;
+    int64_t dt_batch, dt_step;
+    const void* z;
+    int64_t z_batch, z_step;
+    const void* B;
+    int64_t B_batch, B_step, B_group;
+    const void* C;
+    int64_t C_batch, C_step, C_group;
+    const float* A;
+    const float* D;
+    const float* dt_bias;
+    const float* state;
+    const int32_t* lengths;
+} libscan_ssm;
+
+/* Bytes of the checkpoints that selective_scan hands to its gradient, and of
+ * the scratch of either.  Host function; only the sizes in *p are read. */
+int selective_scan_bytes(const libscan_ssm* p, size_t* checkpoints, size_t* scratch,
+                         size_t* backward_scratch);
+
+/* y: batch x steps x dim; state_out (nullable): batch x dim x n fp32, the last
+ * state; checkpoints (nullable): the state before every 16th token, for
+ * selective_scan_backward. */
+int selective_scan(const libscan_ssm* p, void* y, float* state_out, float* checkpoints,
+                   void* scratch, size_t scratch_bytes, void* stream);
+
+/* Gradients for dy (batch x steps x dim, strides dy_batch, dy_step) and
+ * dstate_out (nullable, batch x dim x n fp32: the gradient of the last state),
+ * from the same *p and the checkpoints of its selective_scan call: dx, ddt, dz
+ * (needed with z): batch x steps x dim; dB, dC: batch x steps x groups x n, all of
+ * `type`; dA: dim x n, dD (needed with D), ddt_bias (needed with dt_bias): dim,
+ * dstate (nullable): batch x dim x n, fp32.  Sums run in a fixed order. */
+int selective_scan_backward(const libscan_ssm* p, const void* dy, int64_t dy_batch,
+                            int64_t dy_step, const float* checkpoints, const float* dstate_out,
+                            void* dx, void* ddt, float* dA, void* dB, void* dC, float* dD,
+                            void* dz, float* ddt_bias, float* dstate, void* scratch,
+                            size_t scratch_bytes, void* stream);
+
+/* One token of every row (steps = 1; p->state and p->lengths NULL): y (batch x
+ * dim); the pool states (n_states x dim x n, dense fp32) move on in place. */
+int selective_scan_step(const libscan_ssm* p, float* states, int64_t n_states,
+                        const int32_t* slots, void* y, void* stream);
+
+/* Logits before a sampler.  logits: rows x vocab, row stride logits_row.  In this
+ * order, per row:
+ *  - every token id that history[0 .. history_len) holds: l > 0 ? l / repetition :
+ *    l * repetition;
+ *  - every id that history[prompt_len .. history_len) holds c > 0 times:
+ *    l -= c * frequency + presence;
+ *  - every entry of bias_ids (rows x biases): l += its value (several entries of
+ *    one id add up, in list order);
+ *  - bits of allowed (rows x ceil(vocab / 32) words, lowest bit first): 0 makes
+ *    l -infinity, whatever it was.
+ * history: rows x history_cols int32 with row stride history_row; ids outside
+ * the vocabulary (padding) are skipped, in bias_ids too.  history_len (NULL:
+ * history_cols) and prompt_len (NULL: 0) are taken as 0..history_cols.
+ * repetition, presence, frequency, temperature: rows fp32 each; NULL: 1, 0, 0, 1.
+ * vocab and history_cols <= INT32_MAX. */
+typedef struct {
+    int64_t type, rows, vocab;
+    const void* logits;
+    int64_t logits_row;
+    const int32_t* history;
+    int64_t history_row, history_cols;
+    const int32_t* history_len;
+    const int32_t* prompt_len;
+    const float* repetition;
+    const float* presence;
+    const float* frequency;
+    const int32_t* bias_ids;
+    const float* bias_values;
+    int64_t biases;
+    const int32_t* allowed;
+    int64_t allowed_row;
+    const float* temperature;
+} libscan_logits;
+
+/* out: rows x vocab of `type` with row stride out_row, the processed logits
+ * (temperature is not read).  out == logits with the same stride is allowed. */
+int logits_process(const libscan_logits* p, void* out, int64_t out_row, void* stream);
+
+/* probs: rows x vocab fp32, dense: softmax of the processed logits divided by the
+ * row's temperature, as topp_sample_f32 takes it.  A temperature of 0 is the
+ * limit: equal shares for the places of the largest logit.  Places at -infinity
+ * get 0; so does a row that has no others.  A NaN or +infinity elsewhere (but
+ * for +infinity at temperature 0) makes every place above -infinity NaN.
+ * Scratch: logits_scratch_bytes (a host function). */
+int logits_probs(const libscan_logits* p, float* probs, void* scratch, size_t scratch_bytes,
+                 void* stream);
+int logits_scratch_bytes(const libscan_logits* p, size_t* bytes);
+
 #ifdef __cplusplus
 }
 #endif

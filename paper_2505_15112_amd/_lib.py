@@ -20,6 +20,7 @@ _p = ctypes.c_void_p
 _i64 = ctypes.c_int64
 _int = ctypes.c_int
 _sz = ctypes.c_size_t
+_struct = ctypes.c_char_p  # a struct's bytes, packed from its fields (all 8 bytes wide)
 
 # name -> (restype, argtypes)
 SIGNATURES = {
@@ -61,10 +62,23 @@ SIGNATURES = {
     "libscan_scratch_bytes": (_int, [_int, _i64, _i64, _i64, ctypes.POINTER(_sz)]),
     "topk_rows_f32": (_int, [_p, _p, _p, _i64, _i64, _i64, _int, _p, _sz, _p, _sz, _p]),
     "scan_inclusive_i32_noalloc": (_int, [_p, _p, _i64, _p]),
+    "causal_conv": (_int, [_struct, _p, _p, _p]),
+    "causal_conv_backward": (_int, [_struct, _p, _i64, _i64, _p, _p, _p, _p, _p, _p, _sz, _p]),
+    "causal_conv_scratch_bytes": (_int, [_struct, ctypes.POINTER(_sz)]),
+    "causal_conv_step": (_int, [_struct, _p, _i64, _p, _p, _p]),
+    "selective_scan_bytes": (_int, [_struct, ctypes.POINTER(_sz), ctypes.POINTER(_sz),
+                                    ctypes.POINTER(_sz)]),
+    "selective_scan": (_int, [_struct, _p, _p, _p, _p, _sz, _p]),
+    "selective_scan_backward": (_int, [_struct, _p, _i64, _i64] + [_p] * 12 + [_sz, _p]),
+    "selective_scan_step": (_int, [_struct, _p, _i64, _p, _p, _p]),
+    "logits_process": (_int, [_struct, _p, _i64, _p]),
+    "logits_probs": (_int, [_struct, _p, _p, _sz, _p]),
+    "logits_scratch_bytes": (_int, [_struct, ctypes.POINTER(_sz)]),
 }
 
 OK, EINVAL, ENOSPACE, EHIP, ERANGE = 0, -1, -2, -3, -4
 OP_SCAN, OP_SCAN_RSS, OP_SCAN_ROWS, OP_COMPACT, OP_RADIX_SORT = 1, 2, 3, 4, 5
+F32, F16, BF16 = 0, 1, 2
 OP_SORT_ROWS, OP_WEIGHTED_SAMPLE, OP_TOPP_SAMPLE, OP_TOPK = 6, 7, 8, 9
 
 _LIB = None

@@ -1,0 +1,366 @@
+// conv.hip -- the causal depthwise convolution in front of the selective scan.
+//
+// y[t] = f(bias + sum_j w[j] x[t - (W-1) + j]) per channel, W = 2..4.  HBM bounds
+// it: a thread owns 16 bytes of channels and a run of steps, so that every
+// input is loaded once (but for the W-1 in front of a run) and the window
+// slides through registers.
+#include "launch.hpp"
+#include "lm.hpp"
+
+#include "../../include/libscan.h"
+
+namespace ls {
+
+namespace {
+
+constexpr int kThreads = 256;
+constexpr int kRun = 16;      // steps a thread owns, forward
+constexpr int kBackRun = 32;  // and backward
+constexpr int kBackV = 4;     // channels of a thread, backward
+constexpr int kBackSide = 32; // threads of a workgroup over channels, backward
+constexpr int kBackRuns = kThreads / kBackSide;
+
+// workgroups over the steps of a row, backward (one even where there are none,
+// for the gradient of the first state)
+__host__ __device__ inline int back_runs(int64_t steps) {
+    const int per = kBackRun * kBackRuns;
+    return steps ? (int)((steps + per - 1) / per) : 1;
+}
+
+__device__ __forceinline__ int conv_len(const libscan_conv& p, int b) {
+    if (!p.lengths) return (int)p.steps;
+    const int n = p.lengths[b];
+    return n < 0 ? 0 : n < (int)p.steps ? n : (int)p.steps;
+}
+
+// weight and bias of `V` channels from c0 on, of T or float
+template <class T, int W, int V>
+__device__ __forceinline__ void load_weights(const libscan_conv& p, int c0, int count,
+                                             float (&w)[W][V], float (&bias)[V]) {
+    const bool f32 = p.weight_type == LIBSCAN_F32;
+#pragma unroll
+    for (int i = 0; i < V; ++i) {
+        const bool in = i < count;
+#pragma unroll
+        for (int j = 0; j < W; ++j) {
+            const int64_t at = (int64_t)(c0 + i) * W + j;
+            w[j][i] = !in ? 0.0f
+                          : f32 ? ((const float*)p.weight)[at] : to_f32(((const T*)p.weight)[at]);
+        }
+        bias[i] = !in || !p.bias
+                      ? 0.0f
+                      : f32 ? ((const float*)p.bias)[c0 + i] : to_f32(((const T*)p.bias)[c0 + i]);
+    }
+}
+
+// x of step t, which may lie in the first state (t >= -(W-1)), or past the end (0)
+template <class T, int W, int V>
+__device__ __forceinline__ void load_step(const libscan_conv& p, const T* px, const T* ps, int t,
+                                          int len, int count, Pack<T, V>& v) {
+    if (t >= 0)
+        v.load(px + t * p.x_step, t < len ? count : 0);
+    else
+        v.load(ps + (t + W - 1) * p.dim, ps ? count : 0);
+}
+
+template <class T, int W>
+__global__ __launch_bounds__(kThreads) void k_conv(libscan_conv p, T* y, T* state_out) {
+    constexpr int V = 16 / sizeof(T);
+    const int dim = (int)p.dim, steps = (int)p.steps;
+    const int64_t nc = (dim + V - 1) / V, nr = steps ? (steps + kRun - 1) / kRun : 1;
+    const int64_t id = (int64_t)blockIdx.x * kThreads + threadIdx.x;
+    if (id >= nc * nr * p.batch) return;
+    const int c0 = (int)(id % nc) * V, r = (int)(id / nc % nr), b = (int)(id / (nc * nr));
+    const int count = dim - c0, len = conv_len(p, b), t0 = r * kRun;
+    const T* px = (const T*)p.x + b * p.x_batch + c0;
+    const T* ps = p.state ? (const T*)p.state + (int64_t)b * (W - 1) * dim + c0 : nullptr;
+    T* py = y + (int64_t)b * steps * dim + c0;
+    float w[W][V], bias[V];
+    load_weights<T, W, V>(p, c0, count, w, bias);
+    Pack<T, V> x[kRun + W - 1];
+#pragma unroll
+    for (int i = 0; i < kRun + W - 1; ++i)
+        load_step<T, W, V>(p, px, ps, t0 + i - (W - 1), len, count, x[i]);
+#pragma unroll
+    for (int i = 0; i < kRun; ++i) {
+        const int t = t0 + i;
+        if (t < steps) {
+            Pack<T, V> out;
+#pragma unroll
+            for (int c = 0; c < V; ++c) {
+                float u = bias[c];
+#pragma unroll
+                for (int j = 0; j < W; ++j) u = __builtin_fmaf(w[j][c], to_f32(x[i + j].v[c]), u);
+                if (p.silu) u *= sigmoid(u);
+                out.v[c] = from_f32<T>(t < len ? u : 0.0f);
+            }
+            out.store(py + (int64_t)t * dim, count);
+        }
+    }
+    // the last W-1 inputs, by the thread of the row's last token
+    if (state_out && (len > 0 ? (len - 1) / kRun : 0) == r) {
+#pragma unroll
+        for (int j = 0; j < W - 1; ++j) {
+            Pack<T, V> v;
+            load_step<T, W, V>(p, px, ps, len - (W - 1) + j, len, count, v);
+            v.store(state_out + ((int64_t)b * (W - 1) + j) * dim + c0, count);
+        }
+    }
+}
+
+// One token against the pool.
+template <class T, int W>
+__global__ __launch_bounds__(kThreads) void k_conv_step(libscan_conv p, T* states,
+                                                        int64_t n_states, const int32_t* slots,
+                                                        T* y) {
+    constexpr int V = 8 / sizeof(T);
+    const int dim = (int)p.dim;
+    const int64_t nc = (dim + V - 1) / V;
+    const int64_t id = (int64_t)blockIdx.x * kThreads + threadIdx.x;
+    if (id >= nc * p.batch) return;
+    const int c0 = (int)(id % nc) * V, b = (int)(id / nc), count = dim - c0;
+    const int64_t slot = slots ? slots[b] : b;
+    T* py = y + (int64_t)b * dim + c0;
+    Pack<T, V> out;
+    if (slot < 0 || slot >= n_states) {
+#pragma unroll
+        for (int c = 0; c < V; ++c) out.v[c] = T(0);
+        out.store(py, count);
+        return;
+    }
+    T* ps = states + slot * (W - 1) * dim + c0;
+    Pack<T, V> x[W];
+#pragma unroll
+    for (int j = 0; j < W - 1; ++j) x[j].load(ps + (int64_t)j * dim, count);
+    x[W - 1].load((const T*)p.x + b * p.x_batch + c0, count);
+    float w[W][V], bias[V];
+    load_weights<T, W, V>(p, c0, count, w, bias);
+#pragma unroll
+    for (int c = 0; c < V; ++c) {
+        float u = bias[c];
+#pragma unroll
+        for (int j = 0; j < W; ++j) u = __builtin_fmaf(w[j][c], to_f32(x[j].v[c]), u);
+        if (p.silu) u *= sigmoid(u);
+        out.v[c] = from_f32<T>(u);
+    }
+    out.store(py, count);
+#pragma unroll
+    for (int j = 0; j < W - 1; ++j) x[j + 1].store(ps + (int64_t)j * dim, count);
+}
+
+struct BackArgs {
+    const void* dy;
+    int64_t dy_batch, dy_step;
+    const void* dstate_out;
+    void *dx, *dstate;
+    float* part;  // [row of blocks][W + 1][dim]: sums of dweight's columns and of dbias
+};
+
+// Gradients.  g[t] = dy[t] f'(u[t]), u formed again; dx[t] = sum_j w[j] g[t + W-1 - j],
+// so a thread forms g of its run and of the W-1 steps behind it.
+template <class T, int W>
+__global__ __launch_bounds__(kThreads) void k_conv_back(libscan_conv p, BackArgs o) {
+    constexpr int V = kBackV;
+    __shared__ float s_sum[kBackRuns][W + 1][kBackSide * V];
+    const int dim = (int)p.dim, steps = (int)p.steps;
+    const int side = threadIdx.x % kBackSide, run = threadIdx.x / kBackSide;
+    const int nc = (dim + kBackSide * V - 1) / (kBackSide * V);
+    const int nr = back_runs(steps);
+    const int cb = blockIdx.x % nc, part = blockIdx.x / nc;  // part = b * nr + rb
+    const int b = part / nr, rb = part % nr;
+    const int c0 = (cb * kBackSide + side) * V, count = dim - c0, len = conv_len(p, b);
+    const int t0 = (rb * kBackRuns + run) * kBackRun;
+    const T* px = (const T*)p.x + b * p.x_batch + c0;
+    const T* ps = p.state ? (const T*)p.state + (int64_t)b * (W - 1) * dim + c0 : nullptr;
+    const T* pdy = (const T*)o.dy + b * o.dy_batch + c0;
+    const T* pso = o.dstate_out ? (const T*)o.dstate_out + (int64_t)b * (W - 1) * dim + c0 : nullptr;
+    T* pdx = (T*)o.dx + (int64_t)b * steps * dim + c0;
+    float w[W][V], bias[V], dw[W][V], db[V];
+    load_weights<T, W, V>(p, c0, count, w, bias);
+#pragma unroll
+    for (int c = 0; c < V; ++c) {
+        db[c] = 0.0f;
+#pragma unroll
+        for (int j = 0; j < W; ++j) dw[j][c] = 0.0f;
+    }
+    // the gradient of input t (t >= -(W-1)) from the W outputs that read it
+    auto input_grad = [&](const float(&g)[W][V], int t, Pack<T, V>& out) {
+        Pack<T, V> so;
+        const int j0 = t - (len - (W - 1));  // its place in the last state
+        so.load(pso + (int64_t)j0 * dim, pso && j0 >= 0 && t < len ? count : 0);
+#pragma unroll
+        for (int c = 0; c < V; ++c) {
+            float v = to_f32(so.v[c]);
+#pragma unroll
+            for (int j = 0; j < W; ++j) v = __builtin_fmaf(w[j][c], g[W - 1 - j][c], v);
+            out.v[c] = from_f32<T>(t < len ? v : 0.0f);
+        }
+    };
+
+    if (count > 0 && (t0 < steps || t0 == 0)) {
+        Pack<T, V> x[W];      // x[t - (W-1)] .. x[t]
+        float g[W][V] = {};   // g[t - (W-1)] .. g[t]
+#pragma unroll
+        for (int j = 0; j < W - 1; ++j)
+            load_step<T, W, V>(p, px, ps, t0 - (W - 1) + j, len, count, x[j]);
+        const int end = t0 + kBackRun < steps ? t0 + kBackRun : steps;  // of this run
+#pragma unroll 4
+        for (int t = t0; t < end + W - 1; ++t) {
+            Pack<T, V> dy;
+            load_step<T, W, V>(p, px, ps, t, len, count, x[W - 1]);
+            dy.load(pdy + t * o.dy_step, t < len ? count : 0);
+#pragma unroll
+            for (int c = 0; c < V; ++c) {
+                float gv = to_f32(dy.v[c]);
+                if (p.silu) {
+                    float u = bias[c];
+#pragma unroll
+                    for (int j = 0; j < W; ++j)
+                        u = __builtin_fmaf(w[j][c], to_f32(x[j].v[c]), u);
+                    const float sig = sigmoid(u);
+                    gv *= sig * (1.0f + u * (1.0f - sig));
+                }
+                g[W - 1][c] = t < len ? gv : 0.0f;
+                if (t < end) {
+                    db[c] += g[W - 1][c];
+#pragma unroll
+                    for (int j = 0; j < W; ++j)
+                        dw[j][c] = __builtin_fmaf(g[W - 1][c], to_f32(x[j].v[c]), dw[j][c]);
+                }
+            }
+            const int ti = t - (W - 1);
+            if (ti >= t0) {
+                Pack<T, V> out;
+                input_grad(g, ti, out);
+                out.store(pdx + (int64_t)ti * dim, count);
+            } else if (t0 == 0 && o.dstate) {
+                Pack<T, V> out;
+                input_grad(g, ti, out);
+                out.store((T*)o.dstate + ((int64_t)b * (W - 1) + t) * dim + c0, count);
+            }
+#pragma unroll
+            for (int j = 0; j < W - 1; ++j) {
+                x[j] = x[j + 1];
+#pragma unroll
+                for (int c = 0; c < V; ++c) g[j][c] = g[j + 1][c];
+            }
+        }
+    }
+#pragma unroll
+    for (int c = 0; c < V; ++c) {
+#pragma unroll
+        for (int j = 0; j < W; ++j) s_sum[run][j][side * V + c] = dw[j][c];
+        s_sum[run][W][side * V + c] = db[c];
+    }
+    __syncthreads();
+    for (int e = threadIdx.x; e < (W + 1) * kBackSide * V; e += kThreads) {
+        const int j = e / (kBackSide * V), c = e % (kBackSide * V);
+        if (cb * kBackSide * V + c < dim) {
+            float sum = 0.0f;
+#pragma unroll
+            for (int r = 0; r < kBackRuns; ++r) sum += s_sum[r][j][c];
+            o.part[((int64_t)part * (W + 1) + j) * dim + cb * kBackSide * V + c] = sum;
+        }
+    }
+}
+
+// dweight and dbias: the workgroups' sums, added in order.
+__global__ __launch_bounds__(kThreads) void k_conv_sum(const float* part, int64_t parts, int64_t dim,
+                                                       int width, float* dweight, float* dbias) {
+    const int64_t i = (int64_t)blockIdx.x * kThreads + threadIdx.x;
+    if (i >= dim * (width + 1)) return;
+    const int j = (int)(i / dim);
+    const int64_t c = i % dim;
+    float sum = 0.0f;
+#pragma unroll 8
+    for (int64_t k = 0; k < parts; ++k) sum += part[k * (width + 1) * dim + i];
+    if (j < width)
+        dweight[c * width + j] = sum;
+    else if (dbias)
+        dbias[c] = sum;
+}
+
+int64_t back_parts(const libscan_conv& p) {
+    return p.batch * back_runs(p.steps);
+}
+
+unsigned groups_of(int64_t n, int64_t per) { return (unsigned)((n + per - 1) / per); }
+
+template <class T, int W>
+hipError_t conv_as(const libscan_conv& p, void* y, void* state_out, hipStream_t s) {
+    constexpr int V = 16 / sizeof(T);
+    const int64_t nr = p.steps ? (p.steps + kRun - 1) / kRun : 1;
+    const int64_t n = (p.dim + V - 1) / V * nr * p.batch;
+    k_conv<T, W><<<groups_of(n, kThreads), kThreads, 0, s>>>(p, (T*)y, (T*)state_out);
+    return hipGetLastError();
+}
+
+template <class T, int W>
+hipError_t step_as(const libscan_conv& p, void* states, int64_t n_states, const int32_t* slots,
+                   void* y, hipStream_t s) {
+    constexpr int V = 8 / sizeof(T);
+    const int64_t n = (p.dim + V - 1) / V * p.batch;
+    k_conv_step<T, W><<<groups_of(n, kThreads), kThreads, 0, s>>>(p, (T*)states, n_states, slots,
+                                                                 (T*)y);
+    return hipGetLastError();
+}
+
+template <class T, int W>
+hipError_t back_as(const libscan_conv& p, const BackArgs& o, float* dweight, float* dbias,
+                   hipStream_t s) {
+    const int64_t parts = back_parts(p);
+    const int64_t nc = (p.dim + kBackSide * kBackV - 1) / (kBackSide * kBackV);
+    if (parts > 0) k_conv_back<T, W><<<(unsigned)(parts * nc), kThreads, 0, s>>>(p, o);
+    k_conv_sum<<<groups_of(p.dim * (W + 1), kThreads), kThreads, 0, s>>>(o.part, parts, p.dim, W,
+                                                                       dweight, dbias);
+    return hipGetLastError();
+}
+
+template <class F>
+hipError_t by_type_width(const libscan_conv& p, F f) {
+    auto width = [&](auto t) {
+        switch (p.width) {
+            case 2: return f(t, std::integral_constant<int, 2>());
+            case 3: return f(t, std::integral_constant<int, 3>());
+            default: return f(t, std::integral_constant<int, 4>());
+        }
+    };
+    switch (p.type) {
+        case LIBSCAN_F16: return width(_Float16());
+        case LIBSCAN_BF16: return width(__bf16());
+        default: return width(float());
+    }
+}
+
+}  // namespace
+
+hipError_t launch_conv(const libscan_conv& p, void* y, void* state_out, hipStream_t stream) {
+    if (p.batch == 0 || p.dim == 0) return hipSuccess;
+    return by_type_width(p, [&](auto t, auto w) {
+        return conv_as<decltype(t), decltype(w)::value>(p, y, state_out, stream);
+    });
+}
+
+hipError_t launch_conv_step(const libscan_conv& p, void* states, int64_t n_states,
+                            const int32_t* slots, void* y, hipStream_t stream) {
+    if (p.batch == 0 || p.dim == 0) return hipSuccess;
+    return by_type_width(p, [&](auto t, auto w) {
+        return step_as<decltype(t), decltype(w)::value>(p, states, n_states, slots, y, stream);
+    });
+}
+
+size_t conv_scratch_bytes(const libscan_conv& p) {
+    return (size_t)back_parts(p) * (p.width + 1) * p.dim * 4;
+}
+
+hipError_t launch_conv_back(const libscan_conv& p, const void* dy, int64_t dy_batch,
+                            int64_t dy_step, const void* dstate_out, void* dx, float* dweight,
+                            float* dbias, void* dstate, void* scratch, hipStream_t stream) {
+    if (p.dim == 0) return hipSuccess;
+    const BackArgs o{dy, dy_batch, dy_step, dstate_out, dx, dstate, (float*)scratch};
+    return by_type_width(p, [&](auto t, auto w) {
+        return back_as<decltype(t), decltype(w)::value>(p, o, dweight, dbias, stream);
+    });
+}
+
+}  // namespace ls

@@ -8,6 +8,8 @@
 #include <stddef.h>
 #include <stdint.h>
 
+#include "../../include/libscan.h"
+
 namespace ls {
 
 // Element kinds of the 1-D scans: input type -> accumulation/output type.
@@ -107,5 +109,34 @@ size_t radix_ws_bytes(int64_t n, int bits);
 hipError_t launch_radix_sort(const uint32_t* keys, uint32_t* keys_out, int32_t* perm_out,
                              uint32_t* keys_tmp, int32_t* perm_tmp, int64_t n, int bits, void* ws,
                              size_t ws_bytes, hipStream_t stream);
+
+// Language model operators (structs of libscan.h; sizes and pointers checked
+// by the C ABI).
+hipError_t launch_conv(const libscan_conv& p, void* y, void* state_out, hipStream_t stream);
+hipError_t launch_conv_step(const libscan_conv& p, void* states, int64_t n_states,
+                            const int32_t* slots, void* y, hipStream_t stream);
+size_t conv_scratch_bytes(const libscan_conv& p);
+hipError_t launch_conv_back(const libscan_conv& p, const void* dy, int64_t dy_batch,
+                            int64_t dy_step, const void* dstate_out, void* dx, float* dweight,
+                            float* dbias, void* dstate, void* scratch, hipStream_t stream);
+
+size_t ssm_ckpt_bytes(const libscan_ssm& p);
+size_t ssm_scratch_bytes(const libscan_ssm& p);
+size_t ssm_back_scratch_bytes(const libscan_ssm& p);
+hipError_t launch_ssm_scan(const libscan_ssm& p, void* y, float* state_out, float* ckpt,
+                           void* scratch, hipStream_t stream);
+hipError_t launch_ssm_step(const libscan_ssm& p, float* states, int64_t n_states,
+                           const int32_t* slots, void* y, hipStream_t stream);
+hipError_t launch_ssm_back(const libscan_ssm& p, const void* dy, int64_t dy_batch, int64_t dy_step,
+                           const float* ckpt, const float* dstate_out, void* dx, void* ddt,
+                           float* dA, void* dB, void* dC, float* dD, void* dz, float* ddt_bias,
+                           float* dstate, void* scratch, hipStream_t stream);
+
+bool logits_fit(const libscan_logits& p);  // one launch holds the rows' segments
+size_t logits_scratch(const libscan_logits& p);
+hipError_t launch_logits_process(const libscan_logits& p, void* out, int64_t out_row,
+                                 hipStream_t stream);
+hipError_t launch_logits_probs(const libscan_logits& p, float* probs, void* scratch,
+                               hipStream_t stream);
 
 }  // namespace ls

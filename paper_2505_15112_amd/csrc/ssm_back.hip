@@ -1,0 +1,370 @@
+// ssm_back.hip -- gradients of the selective scan.
+//
+// With G[t] the gradient of h[t] and w = dy silu(z):
+//   G[t] = w[t] C[t] + a[t+1] G[t+1]
+//   dC[t] = sum_d w h[t]            dB[t] = sum_d G[t] delta x
+//   du = sum_i G[t] B[t]            r = G[t] a[t] h[t-1]
+//   ddelta = sum_i r A + du x       dA = sum_t r delta
+//   dx = du delta + D w             ddt = ddelta softplus'(dt + dt_bias)
+// A workgroup owns CH channels of one row and walks the row backwards in
+// blocks of 16 steps, from the checkpoints that the forward pass left: h and a
+// of a block are formed again in registers, then the recurrence of G runs
+// through them.  Sums over a channel's states go to the block's outputs
+// through LDS; sums over channels (dB, dC) are reduced in the workgroup and
+// added over workgroups by a second kernel, in a fixed order.
+#include "launch.hpp"
+#include "lm.hpp"
+#include "ssm.hpp"
+
+namespace ls {
+
+namespace {
+
+constexpr int kThreads = 256;
+constexpr int kT = kSsmBlock;
+
+struct BackArgs {
+    const void* dy;
+    int64_t dy_batch, dy_step;
+    const float* ckpt;
+    const float* dstate_out;
+    void *dx, *ddt, *dz;
+    float* dstate;
+    float2* part_bc;  // [block of the group][batch][step][group][n] of (dB, dC)
+    float* part_a;    // [batch][dim][n]
+    float* part_d;    // [batch][dim]
+    float* part_bias; // [batch][dim]
+};
+
+template <class T, int LN, int SPL>
+__global__ __launch_bounds__(kThreads) void k_ssm_back(libscan_ssm p, BackArgs o, int nb) {
+    using L = SsmLanes<LN, SPL>;
+    constexpr int CH = L::CH, NP = L::NP, VW = CH / 16, YS = CH + 4;
+    constexpr int NBC = (kT * NP + kThreads - 1) / kThreads;
+    __shared__ float4 s_in[kT][CH];            // delta, delta x, w
+    __shared__ float2 s_bc[kT][NP];
+    __shared__ float s_y[kT][YS], s_du[kT][YS], s_dd[kT][YS];
+    __shared__ float2 s_g[4][kT][NP + 1];
+
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    const int steps = (int)p.steps, dim = (int)p.dim, n = (int)p.n, groups = (int)p.groups;
+    const SsmBlock k = ssm_block(p, nb, CH);
+    const int len = ssm_len(p, k.b);
+    const int blocks = (steps + kT - 1) / kT;
+
+    const int row = tid >> 4, lc = (tid & 15) * VW;
+    const int lcount = k.lim - lc;
+    const int64_t ch0 = k.c0 + lc;
+    const T* px = (const T*)p.x + k.b * p.x_batch + ch0;
+    const T* pdt = (const T*)p.dt + k.b * p.dt_batch + ch0;
+    const T* pz = p.z ? (const T*)p.z + k.b * p.z_batch + ch0 : nullptr;
+    const T* pdy = (const T*)o.dy + k.b * o.dy_batch + ch0;
+    const T* pB = (const T*)p.B + k.b * p.B_batch + k.g * p.B_group;
+    const T* pC = (const T*)p.C + k.b * p.C_batch + k.g * p.C_group;
+    const int64_t obase = (int64_t)k.b * steps * dim + ch0;
+    float bias[VW], skip[VW], sum_d[VW], sum_bias[VW];
+#pragma unroll
+    for (int i = 0; i < VW; ++i) {
+        bias[i] = p.dt_bias && i < lcount ? p.dt_bias[ch0 + i] : 0.0f;
+        skip[i] = p.D && i < lcount ? p.D[ch0 + i] : 0.0f;
+        sum_d[i] = sum_bias[i] = 0.0f;
+    }
+
+    const int wc = wave * L::CPW + L::channel(lane), n0 = L::part(lane) * SPL;
+    float a2[SPL], da[SPL], cg[SPL];  // cg: a[t+1] G[t+1] of the step that follows
+    const int64_t sbase = ((int64_t)k.b * dim + k.c0 + wc) * n + n0;
+#pragma unroll
+    for (int s = 0; s < SPL; ++s) {
+        const bool in = wc < k.lim && n0 + s < n;
+        a2[s] = in ? p.A[(int64_t)(k.c0 + wc) * n + n0 + s] * kLog2e : 0.0f;
+        cg[s] = in && o.dstate_out ? o.dstate_out[sbase + s] : 0.0f;
+        da[s] = 0.0f;
+    }
+
+    // the steps past the row's tokens
+    for (int t = (len + kT - 1) / kT * kT + row; t < steps; t += kT) {
+        Pack<T, VW> zero;
+#pragma unroll
+        for (int i = 0; i < VW; ++i) zero.v[i] = T(0);
+        const int64_t at = obase + (int64_t)t * dim;
+        zero.store((T*)o.dx + at, lcount);
+        zero.store((T*)o.ddt + at, lcount);
+        if (pz) zero.store((T*)o.dz + at, lcount);
+    }
+
+    for (int blk = (len + kT - 1) / kT - 1; blk >= 0; --blk) {
+        const int t0 = blk * kT;
+        const bool live = t0 + row < len;
+        const int count = live ? lcount : 0;
+        Pack<T, VW> rx, rdt, rz, rdy;
+        rx.load(px + (t0 + row) * p.x_step, count);
+        rdt.load(pdt + (t0 + row) * p.dt_step, count);
+        rz.load(pz + (t0 + row) * p.z_step, pz ? count : 0);
+        rdy.load(pdy + (t0 + row) * o.dy_step, count);
+#pragma unroll
+        for (int i = 0; i < NBC; ++i) {
+            const int e = tid + i * kThreads, tt = e / NP, nn = e % NP;
+            if (kT * NP % kThreads == 0 || e < kT * NP) {
+                const bool in = t0 + tt < len && nn < n;
+                s_bc[tt][nn] = float2{in ? to_f32(pB[(t0 + tt) * p.B_step + nn]) : 0.0f,
+                                      in ? to_f32(pC[(t0 + tt) * p.C_step + nn]) : 0.0f};
+            }
+        }
+        float delta[VW], w[VW];
+#pragma unroll
+        for (int i = 0; i < VW; ++i) {
+            float d = to_f32(rdt.v[i]) + bias[i];
+            if (p.softplus) d = softplus(d);
+            delta[i] = live && i < lcount ? d : 0.0f;
+            const float z = to_f32(rz.v[i]);
+            w[i] = to_f32(rdy.v[i]) * (pz ? z * sigmoid(z) : 1.0f);
+            s_in[row][lc + i] = float4{delta[i], delta[i] * to_f32(rx.v[i]), w[i], 0.0f};
+        }
+        __syncthreads();
+
+        float h[kT][SPL], a[kT][SPL], h0[SPL];
+        {
+            const float* pc = o.ckpt + (((int64_t)k.b * blocks + blk) * dim + k.c0 + wc) * n + n0;
+#pragma unroll
+            for (int s = 0; s < SPL; ++s) h0[s] = wc < k.lim && n0 + s < n ? pc[s] : 0.0f;
+            float hr[SPL], v[kT];
+#pragma unroll
+            for (int s = 0; s < SPL; ++s) hr[s] = h0[s];
+#pragma unroll
+            for (int t = 0; t < kT; ++t) {
+                const float4 in = s_in[t][wc];
+                float acc = 0.0f;
+#pragma unroll
+                for (int s = 0; s < SPL; ++s) {
+                    const float2 bc = s_bc[t][n0 + s];
+                    a[t][s] = exp2_fast(in.x * a2[s]);
+                    hr[s] = __builtin_fmaf(a[t][s], hr[s], in.y * bc.x);
+                    h[t][s] = hr[s];
+                    acc = __builtin_fmaf(hr[s], bc.y, acc);
+                }
+                v[t] = acc;
+            }
+            if (pz) L::sum_states(v, lane, [&](int t, float sum) { s_y[t][wc] = sum; });
+#pragma unroll
+            for (int s = 0; s < SPL; ++s) {
+#pragma unroll
+                for (int t = 0; t < kT; ++t) v[t] = s_in[t][wc].z * h[t][s];
+                L::sum_channels(v, lane, [&](int t, float sum) { s_g[wave][t][n0 + s].y = sum; });
+            }
+        }
+        {
+            float vu[kT], vd[kT];
+#pragma unroll
+            for (int t = kT - 1; t >= 0; --t) {
+                const float4 in = s_in[t][wc];
+                float du = 0.0f, dd = 0.0f;
+#pragma unroll
+                for (int s = 0; s < SPL; ++s) {
+                    const float2 bc = s_bc[t][n0 + s];
+                    const float g = __builtin_fmaf(in.z, bc.y, cg[s]);
+                    du = __builtin_fmaf(g, bc.x, du);
+                    cg[s] = a[t][s] * g;
+                    const float r = cg[s] * (t ? h[t ? t - 1 : 0][s] : h0[s]);
+                    dd = __builtin_fmaf(r, a2[s], dd);
+                    da[s] = __builtin_fmaf(r, in.x, da[s]);
+                    h[t][s] = g * in.y;  // dB; h[t] is done with
+                }
+                vu[t] = du;
+                vd[t] = dd;
+            }
+            L::sum_states(vu, lane, [&](int t, float sum) { s_du[t][wc] = sum; });
+            L::sum_states(vd, lane, [&](int t, float sum) { s_dd[t][wc] = sum; });
+        }
+#pragma unroll
+        for (int s = 0; s < SPL; ++s) {
+            float v[kT];
+#pragma unroll
+            for (int t = 0; t < kT; ++t) v[t] = h[t][s];
+            L::sum_channels(v, lane, [&](int t, float sum) { s_g[wave][t][n0 + s].x = sum; });
+        }
+        __syncthreads();
+
+        if (t0 + row < steps) {
+            Pack<T, VW> ox, odt, oz;
+#pragma unroll
+            for (int i = 0; i < VW; ++i) {
+                const float x = to_f32(rx.v[i]), du = s_du[row][lc + i];
+                const float v = to_f32(rdt.v[i]) + bias[i];
+                float ddt = __builtin_fmaf(du, x, s_dd[row][lc + i] * kLn2);
+                if (p.softplus) ddt *= sigmoid(v);
+                const float dx = __builtin_fmaf(du, delta[i], skip[i] * w[i]);
+                ox.v[i] = from_f32<T>(live ? dx : 0.0f);
+                odt.v[i] = from_f32<T>(live ? ddt : 0.0f);
+                if (pz) {
+                    const float z = to_f32(rz.v[i]), sig = sigmoid(z);
+                    const float yv = s_y[row][lc + i] + skip[i] * x;
+                    const float dz = to_f32(rdy.v[i]) * yv * sig * (1.0f + z * (1.0f - sig));
+                    oz.v[i] = from_f32<T>(live ? dz : 0.0f);
+                }
+                if (live && i < lcount) {
+                    sum_d[i] = __builtin_fmaf(w[i], x, sum_d[i]);
+                    sum_bias[i] += ddt;
+                }
+            }
+            const int64_t at = obase + (int64_t)(t0 + row) * dim;
+            ox.store((T*)o.dx + at, lcount);
+            odt.store((T*)o.ddt + at, lcount);
+            if (pz) oz.store((T*)o.dz + at, lcount);
+        }
+        for (int e = tid; e < kT * NP; e += kThreads) {
+            const int tt = e / NP, nn = e % NP;
+            if (nn < n && t0 + tt < len) {
+                float2 sum = s_g[0][tt][nn];
+#pragma unroll
+                for (int wv = 1; wv < 4; ++wv) {
+                    sum.x += s_g[wv][tt][nn].x;
+                    sum.y += s_g[wv][tt][nn].y;
+                }
+                o.part_bc[((((int64_t)k.k * p.batch + k.b) * steps + t0 + tt) * groups + k.g) * n +
+                          nn] = sum;
+            }
+        }
+    }
+
+#pragma unroll
+    for (int s = 0; s < SPL; ++s)
+        if (wc < k.lim && n0 + s < n) {
+            if (o.dstate) o.dstate[sbase + s] = cg[s];
+            o.part_a[sbase + s] = da[s];
+        }
+    // dD and ddt_bias: the 16 threads of each channel, in order
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < VW; ++i) {
+        s_y[row][lc + i] = sum_d[i];
+        s_du[row][lc + i] = sum_bias[i];
+    }
+    __syncthreads();
+    if (tid < k.lim) {
+        float d = 0.0f, e = 0.0f;
+        for (int r = 0; r < 16; ++r) {
+            d += s_y[r][tid];
+            e += s_du[r][tid];
+        }
+        o.part_d[(int64_t)k.b * dim + k.c0 + tid] = d;
+        o.part_bias[(int64_t)k.b * dim + k.c0 + tid] = e;
+    }
+}
+
+// dB and dC: the workgroups' sums of a group, added in order.
+template <class T>
+__global__ __launch_bounds__(kThreads) void k_ssm_sum_bc(libscan_ssm p, const float2* part, int nb,
+                                                         T* dB, T* dC) {
+    const int64_t per_step = p.groups * p.n, total = p.batch * p.steps * per_step;
+    const int64_t i = (int64_t)blockIdx.x * kThreads + threadIdx.x;
+    if (i >= total) return;
+    const int64_t bt = i / per_step;
+    const int b = (int)(bt / p.steps), t = (int)(bt % p.steps);
+    float2 sum{0.0f, 0.0f};
+    if (t < ssm_len(p, b)) {
+#pragma unroll 8
+        for (int k = 0; k < nb; ++k) {
+            const float2 v = part[k * total + i];
+            sum.x += v.x;
+            sum.y += v.y;
+        }
+    }
+    dB[i] = from_f32<T>(sum.x);
+    dC[i] = from_f32<T>(sum.y);
+}
+
+// The rows' sums of dA, dD and ddt_bias, added in order.
+__global__ __launch_bounds__(kThreads) void k_ssm_sum_rows(int64_t batch, int64_t dim, int64_t n,
+                                                           const float* part_a,
+                                                           const float* part_d,
+                                                           const float* part_bias, float* dA,
+                                                           float* dD, float* ddt_bias) {
+    const int64_t i = (int64_t)blockIdx.x * kThreads + threadIdx.x;
+    if (i < dim * n) {
+        float sum = 0.0f;
+        for (int64_t b = 0; b < batch; ++b) sum += part_a[b * dim * n + i];
+        dA[i] = sum;
+    }
+    if (i < dim) {
+        float d = 0.0f, e = 0.0f;
+        for (int64_t b = 0; b < batch; ++b) {
+            d += part_d[b * dim + i];
+            e += part_bias[b * dim + i];
+        }
+        if (dD) dD[i] = d;
+        if (ddt_bias) ddt_bias[i] = e;
+    }
+}
+
+// Which lanes a problem takes, the same for the sizes and the launch.
+bool wide(const libscan_ssm& p) { return p.n <= 16 && p.batch * p.dim >= 8192; }
+
+size_t align16(size_t v) { return (v + 15) / 16 * 16; }
+
+template <class T, int LN, int SPL>
+void back_as(const libscan_ssm& p, const BackArgs& o, int nb, hipStream_t stream) {
+    const int64_t grid = p.batch * p.groups * nb;
+    if (grid > 0) k_ssm_back<T, LN, SPL><<<dim3((unsigned)grid), kThreads, 0, stream>>>(p, o, nb);
+}
+
+template <class T>
+hipError_t back_type(const libscan_ssm& p, const BackArgs& o, float* dA, T* dB, T* dC, float* dD,
+                     float* ddt_bias, hipStream_t stream) {
+    const int nb = ssm_blocks(p, wide(p) ? 64 : 16);
+    if (p.n > 32)
+        back_as<T, 16, 4>(p, o, nb, stream);
+    else if (p.n > 16)
+        back_as<T, 16, 2>(p, o, nb, stream);
+    else if (wide(p))
+        back_as<T, 4, 4>(p, o, nb, stream);
+    else
+        back_as<T, 16, 1>(p, o, nb, stream);
+    const int64_t bc = p.batch * p.steps * p.groups * p.n;
+    if (bc > 0)
+        k_ssm_sum_bc<T><<<dim3((unsigned)((bc + kThreads - 1) / kThreads)), kThreads, 0, stream>>>(
+            p, o.part_bc, nb, dB, dC);
+    const int64_t rows = p.dim * p.n;
+    if (rows > 0)
+        k_ssm_sum_rows<<<dim3((unsigned)((rows + kThreads - 1) / kThreads)), kThreads, 0, stream>>>(
+            p.batch, p.dim, p.n, o.part_a, o.part_d, o.part_bias, dA, dD, ddt_bias);
+    return hipGetLastError();
+}
+
+}  // namespace
+
+size_t ssm_ckpt_bytes(const libscan_ssm& p) {
+    return (size_t)p.batch * ((p.steps + kT - 1) / kT) * p.dim * p.n * 4;
+}
+
+size_t ssm_back_scratch_bytes(const libscan_ssm& p) {
+    const size_t nb = ssm_blocks(p, wide(p) ? 64 : 16);
+    return align16(nb * p.batch * p.steps * p.groups * p.n * 8) +
+           align16((size_t)p.batch * p.dim * p.n * 4) + 2 * align16((size_t)p.batch * p.dim * 4);
+}
+
+hipError_t launch_ssm_back(const libscan_ssm& p, const void* dy, int64_t dy_batch, int64_t dy_step,
+                           const float* ckpt, const float* dstate_out, void* dx, void* ddt,
+                           float* dA, void* dB, void* dC, float* dD, void* dz, float* ddt_bias,
+                           float* dstate, void* scratch, hipStream_t stream) {
+    const size_t nb = ssm_blocks(p, wide(p) ? 64 : 16);
+    char* s = (char*)scratch;
+    BackArgs o{dy, dy_batch, dy_step, ckpt, dstate_out, dx, ddt, dz, dstate,
+               nullptr, nullptr, nullptr, nullptr};
+    o.part_bc = (float2*)s;
+    s += align16(nb * p.batch * p.steps * p.groups * p.n * 8);
+    o.part_a = (float*)s;
+    s += align16((size_t)p.batch * p.dim * p.n * 4);
+    o.part_d = (float*)s;
+    s += align16((size_t)p.batch * p.dim * 4);
+    o.part_bias = (float*)s;
+    switch (p.type) {
+        case LIBSCAN_F16:
+            return back_type<_Float16>(p, o, dA, (_Float16*)dB, (_Float16*)dC, dD, ddt_bias, stream);
+        case LIBSCAN_BF16:
+            return back_type<__bf16>(p, o, dA, (__bf16*)dB, (__bf16*)dC, dD, ddt_bias, stream);
+        default:
+            return back_type<float>(p, o, dA, (float*)dB, (float*)dC, dD, ddt_bias, stream);
+    }
+}
+
+}  // namespace ls

@@ -1,0 +1,231 @@
+"""Penalties, biases, grammar masks and the softmax behind them against the
+definition in 64 bits (lm_ref.py, where the bounds are derived)."""
+import pytest
+import torch
+
+import lm_ref as R
+from gpu_util import announce
+from paper_2505_15112_amd import _lib, ops
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda"
+F32, F16, BF16 = torch.float32, torch.float16, torch.bfloat16
+
+
+def inputs(rows, vocab, kind=F32, hist=0, biases=0, grammar=False, seed=0):
+    g = torch.Generator().manual_seed(seed)
+    a = dict(logits=(torch.randn(rows, vocab, generator=g) * 4).to(kind))
+    if hist:
+        a["history"] = torch.randint(-2, vocab + 2, (rows, hist), generator=g).int()
+        a["history"][:, hist // 2:] = torch.randint(0, min(vocab, 7), (rows, hist - hist // 2),
+                                                    generator=g).int()
+        a["history_len"] = torch.randint(0, hist + 1, (rows,), generator=g).int()
+        a["prompt_len"] = torch.randint(0, hist + 1, (rows,), generator=g).int()
+        a["repetition"] = torch.rand(rows, generator=g) + 0.7
+        a["presence"] = torch.rand(rows, generator=g)
+        a["frequency"] = torch.rand(rows, generator=g) * 0.3
+    if biases:
+        # ids repeat and fall outside
+        a["bias_ids"] = torch.randint(-1, vocab + 1, (rows, biases), generator=g).int()
+        a["bias_ids"][:, biases // 2] = a["bias_ids"][:, 0]
+        a["bias_values"] = torch.randn(rows, biases, generator=g) * 3
+    if grammar:
+        a["allowed"] = torch.randint(-2**31, 2**31, (rows, (vocab + 31) // 32), generator=g).int()
+    return a
+
+
+def dev(a):
+    return {k: v.to(DEV) for k, v in a.items()}
+
+
+def ref(a):
+    a = {k: v.double() if v.is_floating_point() else v for k, v in a.items()}
+    return R.logits(a.pop("logits"), **a)
+
+
+def check(a, temperature=None):
+    announce("logits", tuple(a["logits"].shape), a["logits"].dtype, sorted(a))
+    x, mag = ref(a)
+    got = ops.logits_process(**dev(a))
+    inf = x == R.NEG_INF
+    assert torch.equal(got.cpu() == R.NEG_INF, inf)
+    R.assert_within(got.masked_fill(inf.to(DEV), 0), x.masked_fill(inf, 0), mag, 8, "logits")
+    d = dev(a)
+    same = ops.logits_process(**dict(d, out=d["logits"]))  # in place
+    assert torch.equal(same, got)
+    p = ops.logits_probs(**dev(a),
+                         temperature=temperature.to(DEV) if temperature is not None else None)
+    want = R.probs(x, temperature)
+    # the exponent's argument is off by its own size's roundings; so much for p
+    t = torch.ones(x.shape[0]) if temperature is None else temperature
+    size = (mag.max(1, keepdim=True).values + mag) / t.double()[:, None].clamp(min=1e-30)
+    # the sum's roundings: one for each of the at most 64 places a thread adds,
+    # and a few over threads and segments
+    R.assert_within(p, want, want * (8 * size + 128), 1, "probs")
+    assert not p.cpu()[inf].any()
+
+
+@pytest.mark.parametrize("rows,vocab", [(1, 1), (3, 2), (2, 31), (5, 33), (2, 1000), (3, 8191),
+                                        (2, 8192), (2, 8193), (1, 20001), (3, 50257)])
+@pytest.mark.parametrize("kind", [F32, F16, BF16])
+def test_all_parts(rows, vocab, kind):
+    check(inputs(rows, vocab, kind, hist=50, biases=9, grammar=True),
+          torch.linspace(0.3, 1.5, rows))
+
+
+@pytest.mark.parametrize("hist,biases,grammar", [(0, 0, False), (30, 0, False), (0, 5, False),
+                                                 (0, 0, True), (1, 1, False)])
+@pytest.mark.parametrize("vocab", [700, 9001])
+def test_parts_alone(hist, biases, grammar, vocab):
+    check(inputs(4, vocab, BF16, hist, biases, grammar))
+
+
+def test_history_defaults_and_long_history():
+    """No lengths: all columns are generated tokens; counts beyond 16 bits."""
+    a = inputs(2, 300, F32, hist=90000)
+    a["history"][1] = 5
+    for k in ("history_len", "prompt_len", "presence"):
+        del a[k]
+    check(a)
+
+
+def test_many_rows():
+    check(inputs(700, 300, F16, hist=20, biases=3, grammar=True))
+
+
+def test_rows_that_the_mask_leaves_empty():
+    a = inputs(4, 20000, F32, grammar=True)
+    a["allowed"][1] = 0
+    a["allowed"][2] = 0
+    a["allowed"][2, 600] = 1 << 7
+    p = ops.logits_probs(**dev(a)).cpu()
+    assert not p[1].any()
+    assert p[2, 600 * 32 + 7] == 1 and p[2].sum() == 1
+    check(a)
+
+
+def test_special_values():
+    """The type's lowest value, infinities and NaN, in masked and open places."""
+    a = inputs(8, 9000, F32, grammar=True)
+    x, al = a["logits"], a["allowed"]
+    al[:] = -1
+    x[0, 5] = float("nan")
+    al[0, 0] = ~(1 << 5)                    # masked: no trace of it
+    x[1, 8500] = float("inf")
+    al[1, 8500 // 32] = ~(1 << (8500 % 32))
+    x[2, :] = torch.finfo(F32).min          # equal shares of the lowest value
+    x[3, 10] = R.NEG_INF                    # open, but nothing there
+    x[4, 20] = float("nan")
+    x[5, 30] = float("inf")
+    x[6, :] = R.NEG_INF
+    x[7, :8999] = R.NEG_INF
+    p = ops.logits_probs(**dev(a)).cpu()
+    want = R.probs(*ref(a)[:1])
+    assert torch.equal(p.isnan(), want.isnan())
+    assert p[4].isnan().all() and p[5].isnan().all() and not p[6].any() and p[7, 8999] == 1
+    ok = [0, 1, 2, 3, 7]
+    R.assert_within(p[ok], want[ok], want[ok] * 400, 1, "probs")
+    hot = torch.zeros(8)
+    cold = ops.logits_probs(**dev(a), temperature=hot.to(DEV)).cpu()
+    wcold = R.probs(ref(a)[0], hot)
+    assert torch.equal(cold.isnan(), wcold.isnan()) and cold[5, 30] == 1
+    assert ((cold - wcold).nan_to_num().abs() <= 2.0**-23 * wcold.nan_to_num()).all()
+
+
+def test_low_masks_of_half_types():
+    for kind in (F16, BF16):
+        a = inputs(2, 600, kind)
+        a["logits"][0, :599] = torch.finfo(kind).min
+        a["logits"][1, :] = torch.finfo(kind).min
+        p = ops.logits_probs(**dev(a)).cpu()
+        assert p[0, 599] == 1 and not p[0, :599].any()
+        R.assert_within(p[1], torch.full((600,), 1 / 600).double(), torch.full((600,), 1 / 600), 64,
+                        "equal")
+
+
+def test_temperature_zero_shares_ties():
+    a = inputs(2, 10000, F32)
+    a["logits"][0, [3, 9000]] = 50.0
+    p = ops.logits_probs(**dev(a), temperature=torch.tensor([0.0, 1.0], device=DEV)).cpu()
+    assert p[0, 3] == 0.5 and p[0, 9000] == 0.5 and p[0].sum() == 1
+    assert abs(float(p[1].double().sum()) - 1) < 1e-5
+
+
+@pytest.mark.parametrize("vocab", [999, 16385])
+def test_strides(vocab):
+    a = inputs(3, vocab, BF16, hist=12, grammar=True)
+    d = dev(a)
+    want = ops.logits_process(**d)
+    big = torch.full((3, vocab + 7), float("nan"), dtype=BF16, device=DEV)
+    big[:, 3:3 + vocab] = d["logits"]
+    hist = torch.full((3, 20), 1, dtype=torch.int32, device=DEV)
+    hist[:, 4:16] = d["history"]
+    allowed = torch.zeros(3, d["allowed"].shape[1] + 1, dtype=torch.int32, device=DEV)
+    allowed[:, 1:] = d["allowed"]
+    s = dict(d, logits=big[:, 3:3 + vocab], history=hist[:, 4:16], allowed=allowed[:, 1:])
+    assert torch.equal(ops.logits_process(**s), want)
+    assert torch.equal(ops.logits_probs(**s), ops.logits_probs(**d))
+    into = torch.zeros(3, vocab + 5, dtype=BF16, device=DEV)
+    ops.logits_process(**s, out=into[:, 2:2 + vocab])
+    assert torch.equal(into[:, 2:2 + vocab], want)
+    assert not into[:, :2].any() and not into[:, 2 + vocab:].any()
+
+
+def test_empty():
+    for rows, vocab in ((0, 10), (3, 0)):
+        x = torch.zeros(rows, vocab, device=DEV)
+        assert ops.logits_process(x).shape == (rows, vocab)
+        assert ops.logits_probs(x).shape == (rows, vocab)
+
+
+def test_probabilities_go_into_the_sampler():
+    """A grammar's tokens only, and the most likely at temperature 0."""
+    a = inputs(16, 40000, BF16, hist=64, biases=4, grammar=True)
+    d = dev(a)
+    p = ops.logits_probs(**d, temperature=torch.full((16,), 0.8, device=DEV))
+    tok = ops.topp_sample_f32(p, torch.rand(16, device=DEV), 0.9).cpu().long()
+    bits = (a["allowed"].gather(1, (tok // 32)[:, None])[:, 0] >> (tok % 32)) & 1
+    assert bits.all()
+    cold = ops.logits_probs(**d, temperature=torch.zeros(16, device=DEV))
+    tok = ops.topp_sample_f32(cold, torch.rand(16, device=DEV) * 0.4, 0.9).cpu().long()
+    best = ops.logits_process(**dict(d, logits=d["logits"].float())).cpu()
+    assert torch.equal(best.gather(1, tok[:, None])[:, 0], best.max(1).values)
+
+
+def test_in_a_graph():
+    a = dev(inputs(4, 30000, BF16, hist=40, grammar=True))
+    want = ops.logits_probs(**a)
+    out = torch.empty_like(want)
+    buf = torch.empty(1 << 16, dtype=torch.uint8, device=DEV)
+    ops.logits_probs(**a, out=out, scratch_buf=buf)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        ops.logits_probs(**a, out=out, scratch_buf=buf)
+    for i in range(4):
+        out.zero_()
+        buf.fill_(i)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(out, want)
+
+
+def test_refusals():
+    a = dev(inputs(2, 100, F32, hist=5, biases=3, grammar=True))
+    bad = [(dict(logits=a["logits"].double()), TypeError), (dict(logits=a["logits"][0]), ValueError),
+           (dict(history=a["history"].long()), TypeError), (dict(history=None), ValueError),
+           (dict(history_len=a["history_len"][:1]), ValueError),
+           (dict(repetition=a["repetition"].half()), TypeError),
+           (dict(bias_ids=None), ValueError), (dict(bias_values=a["bias_values"][:, :2]), ValueError),
+           (dict(allowed=a["allowed"][:, :3]), ValueError), (dict(presence=1.0), TypeError),
+           (dict(allowed=a["allowed"].cpu()), ValueError),
+           (dict(out=torch.empty(2, 99, device=DEV)), ValueError)]
+    for change, error in bad:
+        with pytest.raises(error):
+            ops.logits_process(**dict(a, **change))
+    with pytest.raises(_lib.LibscanError):  # over its input, a place further on
+        buf = torch.zeros(2 * 100 + 1, device=DEV)
+        ops.logits_process(buf[:200].view(2, 100), out=buf[1:].view(2, 100))
+    with pytest.raises(_lib.LibscanError):  # too little scratch
+        ops.logits_probs(torch.zeros(2, 50000, device=DEV),
+                         scratch_buf=torch.empty(16, dtype=torch.uint8, device=DEV))
