@@ -61,15 +61,15 @@ __device__ __forceinline__ float sigmoid(float v) {
     return rcp_fast(1.0f + exp2_fast(-v * kLog2e));
 }
 
-// log(1 + e^v) = max(v, 0) + log1p(e^-|v|), with log1p(e) = log(w) e / (w - 1),
-// w = 1 + e rounded: the quotient takes the rounding of w back out (step sizes
-// near e^-7 would otherwise lose half their bits).
+// log(1 + e^v) = max(v, 0) + log(1 + e), e = e^-|v|.  w = 1 + e is rounded; what it
+// lost, c = e - (w - 1), is put back as log(w + c) = log(w) + c / w, with c for c / w
+// (c <= 2^-24, and w is near 1 where c counts).  Step sizes near e^-7 would
+// otherwise lose half their bits.  A NaN, which the maximum drops, stays in e.
 __device__ __forceinline__ float softplus(float v) {
     const float e = exp2_fast(-__builtin_fabsf(v) * kLog2e);
     const float w = 1.0f + e;
-    const float d = w - 1.0f;
-    const float l = d > 0.0f ? __builtin_amdgcn_logf(w) * kLn2 * (e * rcp_fast(d)) : e;
-    return __builtin_fmaxf(v, 0.0f) + l;  // the maximum drops a NaN, l keeps it
+    const float c = e - (w - 1.0f);
+    return __builtin_fmaf(__builtin_amdgcn_logf(w), kLn2, c) + __builtin_fmaxf(v, 0.0f);
 }
 
 // ------------------------------------------------ reductions inside a wave

@@ -31,7 +31,7 @@ __global__ __launch_bounds__(kThreads) void k_ssm_scan(libscan_ssm p, T* y, floa
 
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     const int steps = (int)p.steps, dim = (int)p.dim, n = (int)p.n;
-    const SsmBlock k = ssm_block(p, nb, CH);
+    const SsmBlock k = ssm_block(p, nb, CH, blockIdx.x);
     const int len = ssm_len(p, k.b);
 
     // loader: one step, VW channels
@@ -153,6 +153,355 @@ __global__ __launch_bounds__(kThreads) void k_ssm_scan(libscan_ssm p, T* y, floa
     }
 }
 
+// ---------------------------------------------------------------- long rows
+
+typedef const __attribute__((address_space(4))) float* ScalarPtr;
+
+// B and C as fp32, in groups of GP states (GP of B, then GP of C; padding and the
+// steps past a row's tokens are 0), as the scanning waves read them with scalar
+// loads: one group at a time, the next one on its way while the last is used.
+template <int NP>
+struct LaneGroups {
+    static constexpr int GP = NP < 16 ? NP : 16, NG = NP / GP;
+    float v[2 * GP];
+    template <int COUNT>
+    __device__ __forceinline__ void load(ScalarPtr p) {
+        asm volatile("" : "+s"(p));  // not earlier than here
+#pragma unroll
+        for (int i = 0; i < COUNT; ++i) v[i] = p[i];
+    }
+};
+
+template <class T, int NP>
+__global__ __launch_bounds__(kThreads) void k_ssm_bc(libscan_ssm p, float* bc) {
+    constexpr int GP = LaneGroups<NP>::GP;
+    const int64_t i = (int64_t)blockIdx.x * kThreads + threadIdx.x;
+    if (i >= p.batch * p.steps * p.groups * NP) return;
+    const int nn = (int)(i % NP);
+    const int64_t tok = i / NP, bt = tok / p.groups;
+    const int g = (int)(tok % p.groups), b = (int)(bt / p.steps), t = (int)(bt % p.steps);
+    const bool in = nn < p.n && t < ssm_len(p, b);
+    const T* pB = (const T*)p.B + b * p.B_batch + t * p.B_step + g * p.B_group;
+    const T* pC = (const T*)p.C + b * p.C_batch + t * p.C_step + g * p.C_group;
+    float* out = bc + tok * 2 * NP + nn / GP * 2 * GP + nn % GP;
+    out[0] = in ? to_f32(pB[nn]) : 0.0f;
+    out[GP] = in ? to_f32(pC[nn]) : 0.0f;
+}
+
+// Waits for the scalar loads in flight, which return in no order, before new
+// ones start, and keeps the compiler from mixing the two.
+__device__ __forceinline__ void scalar_loads_done() {
+    __builtin_amdgcn_sched_barrier(0);
+    __builtin_amdgcn_s_waitcnt(0xC07F);  // lgkmcnt(0)
+    __builtin_amdgcn_sched_barrier(0);
+}
+
+// Waves of a workgroup: neighbours in channels, on the same steps, so that all
+// but the first to get there find B and C in the scalar cache.
+constexpr int kLaneWaves = 8;
+
+// The channel block and chunk of steps of a wave.
+struct LaneBlock {
+    SsmBlock k;
+    int c, t0, end, len;  // steps t0 .. end of chunk c are this wave's; end <= len
+    uint32_t lo;          // this lane's channel after k.c0; lanes past the last channel double
+                          // it, and store what it stores
+};
+__device__ __forceinline__ LaneBlock lane_block(const libscan_ssm& p, int nb, int chunk) {
+    LaneBlock r;
+    r.k = ssm_block(p, nb, kWave, blockIdx.x * kLaneWaves + uni(threadIdx.x / kWave));
+    r.c = blockIdx.y;
+    r.len = ssm_len(p, r.k.b);
+    r.t0 = r.c * chunk;
+    r.end = r.t0 + chunk < r.len ? r.t0 + chunk : r.len;
+    const int lane = threadIdx.x % kWave;
+    r.lo = (uint32_t)(lane < r.k.lim ? lane : r.k.lim - 1);
+    return r;
+}
+
+// A row of a tensor at one step after the other: the address is uniform and
+// stays in one pair of scalar registers (the empty asm keeps the compiler from
+// holding the multiples of the stride instead), the lanes add their channel.
+template <class T>
+struct StepPtr {
+    __attribute__((address_space(1))) T* p;
+    int64_t stride;
+    __device__ __forceinline__ StepPtr(T* first, int64_t step)
+        : p((__attribute__((address_space(1))) T*)first), stride(step) {}
+    __device__ __forceinline__ void next() {
+        p += stride;
+        asm("" : "+s"(p));
+    }
+};
+
+// The step sizes of COUNT steps, in the lane that owns the channel (one branch
+// for all of them: branches between the steps would keep them apart).
+template <int COUNT, class T>
+__device__ __forceinline__ void step_sizes(const libscan_ssm& p, const T (&dt)[COUNT], float bias,
+                                           float (&delta)[COUNT]) {
+#pragma unroll
+    for (int i = 0; i < COUNT; ++i) delta[i] = to_f32(dt[i]) + bias;
+    if (p.softplus) {
+#pragma unroll
+        for (int i = 0; i < COUNT; ++i) delta[i] = softplus(delta[i]);
+    }
+}
+
+constexpr int kAhead = 8;  // steps whose inputs a lane loads together
+
+// A lane's states (or rates): `have` consecutive floats, 0 after them.
+template <int NP>
+__device__ __forceinline__ void load_states(const float* p, int have, float (&v)[NP]) {
+#pragma unroll
+    for (int i = 0; i < NP; i += 4) {
+        Pack<float, 4> w;
+        w.load(p + i, have - i);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) v[i + j] = w.v[j];
+    }
+}
+template <int NP>
+__device__ __forceinline__ void store_states(float* p, int have, const float (&v)[NP]) {
+#pragma unroll
+    for (int i = 0; i < NP; i += 4) {
+        Pack<float, 4> w;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) w.v[j] = v[i + j];
+        w.store(p + i, have - i);
+    }
+}
+
+// The scan with a channel to a lane, all of its states in registers, and one
+// wave to a workgroup: B and C are the same for all lanes and come by scalar
+// loads, so that a step costs five vector instructions for each state (one of
+// them the exponential) and nothing goes through LDS.  Rows are cut into
+// chunks until the waves fill the chip; `starts` (NULL for one chunk) holds
+// the states that the chunks start from.
+template <class T, int NP, bool GATE>
+__global__ __launch_bounds__(kWave * kLaneWaves) void k_ssm_lanes(libscan_ssm p, const float* bc_,
+                                                     const float* starts, T* y, float* state_out,
+                                                     float* ckpt, int nb, int chunk,
+                                                                uint32_t waves) {
+    using Groups = LaneGroups<NP>;
+    constexpr int GP = Groups::GP, NG = Groups::NG;
+    if (blockIdx.x * kLaneWaves + threadIdx.x / kWave >= waves) return;
+    const LaneBlock w = lane_block(p, nb, chunk);
+    const int b = w.k.b, c0 = w.k.c0, ch = c0 + (int)w.lo;
+    const uint32_t lo = w.lo;
+    const int dim = (int)p.dim, n = (int)p.n, steps = (int)p.steps;
+    const int64_t bc_step = p.groups * 2 * NP;
+    ScalarPtr bc = (ScalarPtr)bc_ + (((int64_t)b * steps + w.t0) * p.groups + w.k.g) * 2 * NP;
+    StepPtr<const T> px{(const T*)p.x + b * p.x_batch + w.t0 * p.x_step + c0, p.x_step};
+    StepPtr<const T> pdt{(const T*)p.dt + b * p.dt_batch + w.t0 * p.dt_step + c0, p.dt_step};
+    StepPtr<const T> pz{GATE ? (const T*)p.z + b * p.z_batch + w.t0 * p.z_step + c0 : nullptr,
+                        p.z_step};
+    StepPtr<T> py{y + ((int64_t)b * steps + w.t0) * dim + c0, dim};
+    const float bias = p.dt_bias ? p.dt_bias[ch] : 0.0f, skip = p.D ? p.D[ch] : 0.0f;
+    const int64_t row = (int64_t)b * dim + ch;
+    float a2[NP], h[NP];
+    {
+        const float* from = starts ? starts + ((int64_t)w.c * p.batch * dim + row) * NP
+                                   : p.state ? p.state + row * n : nullptr;
+        const int have = starts ? NP : p.state ? n : 0;
+        load_states<NP>(p.A + (int64_t)ch * n, n, a2);
+        load_states<NP>(from, have, h);
+#pragma unroll
+        for (int i = 0; i < NP; ++i) a2[i] *= kLog2e;
+    }
+
+    Groups cur;
+    if (w.t0 < w.end) cur.template load<2 * GP>(bc);
+    auto step = [&](T x, float delta, T z) {
+        const float u = delta * to_f32(x);
+        float acc[2] = {skip * to_f32(x), 0.0f};
+#pragma unroll
+        for (int g = 0; g < NG; ++g) {
+            scalar_loads_done();
+            Groups next;  // of this step, or the first of the next (one past the last is there)
+            if (g + 1 == NG) bc += bc_step;
+            next.template load<2 * GP>(g + 1 < NG ? bc + (g + 1) * 2 * GP : bc);
+            __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+            for (int i = 0; i < GP; ++i) {
+                float& hi = h[g * GP + i];
+                hi = __builtin_fmaf(exp2_fast(delta * a2[g * GP + i]), hi, u * cur.v[i]);
+                acc[i & 1] = __builtin_fmaf(hi, cur.v[GP + i], acc[i & 1]);
+            }
+            cur = next;
+        }
+        float v = acc[0] + acc[1];
+        if (GATE) {
+            const float zf = to_f32(z);
+            v *= zf * sigmoid(zf);
+        }
+        py.p[lo] = from_f32<T>(v);
+        py.next();
+    };
+    auto keep = [&](int t) {
+        if (!ckpt || t % kSsmBlock) return;
+        const int64_t blk = (int64_t)b * ((steps + kSsmBlock - 1) / kSsmBlock) + t / kSsmBlock;
+        store_states<NP>(ckpt + (blk * dim + ch) * n, n, h);
+    };
+
+    int t = w.t0;
+    T nx[kAhead], ndt[kAhead], nz[kAhead];
+    auto fetch = [&]() {
+#pragma unroll
+        for (int i = 0; i < kAhead; ++i) {
+            nx[i] = px.p[lo];
+            ndt[i] = pdt.p[lo];
+            nz[i] = GATE ? pz.p[lo] : T(0);
+            px.next();
+            pdt.next();
+            if (GATE) pz.next();
+        }
+    };
+    if (t + kAhead <= w.end) fetch();
+    for (; t + kAhead <= w.end; t += kAhead) {
+        T cx[kAhead], cz[kAhead];
+        float delta[kAhead];
+        step_sizes(p, ndt, bias, delta);
+#pragma unroll
+        for (int i = 0; i < kAhead; ++i) {
+            cx[i] = nx[i];
+            cz[i] = nz[i];
+        }
+        if (t + 2 * kAhead <= w.end) fetch();
+        keep(t);
+#pragma unroll
+        for (int i = 0; i < kAhead; ++i) step(cx[i], delta[i], cz[i]);
+    }
+#pragma unroll 1
+    for (; t < w.end; ++t) {
+        keep(t);
+        const T dt[1] = {pdt.p[lo]};
+        float delta[1];
+        step_sizes(p, dt, bias, delta);
+        step(px.p[lo], delta[0], GATE ? pz.p[lo] : T(0));
+        px.next();
+        pdt.next();
+        if (GATE) pz.next();
+    }
+    const int stop = w.t0 + chunk < steps ? w.t0 + chunk : steps;
+#pragma unroll 1
+    for (t = w.t0 > w.len ? w.t0 : w.len; t < stop; ++t) {
+        py.p[lo] = T(0);
+        py.next();
+    }
+    if (state_out && stop == steps) store_states<NP>(state_out + row * n, n, h);
+}
+
+// What a chunk does to any state it starts from: its decay exp(A sum delta) and
+// the state it ends in from zero.
+template <class T, int NP>
+__global__ __launch_bounds__(kWave * kLaneWaves) void k_ssm_ends(libscan_ssm p, const float* bc_, float* ends,
+                                                    float* sums, int nb, int chunk,
+                                                                uint32_t waves) {
+    using Groups = LaneGroups<NP>;
+    constexpr int GP = Groups::GP, NG = Groups::NG;
+    if (blockIdx.x * kLaneWaves + threadIdx.x / kWave >= waves) return;
+    const LaneBlock w = lane_block(p, nb, chunk);
+    const int b = w.k.b, c0 = w.k.c0, ch = c0 + (int)w.lo;
+    const uint32_t lo = w.lo;
+    const int dim = (int)p.dim, n = (int)p.n;
+    const int64_t bc_step = p.groups * 2 * NP;
+    ScalarPtr bc = (ScalarPtr)bc_ + (((int64_t)b * p.steps + w.t0) * p.groups + w.k.g) * 2 * NP;
+    StepPtr<const T> px{(const T*)p.x + b * p.x_batch + w.t0 * p.x_step + c0, p.x_step};
+    StepPtr<const T> pdt{(const T*)p.dt + b * p.dt_batch + w.t0 * p.dt_step + c0, p.dt_step};
+    const float bias = p.dt_bias ? p.dt_bias[ch] : 0.0f;
+    float a2[NP], h[NP], sum = 0.0f;
+    load_states<NP>(p.A + (int64_t)ch * n, n, a2);
+#pragma unroll
+    for (int i = 0; i < NP; ++i) {
+        a2[i] *= kLog2e;
+        h[i] = 0.0f;
+    }
+    Groups cur;
+    if (w.t0 < w.end) cur.template load<GP>(bc);
+    auto step = [&](T x, float delta) {
+        const float u = delta * to_f32(x);
+        sum += delta;
+#pragma unroll
+        for (int g = 0; g < NG; ++g) {
+            scalar_loads_done();
+            Groups next;
+            if (g + 1 == NG) bc += bc_step;
+            next.template load<GP>(g + 1 < NG ? bc + (g + 1) * 2 * GP : bc);
+            __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+            for (int i = 0; i < GP; ++i) {
+                float& hi = h[g * GP + i];
+                hi = __builtin_fmaf(exp2_fast(delta * a2[g * GP + i]), hi, u * cur.v[i]);
+            }
+            cur = next;
+        }
+    };
+    int t = w.t0;
+    T nx[kAhead], ndt[kAhead];
+    auto fetch = [&]() {
+#pragma unroll
+        for (int i = 0; i < kAhead; ++i) {
+            nx[i] = px.p[lo];
+            ndt[i] = pdt.p[lo];
+            px.next();
+            pdt.next();
+        }
+    };
+    if (t + kAhead <= w.end) fetch();
+    for (; t + kAhead <= w.end; t += kAhead) {
+        T cx[kAhead];
+        float delta[kAhead];
+        step_sizes(p, ndt, bias, delta);
+#pragma unroll
+        for (int i = 0; i < kAhead; ++i) cx[i] = nx[i];
+        if (t + 2 * kAhead <= w.end) fetch();
+#pragma unroll
+        for (int i = 0; i < kAhead; ++i) step(cx[i], delta[i]);
+    }
+#pragma unroll 1
+    for (; t < w.end; ++t) {
+        const T dt[1] = {pdt.p[lo]};
+        float delta[1];
+        step_sizes(p, dt, bias, delta);
+        step(px.p[lo], delta[0]);
+        px.next();
+        pdt.next();
+    }
+    const int64_t row = ((int64_t)w.c * p.batch + b) * dim + ch;
+    store_states<NP>(ends + row * NP, NP, h);
+    sums[row] = sum;
+}
+
+// The states that the chunks start from, in the place of the ends (of which
+// the last chunk has none).
+template <int NP>
+__global__ __launch_bounds__(kThreads) void k_ssm_starts(libscan_ssm p, float* ends,
+                                                         const float* sums, int chunks) {
+    const int64_t i = (int64_t)blockIdx.x * kThreads + threadIdx.x, rows = p.batch * p.dim;
+    if (i >= rows * NP) return;
+    const int64_t row = i / NP;
+    const int nn = (int)(i % NP);
+    const float a2 = nn < p.n ? p.A[row % p.dim * p.n + nn] * kLog2e : 0.0f;
+    float h = p.state && nn < p.n ? p.state[row * p.n + nn] : 0.0f;
+    constexpr int kBatch = 16;  // loads in flight together
+    for (int c0 = 0; c0 < chunks; c0 += kBatch) {
+        float e[kBatch], s[kBatch];
+#pragma unroll
+        for (int j = 0; j < kBatch; ++j) {
+            const bool in = c0 + j + 1 < chunks;
+            const int64_t at = (int64_t)(c0 + j) * rows;
+            e[j] = in ? ends[at * NP + i] : 0.0f;
+            s[j] = in ? sums[at + row] : 0.0f;
+        }
+#pragma unroll
+        for (int j = 0; j < kBatch; ++j)
+            if (c0 + j < chunks) {
+                ends[(int64_t)(c0 + j) * rows * NP + i] = h;
+                h = __builtin_fmaf(exp2_fast(s[j] * a2), h, e[j]);
+            }
+    }
+}
+
 // One token.  A quad of lanes owns a channel's states, four at a time: the
 // states, read and written once, are all the traffic that counts.
 template <class T>
@@ -218,18 +567,85 @@ hipError_t scan_as(const libscan_ssm& p, void* y, float* state_out, float* ckpt,
     return hipGetLastError();
 }
 
+// From so many channels on, the tiles of a quad per channel fill the chip
+// without cutting rows (n <= 16).
+constexpr int64_t kTileChannels = 16384;
+
+// How a call is cut up: `np` states to a lane and chunks of `chunk` steps.  np = 0:
+// the tiles, whose workgroups share a channel's states out over lanes.
+struct LanePlan {
+    int np, nb, chunk, chunks;
+    size_t bc, ends, sums;  // bytes of scratch
+};
+LanePlan lane_plan(const libscan_ssm& p) {
+    LanePlan r{0, 0, 0, 0, 0, 0, 0};
+    if (p.batch == 0 || p.dim == 0) return r;
+    const int64_t per = p.dim / p.groups;
+    if (p.steps < 64 || per < 48 || (p.n <= 16 && p.batch * p.dim >= kTileChannels)) return r;
+    r.np = p.n <= 8 ? 8 : p.n <= 16 ? 16 : p.n <= 32 ? 32 : 64;
+    r.nb = ssm_blocks(p, kWave);
+    const int64_t waves = p.batch * p.groups * r.nb;
+    int64_t chunks = (4096 + waves - 1) / waves;  // 4 waves to each of the 1024 SIMDs
+    if (chunks > p.steps / 32) chunks = p.steps / 32;
+    r.chunk = (int)(((p.steps + chunks - 1) / chunks + kSsmBlock - 1) / kSsmBlock * kSsmBlock);
+    r.chunks = (int)((p.steps + r.chunk - 1) / r.chunk);
+    // one more token, which the last scalar load of a row runs into
+    r.bc = (size_t)(p.batch * p.steps + 1) * p.groups * 2 * r.np * 4;
+    if (r.chunks > 1) {
+        r.ends = (size_t)r.chunks * p.batch * p.dim * r.np * 4;
+        r.sums = (size_t)r.chunks * p.batch * p.dim * 4;
+    }
+    return r;
+}
+
+template <class T, int NP>
+hipError_t lanes_as(const libscan_ssm& p, const LanePlan& l, void* y, float* state_out,
+                    float* ckpt, void* scratch, hipStream_t stream) {
+    float* bc = (float*)scratch;
+    float* ends = bc + l.bc / 4;
+    float* sums = ends + l.ends / 4;
+    const int64_t words = p.batch * p.steps * p.groups * NP;
+    k_ssm_bc<T, NP><<<dim3((unsigned)((words + kThreads - 1) / kThreads)), kThreads, 0, stream>>>(
+        p, bc);
+    const unsigned waves = (unsigned)(p.batch * p.groups * l.nb);
+    const unsigned grid = (waves + kLaneWaves - 1) / kLaneWaves;
+    if (l.chunks > 1) {
+        k_ssm_ends<T, NP><<<dim3(grid, l.chunks - 1), kWave * kLaneWaves, 0, stream>>>(
+            p, bc, ends, sums, l.nb, l.chunk, waves);
+        const int64_t states = p.batch * p.dim * NP;
+        k_ssm_starts<NP><<<dim3((unsigned)((states + kThreads - 1) / kThreads)), kThreads, 0,
+                           stream>>>(p, ends, sums, l.chunks);
+    }
+    auto* scan = p.z ? k_ssm_lanes<T, NP, true> : k_ssm_lanes<T, NP, false>;
+    scan<<<dim3(grid, l.chunks), kWave * kLaneWaves, 0, stream>>>(
+        p, bc, l.chunks > 1 ? ends : nullptr, (T*)y, state_out, ckpt, l.nb, l.chunk,
+        waves);
+    return hipGetLastError();
+}
+
 template <class T>
 hipError_t scan_type(const libscan_ssm& p, void* y, float* state_out, float* ckpt, void* scratch,
                      hipStream_t stream) {
+    const LanePlan l = lane_plan(p);
+    switch (l.np) {
+        case 8: return lanes_as<T, 8>(p, l, y, state_out, ckpt, scratch, stream);
+        case 16: return lanes_as<T, 16>(p, l, y, state_out, ckpt, scratch, stream);
+        case 32: return lanes_as<T, 32>(p, l, y, state_out, ckpt, scratch, stream);
+        case 64: return lanes_as<T, 64>(p, l, y, state_out, ckpt, scratch, stream);
+        default: break;
+    }
     if (p.n > 32) return scan_as<T, 16, 4>(p, y, state_out, ckpt, stream);
     if (p.n > 16) return scan_as<T, 16, 2>(p, y, state_out, ckpt, stream);
-    if (p.batch * p.dim >= 16384) return scan_as<T, 4, 4>(p, y, state_out, ckpt, stream);
+    if (p.batch * p.dim >= kTileChannels) return scan_as<T, 4, 4>(p, y, state_out, ckpt, stream);
     return scan_as<T, 16, 1>(p, y, state_out, ckpt, stream);
 }
 
 }  // namespace
 
-size_t ssm_scratch_bytes(const libscan_ssm&) { return 0; }
+size_t ssm_scratch_bytes(const libscan_ssm& p) {
+    const LanePlan l = lane_plan(p);
+    return l.bc + l.ends + l.sums;
+}
 
 hipError_t launch_ssm_scan(const libscan_ssm& p, void* y, float* state_out, float* ckpt,
                            void* scratch, hipStream_t stream) {

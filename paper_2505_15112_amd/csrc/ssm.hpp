@@ -48,11 +48,12 @@ struct SsmLanes {
 struct SsmBlock {
     int b, g, k, c0, lim;
 };
-__device__ __forceinline__ SsmBlock ssm_block(const libscan_ssm& p, int nb, int ch) {
+__device__ __forceinline__ SsmBlock ssm_block(const libscan_ssm& p, int nb, int ch,
+                                              uint32_t index) {
     SsmBlock r;
     const int groups = (int)p.groups, per = (int)p.dim / groups;
-    r.k = blockIdx.x % nb;
-    const int bg = blockIdx.x / nb;
+    r.k = index % nb;
+    const int bg = index / nb;
     r.g = bg % groups;
     r.b = bg / groups;
     r.c0 = r.g * per + r.k * ch;

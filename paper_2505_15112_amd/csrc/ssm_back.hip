@@ -48,7 +48,7 @@ __global__ __launch_bounds__(kThreads) void k_ssm_back(libscan_ssm p, BackArgs o
 
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     const int steps = (int)p.steps, dim = (int)p.dim, n = (int)p.n, groups = (int)p.groups;
-    const SsmBlock k = ssm_block(p, nb, CH);
+    const SsmBlock k = ssm_block(p, nb, CH, blockIdx.x);
     const int len = ssm_len(p, k.b);
     const int blocks = (steps + kT - 1) / kT;
 

@@ -140,6 +140,28 @@ def test_scan_ragged_rows_do_not_read_past_their_tokens(dim):
         check_backward(clean, dy_clean, dstate_out=so)
 
 
+@pytest.mark.parametrize("n,groups", [(1, 1), (8, 1), (16, 2), (20, 1), (64, 2)])
+@pytest.mark.parametrize("kind", [F32, BF16])
+def test_scan_long_ragged_rows(n, groups, kind):
+    """Rows cut into chunks: lengths at, around and between the cuts, on strided
+    inputs with NaN behind the tokens."""
+    lengths = [0, 5, 32, 33, 64, 95, 150, 200]
+    a, dy = inputs(8, 150, 130, n, groups, kind=kind, state=True, lengths=lengths)
+    for b, count in enumerate(lengths):
+        for k in ("x", "dt", "z", "B", "C"):
+            a[k][b, count:] = float("nan")
+        dy[b, count:] = float("nan")
+    check_forward(a)
+    check_backward(a, dy, dstate_out=torch.randn(8, 130, n))
+    d = dev(a)
+    y = ops.selective_scan(**d)[0]
+    both = torch.full((8, 150, 3 * 130 + 1), float("nan"), dtype=kind, device=DEV)
+    for i, k in enumerate(("x", "dt", "z")):
+        both[:, :, 1 + i * 130:1 + (i + 1) * 130] = d[k]
+        d[k] = both[:, :, 1 + i * 130:1 + (i + 1) * 130]
+    assert torch.equal(ops.selective_scan(**d)[0], y)
+
+
 def test_scan_wide_layout():
     """Enough channels for a quad of lanes per channel, in both directions."""
     a, dy = inputs(2, 35, 8200, 16, groups=2, kind=BF16, state=True)
