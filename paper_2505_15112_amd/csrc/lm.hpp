@@ -80,58 +80,45 @@ __device__ __forceinline__ float dpp_f(float v) {
     return __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, b, CTRL, 0xf, 0xf, true));
 }
 
-// Sums of K values over the four lanes of a quad, shared out: lane q of the
-// quad is left with v[j] = the sum of the former v[quad_index(q, j)], j < K / 4.
-template <int K>
-__device__ __forceinline__ int quad_index(int lane, int j) {
-    return (lane & 1) * (K / 2) + ((lane >> 1) & 1) * (K / 4) + j;
-}
-template <int K>
-__device__ __forceinline__ void quad_reduce(float (&v)[K], int lane) {
-    static_assert(K % 4 == 0, "a quad shares out multiples of four sums");
-#pragma unroll
-    for (int i = 0; i < K / 2; ++i) {
-        const float p = v[i] + dpp_f<0xB1>(v[i]);                  // quad_perm 1,0,3,2
-        const float q = v[i + K / 2] + dpp_f<0xB1>(v[i + K / 2]);
-        v[i] = (lane & 1) ? q : p;
-    }
-#pragma unroll
-    for (int i = 0; i < K / 4; ++i) {
-        const float p = v[i] + dpp_f<0x4E>(v[i]);                  // quad_perm 2,3,0,1
-        const float q = v[i + K / 4] + dpp_f<0x4E>(v[i + K / 4]);
-        v[i] = (lane & 2) ? q : p;
-    }
-}
-
 __device__ __forceinline__ float as_f32(unsigned b) { return __builtin_bit_cast(float, b); }
 __device__ __forceinline__ unsigned as_u32(float v) { return __builtin_bit_cast(unsigned, v); }
 
-// Sums of 16 values over the 16 quads of the wave (lanes of one place in
-// their quads), shared out: the returned value is the sum of v[lane >> 2].
-// Halves are exchanged by the two swap instructions (rows of 32 and 16 lanes),
-// then inside rows by rotations.
-__device__ __forceinline__ float quads_reduce16(float (&v)[16], int lane) {
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-        const auto r = __builtin_amdgcn_permlane32_swap(as_u32(v[i]), as_u32(v[i + 8]), false,
-                                                        false);
-        v[i] = as_f32(r[0]) + as_f32(r[1]);
+// Two sums over the pairs of lanes that differ in bit BIT, one to a lane of the
+// pair: p's where the bit is 0, q's where it is 1.  Rows of 32 and of 16 lanes
+// exchange halves by the swap instructions, lanes inside a row by DPP.
+template <int BIT>
+__device__ __forceinline__ float pair_sum(float p, float q, int lane) {
+    if constexpr (BIT == 5) {
+        const auto r = __builtin_amdgcn_permlane32_swap(as_u32(p), as_u32(q), false, false);
+        return as_f32(r[0]) + as_f32(r[1]);
+    } else if constexpr (BIT == 4) {
+        const auto r = __builtin_amdgcn_permlane16_swap(as_u32(p), as_u32(q), false, false);
+        return as_f32(r[0]) + as_f32(r[1]);
+    } else {
+        // row_ror:8; row_ror:12 and :4 (from four lanes up, and down); quad_perm
+        constexpr int kP = BIT == 3 ? 0x128 : BIT == 2 ? 0x12C : BIT == 1 ? 0x4E : 0xB1;
+        constexpr int kQ = BIT == 2 ? 0x124 : kP;
+        p += dpp_f<kP>(p);
+        q += dpp_f<kQ>(q);
+        return (lane & (1 << BIT)) ? q : p;
     }
+}
+
+// Sums of K values over the lanes that differ in the given bits, shared out: a
+// lane is left with v[j] = the sum of the former v[share_index<K, BITS...>(lane) + j],
+// j < K / 2^(number of bits).
+template <int K, int BIT, int... REST>
+__device__ __forceinline__ int share_index(int lane) {
+    int i = ((lane >> BIT) & 1) * (K / 2);
+    if constexpr (sizeof...(REST) > 0) i += share_index<K / 2, REST...>(lane);
+    return i;
+}
+template <int K, int BIT, int... REST, int N>
+__device__ __forceinline__ void share_sums(float (&v)[N], int lane) {
+    static_assert(K % 2 == 0 && K <= N, "every bit halves the sums");
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        const auto r = __builtin_amdgcn_permlane16_swap(as_u32(v[i]), as_u32(v[i + 4]), false,
-                                                        false);
-        v[i] = as_f32(r[0]) + as_f32(r[1]);
-    }
-#pragma unroll
-    for (int i = 0; i < 2; ++i) {
-        const float p = v[i] + dpp_f<0x128>(v[i]);  // row_ror:8
-        const float q = v[i + 2] + dpp_f<0x128>(v[i + 2]);
-        v[i] = (lane & 8) ? q : p;
-    }
-    const float p = v[0] + dpp_f<0x12C>(v[0]);  // row_ror:12: from four lanes up
-    const float q = v[1] + dpp_f<0x124>(v[1]);  // row_ror:4: from four lanes down
-    return (lane & 4) ? q : p;
+    for (int i = 0; i < K / 2; ++i) v[i] = pair_sum<BIT>(v[i], v[i + K / 2], lane);
+    if constexpr (sizeof...(REST) > 0) share_sums<K / 2, REST...>(v, lane);
 }
 
 }  // namespace ls

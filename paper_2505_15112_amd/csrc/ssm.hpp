@@ -10,37 +10,49 @@ namespace ls {
 constexpr int kSsmBlock = 16;  // steps between checkpoints
 
 // LN lanes share a channel, each with SPL of its NP = LN * SPL states (indices
-// past n are padding: A = B = C = 0).  With LN = 4 a quad is a channel, and a wave
-// holds 16 channels; with LN = 16 the four lanes of a quad are four channels and
-// the 16 quads hold the states.  Four waves to a workgroup.
+// past n are padding: A = B = C = 0); the other lanes of the wave hold other
+// channels.  Four waves to a workgroup.  Sums over the lanes of one kind are
+// shared out over them (share_sums), which is cheapest over the high bits of
+// the lane, so the larger number of lanes lies there.
 template <int LN_, int SPL_>
 struct SsmLanes {
-    static_assert(LN_ == 4 || LN_ == 16, "a channel lies on a quad or across the quads");
+    static_assert(LN_ == 4 || LN_ == 8 || LN_ == 16, "lanes of a channel");
     static constexpr int LN = LN_, SPL = SPL_, NP = LN * SPL, CPW = 64 / LN, CH = 4 * CPW;
-    __device__ static __forceinline__ int channel(int lane) { return LN == 4 ? lane >> 2 : lane & 3; }
-    __device__ static __forceinline__ int part(int lane) { return LN == 4 ? lane & 3 : lane >> 2; }
+    __device__ static __forceinline__ int channel(int lane) {
+        return LN == 16 ? lane & 3 : lane / LN;
+    }
+    __device__ static __forceinline__ int part(int lane) {
+        return LN == 16 ? lane >> 2 : lane % LN;
+    }
     // v[t], t < 16: this lane's share of a sum over its channel's states at step
     // t.  Calls put(t, sum) for the steps whose sums end up in this lane.
     template <class F>
     __device__ static __forceinline__ void sum_states(float (&v)[kSsmBlock], int lane, F put) {
-        if constexpr (LN == 4) {
-            quad_reduce<kSsmBlock>(v, lane);
-#pragma unroll
-            for (int j = 0; j < kSsmBlock / 4; ++j) put(quad_index<kSsmBlock>(lane, j), v[j]);
-        } else {
-            put(lane >> 2, quads_reduce16(v, lane));
-        }
+        if constexpr (LN == 4)
+            share<0, 1>(v, lane, put);
+        else if constexpr (LN == 8)
+            share<2, 1, 0>(v, lane, put);
+        else
+            share<5, 4, 3, 2>(v, lane, put);
     }
     // The same for sums over the wave's channels, of one state index.
     template <class F>
     __device__ static __forceinline__ void sum_channels(float (&v)[kSsmBlock], int lane, F put) {
-        if constexpr (LN == 4) {
-            put(lane >> 2, quads_reduce16(v, lane));
-        } else {
-            quad_reduce<kSsmBlock>(v, lane);
+        if constexpr (LN == 4)
+            share<5, 4, 3, 2>(v, lane, put);
+        else if constexpr (LN == 8)
+            share<5, 4, 3>(v, lane, put);
+        else
+            share<0, 1>(v, lane, put);
+    }
+
+private:
+    template <int... BITS, class F>
+    __device__ static __forceinline__ void share(float (&v)[kSsmBlock], int lane, F put) {
+        share_sums<kSsmBlock, BITS...>(v, lane);
+        const int t = share_index<kSsmBlock, BITS...>(lane);
 #pragma unroll
-            for (int j = 0; j < kSsmBlock / 4; ++j) put(quad_index<kSsmBlock>(lane, j), v[j]);
-        }
+        for (int j = 0; j < kSsmBlock >> sizeof...(BITS); ++j) put(t + j, v[j]);
     }
 };
 

@@ -36,6 +36,18 @@ struct BackArgs {
     float* part_bias; // [batch][dim]
 };
 
+// Keeps the loads from two LDS addresses behind the computation of v: left
+// alone, the compiler loads a whole block's inputs first, into registers that
+// the block's states need.
+constexpr int kGroup = 4;  // steps whose inputs are loaded together
+typedef const __attribute__((address_space(3))) float4* LdsIn;
+typedef const __attribute__((address_space(3))) float2* LdsBc;
+__device__ __forceinline__ float4 load_lds(LdsIn p) { return float4{p->x, p->y, p->z, p->w}; }
+__device__ __forceinline__ float2 load_lds(LdsBc p) { return float2{p->x, p->y}; }
+__device__ __forceinline__ void after(float v, LdsIn& p, LdsBc& q) {
+    asm volatile("" : "+v"(p), "+v"(q) : "v"(v));
+}
+
 template <class T, int LN, int SPL>
 __global__ __launch_bounds__(kThreads) void k_ssm_back(libscan_ssm p, BackArgs o, int nb) {
     using L = SsmLanes<LN, SPL>;
@@ -92,23 +104,42 @@ __global__ __launch_bounds__(kThreads) void k_ssm_back(libscan_ssm p, BackArgs o
         if (pz) zero.store((T*)o.dz + at, lcount);
     }
 
-    for (int blk = (len + kT - 1) / kT - 1; blk >= 0; --blk) {
-        const int t0 = blk * kT;
-        const bool live = t0 + row < len;
-        const int count = live ? lcount : 0;
-        Pack<T, VW> rx, rdt, rz, rdy;
-        rx.load(px + (t0 + row) * p.x_step, count);
-        rdt.load(pdt + (t0 + row) * p.dt_step, count);
-        rz.load(pz + (t0 + row) * p.z_step, pz ? count : 0);
-        rdy.load(pdy + (t0 + row) * o.dy_step, count);
+    // what a block reads, loaded while the block after it is worked on
+    Pack<T, VW> nx, ndt, nz, ndy;
+    T nB[NBC], nC[NBC];
+    float nh[SPL];
+    auto fetch = [&](int blk) {
+        const int t0 = blk * kT, count = t0 + row < len ? lcount : 0;
+        nx.load(px + (t0 + row) * p.x_step, count);
+        ndt.load(pdt + (t0 + row) * p.dt_step, count);
+        nz.load(pz + (t0 + row) * p.z_step, pz ? count : 0);
+        ndy.load(pdy + (t0 + row) * o.dy_step, count);
 #pragma unroll
         for (int i = 0; i < NBC; ++i) {
             const int e = tid + i * kThreads, tt = e / NP, nn = e % NP;
-            if (kT * NP % kThreads == 0 || e < kT * NP) {
-                const bool in = t0 + tt < len && nn < n;
-                s_bc[tt][nn] = float2{in ? to_f32(pB[(t0 + tt) * p.B_step + nn]) : 0.0f,
-                                      in ? to_f32(pC[(t0 + tt) * p.C_step + nn]) : 0.0f};
-            }
+            const bool in = e < kT * NP && t0 + tt < len && nn < n;
+            nB[i] = in ? pB[(t0 + tt) * p.B_step + nn] : T(0);
+            nC[i] = in ? pC[(t0 + tt) * p.C_step + nn] : T(0);
+        }
+        const float* pc = o.ckpt + (((int64_t)k.b * blocks + blk) * dim + k.c0 + wc) * n + n0;
+#pragma unroll
+        for (int s = 0; s < SPL; ++s) nh[s] = wc < k.lim && n0 + s < n ? pc[s] : 0.0f;
+    };
+
+    const int last = (len + kT - 1) / kT - 1;
+    if (last >= 0) fetch(last);
+    for (int blk = last; blk >= 0; --blk) {
+        const int t0 = blk * kT;
+        const bool live = t0 + row < len;
+        const Pack<T, VW> rx = nx, rdt = ndt, rz = nz, rdy = ndy;
+        float h0[SPL];
+#pragma unroll
+        for (int s = 0; s < SPL; ++s) h0[s] = nh[s];
+#pragma unroll
+        for (int i = 0; i < NBC; ++i) {
+            const int e = tid + i * kThreads;
+            if (kT * NP % kThreads == 0 || e < kT * NP)
+                s_bc[e / NP][e % NP] = float2{to_f32(nB[i]), to_f32(nC[i])};
         }
         float delta[VW], w[VW];
 #pragma unroll
@@ -120,23 +151,24 @@ __global__ __launch_bounds__(kThreads) void k_ssm_back(libscan_ssm p, BackArgs o
             w[i] = to_f32(rdy.v[i]) * (pz ? z * sigmoid(z) : 1.0f);
             s_in[row][lc + i] = float4{delta[i], delta[i] * to_f32(rx.v[i]), w[i], 0.0f};
         }
+        if (blk > 0) fetch(blk - 1);
         __syncthreads();
 
-        float h[kT][SPL], a[kT][SPL], h0[SPL];
+        float h[kT][SPL], a[kT][SPL];
+        LdsIn in_at = (LdsIn)&s_in[0][wc];
+        LdsBc bc_at = (LdsBc)&s_bc[0][n0];
         {
-            const float* pc = o.ckpt + (((int64_t)k.b * blocks + blk) * dim + k.c0 + wc) * n + n0;
-#pragma unroll
-            for (int s = 0; s < SPL; ++s) h0[s] = wc < k.lim && n0 + s < n ? pc[s] : 0.0f;
             float hr[SPL], v[kT];
 #pragma unroll
             for (int s = 0; s < SPL; ++s) hr[s] = h0[s];
 #pragma unroll
             for (int t = 0; t < kT; ++t) {
-                const float4 in = s_in[t][wc];
+                if (t % kGroup == 0) after(hr[0], in_at, bc_at);
+                const float4 in = load_lds(in_at + t * CH);
                 float acc = 0.0f;
 #pragma unroll
                 for (int s = 0; s < SPL; ++s) {
-                    const float2 bc = s_bc[t][n0 + s];
+                    const float2 bc = load_lds(bc_at + t * NP + s);
                     a[t][s] = exp2_fast(in.x * a2[s]);
                     hr[s] = __builtin_fmaf(a[t][s], hr[s], in.y * bc.x);
                     h[t][s] = hr[s];
@@ -145,42 +177,45 @@ __global__ __launch_bounds__(kThreads) void k_ssm_back(libscan_ssm p, BackArgs o
                 v[t] = acc;
             }
             if (pz) L::sum_states(v, lane, [&](int t, float sum) { s_y[t][wc] = sum; });
-#pragma unroll
-            for (int s = 0; s < SPL; ++s) {
-#pragma unroll
-                for (int t = 0; t < kT; ++t) v[t] = s_in[t][wc].z * h[t][s];
-                L::sum_channels(v, lane, [&](int t, float sum) { s_g[wave][t][n0 + s].y = sum; });
-            }
         }
         {
             float vu[kT], vd[kT];
 #pragma unroll
             for (int t = kT - 1; t >= 0; --t) {
-                const float4 in = s_in[t][wc];
+                if (t % kGroup == kGroup - 1) after(cg[0], in_at, bc_at);
+                const float4 in = load_lds(in_at + t * CH);
                 float du = 0.0f, dd = 0.0f;
 #pragma unroll
                 for (int s = 0; s < SPL; ++s) {
-                    const float2 bc = s_bc[t][n0 + s];
+                    const float2 bc = load_lds(bc_at + t * NP + s);
                     const float g = __builtin_fmaf(in.z, bc.y, cg[s]);
                     du = __builtin_fmaf(g, bc.x, du);
                     cg[s] = a[t][s] * g;
                     const float r = cg[s] * (t ? h[t ? t - 1 : 0][s] : h0[s]);
                     dd = __builtin_fmaf(r, a2[s], dd);
                     da[s] = __builtin_fmaf(r, in.x, da[s]);
-                    h[t][s] = g * in.y;  // dB; h[t] is done with
+                    a[t][s] = g * in.y;  // a and h of this step are done with: dB and dC
+                    h[t][s] *= in.z;
+                    // formed here and now: put off, the products hold both factors
+                    asm volatile("" : "+v"(a[t][s]), "+v"(h[t][s]));
                 }
                 vu[t] = du;
                 vd[t] = dd;
+                asm volatile("" : "+v"(vu[t]), "+v"(vd[t]));
             }
             L::sum_states(vu, lane, [&](int t, float sum) { s_du[t][wc] = sum; });
             L::sum_states(vd, lane, [&](int t, float sum) { s_dd[t][wc] = sum; });
         }
 #pragma unroll
         for (int s = 0; s < SPL; ++s) {
-            float v[kT];
+            float v[kT], u[kT];
 #pragma unroll
-            for (int t = 0; t < kT; ++t) v[t] = h[t][s];
+            for (int t = 0; t < kT; ++t) {
+                v[t] = a[t][s];
+                u[t] = h[t][s];
+            }
             L::sum_channels(v, lane, [&](int t, float sum) { s_g[wave][t][n0 + s].x = sum; });
+            L::sum_channels(u, lane, [&](int t, float sum) { s_g[wave][t][n0 + s].y = sum; });
         }
         __syncthreads();
 
@@ -296,8 +331,9 @@ __global__ __launch_bounds__(kThreads) void k_ssm_sum_rows(int64_t batch, int64_
     }
 }
 
-// Which lanes a problem takes, the same for the sizes and the launch.
-bool wide(const libscan_ssm& p) { return p.n <= 16 && p.batch * p.dim >= 8192; }
+// Lanes to a channel, the same for the sizes and the launch.
+int lanes(const libscan_ssm& p) { return p.n > 32 ? 16 : p.batch * p.dim >= 8192 ? 8 : 16; }
+int blocks_of(const libscan_ssm& p) { return ssm_blocks(p, 256 / lanes(p)); }
 
 size_t align16(size_t v) { return (v + 15) / 16 * 16; }
 
@@ -310,15 +346,14 @@ void back_as(const libscan_ssm& p, const BackArgs& o, int nb, hipStream_t stream
 template <class T>
 hipError_t back_type(const libscan_ssm& p, const BackArgs& o, float* dA, T* dB, T* dC, float* dD,
                      float* ddt_bias, hipStream_t stream) {
-    const int nb = ssm_blocks(p, wide(p) ? 64 : 16);
+    const int nb = blocks_of(p);
+    const bool eight = lanes(p) == 8;
     if (p.n > 32)
         back_as<T, 16, 4>(p, o, nb, stream);
     else if (p.n > 16)
-        back_as<T, 16, 2>(p, o, nb, stream);
-    else if (wide(p))
-        back_as<T, 4, 4>(p, o, nb, stream);
+        eight ? back_as<T, 8, 4>(p, o, nb, stream) : back_as<T, 16, 2>(p, o, nb, stream);
     else
-        back_as<T, 16, 1>(p, o, nb, stream);
+        eight ? back_as<T, 8, 2>(p, o, nb, stream) : back_as<T, 16, 1>(p, o, nb, stream);
     const int64_t bc = p.batch * p.steps * p.groups * p.n;
     if (bc > 0)
         k_ssm_sum_bc<T><<<dim3((unsigned)((bc + kThreads - 1) / kThreads)), kThreads, 0, stream>>>(
@@ -337,7 +372,7 @@ size_t ssm_ckpt_bytes(const libscan_ssm& p) {
 }
 
 size_t ssm_back_scratch_bytes(const libscan_ssm& p) {
-    const size_t nb = ssm_blocks(p, wide(p) ? 64 : 16);
+    const size_t nb = blocks_of(p);
     return align16(nb * p.batch * p.steps * p.groups * p.n * 8) +
            align16((size_t)p.batch * p.dim * p.n * 4) + 2 * align16((size_t)p.batch * p.dim * 4);
 }
@@ -346,7 +381,7 @@ hipError_t launch_ssm_back(const libscan_ssm& p, const void* dy, int64_t dy_batc
                            const float* ckpt, const float* dstate_out, void* dx, void* ddt,
                            float* dA, void* dB, void* dC, float* dD, void* dz, float* ddt_bias,
                            float* dstate, void* scratch, hipStream_t stream) {
-    const size_t nb = ssm_blocks(p, wide(p) ? 64 : 16);
+    const size_t nb = blocks_of(p);
     char* s = (char*)scratch;
     BackArgs o{dy, dy_batch, dy_step, ckpt, dstate_out, dx, ddt, dz, dstate,
                nullptr, nullptr, nullptr, nullptr};
