@@ -6,13 +6,16 @@ Compiles every csrc/*.hip into _build/ and links paper_2505_15112_amd/libscan.so
 in-tree.  Always recompiles.  Also links libscan_adv.so, the same sources built
 with LS_ADVERSARIAL_DELAYS (pseudo-random pauses before every inter-workgroup
 protocol step) for the adversarial-scheduling tests; it binds its own symbols
-(-Bsymbolic) so that it can be loaded beside libscan.so.
+(-Bsymbolic) so that it can be loaded beside libscan.so.  csrc/torch_args.cpp,
+which checks torch tensors for the binding, becomes _torch_args.so (host code,
+against torch's headers).
 """
 import concurrent.futures as cf
 import glob
 import os
 import subprocess
 import sys
+import sysconfig
 
 PKG = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(PKG)
@@ -20,6 +23,7 @@ CSRC = os.path.join(PKG, "csrc")
 BUILD = os.path.join(ROOT, "_build", "libscan")
 LIB = os.path.join(PKG, "libscan.so")
 LIB_ADV = os.path.join(PKG, "libscan_adv.so")
+LIB_ARGS = os.path.join(PKG, "_torch_args.so")
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 ARCH = "gfx950"
 
@@ -60,14 +64,36 @@ def _link(objs, out: str, verbose: bool, extra=()) -> str:
     return out
 
 
+def _torch_args(verbose: bool) -> str:
+    import torch
+    from torch.utils.cpp_extension import include_paths
+
+    inc = [os.path.join(ROOT, "include"), *include_paths(), sysconfig.get_path("include")]
+    libs = os.path.join(os.path.dirname(torch.__file__), "lib")
+    tmp = LIB_ARGS + ".tmp"
+    cmd = ["g++", "-O2", "-std=c++17", "-fPIC", "-shared", "-fvisibility=hidden",
+           f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}",
+           *[f for d in inc for f in ("-isystem", d)], os.path.join(CSRC, "torch_args.cpp"),
+           "-o", tmp, "-L", libs, "-ltorch_python", "-ltorch_cpu", "-lc10"]
+    if verbose:
+        print(" ".join(cmd), flush=True)
+    r = subprocess.run(cmd, capture_output=True, text=True)
+    if r.returncode != 0:
+        raise RuntimeError(f"g++ failed for torch_args.cpp:\n{r.stdout}\n{r.stderr}")
+    os.replace(tmp, LIB_ARGS)
+    return LIB_ARGS
+
+
 def build(verbose: bool = False) -> str:
     srcs = sorted(glob.glob(os.path.join(CSRC, "*.hip")))
     adv_dir = BUILD + "_adv"
     os.makedirs(BUILD, exist_ok=True)
     os.makedirs(adv_dir, exist_ok=True)
     jobs = [(s, BUILD, ()) for s in srcs] + [(s, adv_dir, ("-DLS_ADVERSARIAL_DELAYS",)) for s in srcs]
-    with cf.ThreadPoolExecutor(max_workers=min(8, len(jobs))) as ex:
+    with cf.ThreadPoolExecutor(max_workers=min(8, len(jobs) + 1)) as ex:
+        args = ex.submit(_torch_args, verbose)
         objs = list(ex.map(lambda j: _compile(j[0], verbose, j[1], j[2]), jobs))
+    args.result()
     _link(objs[:len(srcs)], LIB, verbose)
     _link(objs[len(srcs):], LIB_ADV, verbose, ("-Wl,-Bsymbolic",))
     return LIB

@@ -6,8 +6,8 @@ of the same name on the current torch stream.  Every step of the computation
 runs in libscan's HIP kernels; there is no fallback path.
 """
 import ctypes
+import importlib.util
 import os
-import struct
 
 import torch
 
@@ -448,54 +448,32 @@ def topk_rows_f32(x, k, largest=True, values_out=None, idx_out=None, ws=None, sc
 
 # ---------------------------------------------------------------- language model operators
 
-_TYPES = {torch.float32: _lib.F32, torch.float16: _lib.F16, torch.bfloat16: _lib.BF16}
-_CONV = struct.Struct("14q")    # libscan_conv
-_SSM = struct.Struct("29q")     # libscan_ssm
-_LOGITS = struct.Struct("19q")  # libscan_logits
+class _Args:
+    """The compiled checks of torch_args.cpp, loaded at the first use: conv, ssm and
+    logits check an operator's tensors and return its struct's bytes."""
+
+    def __getattr__(self, name):
+        path = os.path.join(_lib.PKG, "_torch_args.so")
+        if not os.path.exists(path):
+            raise RuntimeError(f"{path} is not built; run `python -m paper_2505_15112_amd.build`")
+        spec = importlib.util.spec_from_file_location("_torch_args", path)
+        module = importlib.util.module_from_spec(spec)
+        spec.loader.exec_module(module)
+        self.__dict__.update({k: getattr(module, k)
+                              for k in ("conv", "ssm", "logits", "dense", "empty")})
+        return self.__dict__[name]
 
 
-def _arg(t, name, dtype, shape, device, dense=False):
-    """Check an operand: its type, place and shape, and that its last dimension
-    has unit stride (dense: all of it is contiguous).  Returns its address."""
-    if not isinstance(t, torch.Tensor):
-        raise TypeError(f"{name}: expected a torch.Tensor")
-    if t.dtype != dtype:
-        raise TypeError(f"{name}: expected {dtype}, got {t.dtype}")
-    if t.shape != shape:
-        raise ValueError(f"{name}: expected shape {tuple(shape)}, got {tuple(t.shape)}")
-    if t.get_device() != device:
-        raise ValueError(f"{name}: expected a tensor on the GPU of the first operand, got "
-                         f"{t.device}")
-    if dense:
-        if not t.is_contiguous():
-            raise ValueError(f"{name}: must be contiguous")
-    elif t.stride(-1) != 1 and t.shape[-1] > 1 and t.numel() > 0:
-        raise ValueError(f"{name}: the last dimension must have unit stride")
-    return t.data_ptr()
+_args = _Args()
 
 
-def _opt(t, name, dtype, shape, device, dense=True):
-    return 0 if t is None else _arg(t, name, dtype, shape, device, dense)
-
-
-def _first(t, name, dims):
-    """The operand that sets the others' sizes.  Returns its type code and GPU."""
-    if not isinstance(t, torch.Tensor):
-        raise TypeError(f"{name}: expected a torch.Tensor")
-    if t.dtype not in _TYPES:
-        raise TypeError(f"{name}: expected float32, float16 or bfloat16, got {t.dtype}")
-    if not t.is_cuda:
-        raise ValueError(f"{name}: expected a GPU tensor, got {t.device}")
-    if t.dim() != dims:
-        raise ValueError(f"{name}: expected {dims} dims, got {t.dim()}")
-    return _TYPES[t.dtype], t.get_device()
-
-
-def _into(out, like, shape, dtype, name="out"):
-    """The given output, checked, or a new one."""
+def _into(out, like, shape=None, f32=False, name="out"):
+    """The given output, checked, or a new one: of like's shape and type unless said."""
     if out is None:
-        return torch.empty(shape, dtype=dtype, device=like.device)
-    _arg(out, name, dtype, torch.Size(shape), like.get_device(), dense=True)
+        if shape is None:
+            return _args.empty(like, f32)
+        return torch.empty(shape, dtype=torch.float32 if f32 else like.dtype, device=like.device)
+    _args.dense(out, name, like, tuple(like.shape) if shape is None else shape, f32)
     return out
 
 
@@ -507,24 +485,6 @@ def _scratch_for(buf, nbytes, like):
     return buf
 
 
-def _conv(x, weight, bias, state, lengths, silu, step=False):
-    """A libscan_conv and the width."""
-    code, dev = _first(x, "x", 2 if step else 3)
-    batch, steps, dim = (x.shape[0], 1, x.shape[1]) if step else x.shape
-    if not isinstance(weight, torch.Tensor) or weight.dim() != 2:
-        raise TypeError("weight: expected a torch.Tensor of dim x width")
-    if weight.dtype not in (x.dtype, torch.float32):
-        raise TypeError(f"weight: expected {x.dtype} or float32, got {weight.dtype}")
-    width = weight.shape[1]
-    px = _arg(x, "x", x.dtype, x.shape, dev)
-    pw = _arg(weight, "weight", weight.dtype, (dim, width), dev, True)
-    pb = _opt(bias, "bias", weight.dtype, (dim,), dev)
-    ps = _opt(state, "state", x.dtype, (batch, width - 1, dim), dev)
-    pl = _opt(lengths, "lengths", torch.int32, (batch,), dev)
-    return _CONV.pack(code, _TYPES[weight.dtype], batch, steps, dim, width, int(bool(silu)), px,
-                      x.stride(0), 0 if step else x.stride(1), pw, pb, ps, pl), width
-
-
 def causal_conv(x, weight, bias=None, state=None, lengths=None, silu=True, with_state=False,
                 out=None, state_out=None):
     """Causal depthwise convolution over time: x is batch x steps x dim, weight
@@ -532,10 +492,11 @@ def causal_conv(x, weight, bias=None, state=None, lengths=None, silu=True, with_
     batch x (width-1) x dim inputs before the first.  Returns (y, state_out): the
     last width-1 inputs of every row when with_state (or state_out is given),
     else None."""
-    p, width = _conv(x, weight, bias, state, lengths, silu)
-    y = _into(out, x, x.shape, x.dtype)
+    p = _args.conv(x, weight, bias, state, lengths, silu, False)
+    y = _into(out, x)
     if with_state or state_out is not None:
-        state_out = _into(state_out, x, (x.shape[0], width - 1, x.shape[2]), x.dtype, "state_out")
+        state_out = _into(state_out, x, (x.shape[0], weight.shape[1] - 1, x.shape[2]),
+                          name="state_out")
     _launch("causal_conv", x, p, _ptr(y), _ptr(state_out))
     return y, state_out
 
@@ -545,11 +506,11 @@ def causal_conv_backward(dy, x, weight, bias=None, state=None, lengths=None, sil
     """Gradients of causal_conv from those of its outputs.  Returns (dx, dweight
     fp32, dbias fp32 or None, dstate or None: by default formed when there is
     a state)."""
-    p, width = _conv(x, weight, bias, state, lengths, silu)
-    dev, (batch, steps, dim) = x.get_device(), x.shape
-    pdy = _arg(dy, "dy", x.dtype, x.shape, dev)
-    pso = _opt(dstate_out, "dstate_out", x.dtype, (batch, width - 1, dim), dev)
-    dx = torch.empty(x.shape, dtype=x.dtype, device=x.device)
+    p = _args.conv(x, weight, bias, state, lengths, silu, False)
+    (batch, _, dim), width = x.shape, weight.shape[1]
+    pdy = _strided(dy, "dy", x)
+    pso = _args.dense(dstate_out, "dstate_out", x, (batch, width - 1, dim), False)
+    dx = _args.empty(x, False)
     dweight = torch.empty((dim, width), dtype=torch.float32, device=x.device)
     dbias = dweight.new_empty(dim) if bias is not None else None
     if with_dstate is None:
@@ -557,9 +518,24 @@ def causal_conv_backward(dy, x, weight, bias=None, state=None, lengths=None, sil
     dstate = x.new_empty((batch, width - 1, dim)) if with_dstate else None
     need = _sizes("causal_conv_scratch_bytes", p, 1)[0]
     buf = _scratch_for(scratch_buf, need, x)
-    _launch("causal_conv_backward", x, p, pdy or None, dy.stride(0), dy.stride(1), pso or None,
-            _ptr(dx), _ptr(dweight), _ptr(dbias), _ptr(dstate), _ptr(buf), buf.numel())
+    _launch("causal_conv_backward", x, p, pdy, dy.stride(0), dy.stride(1), pso, _ptr(dx),
+            _ptr(dweight), _ptr(dbias), _ptr(dstate), _ptr(buf), buf.numel())
     return dx, dweight, dbias, dstate
+
+
+def _strided(t, name, like):
+    """Check an operand of like's type, shape and GPU whose last dimension has unit
+    stride; returns its address."""
+    if not isinstance(t, torch.Tensor):
+        raise TypeError(f"{name}: expected a torch.Tensor")
+    if t.dtype != like.dtype:
+        raise TypeError(f"{name}: expected {like.dtype}, got {t.dtype}")
+    if t.shape != like.shape or t.get_device() != like.get_device():
+        raise ValueError(f"{name}: expected shape {tuple(like.shape)} on {like.device}, got "
+                         f"{tuple(t.shape)} on {t.device}")
+    if t.shape[-1] > 1 and t.stride(-1) != 1 and t.numel() > 0:
+        raise ValueError(f"{name}: the last dimension must have unit stride")
+    return _ptr(t)
 
 
 def _sizes(cname, p, count):
@@ -568,59 +544,33 @@ def _sizes(cname, p, count):
     return [g.value for g in got]
 
 
-def _pool(states, x, name, tail, slots):
-    """Check a pool of states and the rows' numbers in it; returns the slots' address."""
-    if not isinstance(states, torch.Tensor) or states.dim() != 1 + len(tail):
-        raise ValueError(f"{name}: expected states x {' x '.join(map(str, tail))}")
-    return _opt(slots, "slots", torch.int32, (x.shape[0],), x.get_device())
+def _pool(states, x, tail, f32, slots):
+    """Check a pool of states and the rows' numbers in it."""
+    if not isinstance(states, torch.Tensor):
+        raise TypeError("states: expected a torch.Tensor")
+    count = states.shape[0] if states.dim() else 0
+    ps = _args.dense(states, "states", x, (count, *tail), f32)
+    if slots is None:
+        if count < x.shape[0]:
+            raise ValueError("states: fewer than the rows of x")
+        return ps, count, None
+    if slots.dtype != torch.int32:
+        raise TypeError(f"slots: expected torch.int32, got {slots.dtype}")
+    _check(slots, torch.int32, "slots", (1,))
+    if slots.shape[0] != x.shape[0] or slots.get_device() != x.get_device():
+        raise ValueError("slots: expected one for each row of x, on its GPU")
+    return ps, count, _ptr(slots)
 
 
 def causal_conv_step(x, states, weight, bias=None, slots=None, silu=True, out=None):
     """One token of every row: x is batch x dim, states a pool of (width-1) x dim
     windows (row b's is number slots[b], or b), which move on in place.
     Returns y, batch x dim."""
-    p, width = _conv(x, weight, bias, None, None, silu, step=True)
-    tail = (width - 1, x.shape[1])
-    psl = _pool(states, x, "states", tail, slots)
-    _arg(states, "states", x.dtype, (states.shape[0], *tail), x.get_device(), True)
-    if slots is None and states.shape[0] < x.shape[0]:
-        raise ValueError("states: fewer than the rows of x")
-    y = _into(out, x, x.shape, x.dtype)
-    _launch("causal_conv_step", x, p, _ptr(states), states.shape[0], psl or None, _ptr(y))
+    p = _args.conv(x, weight, bias, None, None, silu, True)
+    pool = _pool(states, x, (weight.shape[1] - 1, x.shape[1]), False, slots)
+    y = _into(out, x)
+    _launch("causal_conv_step", x, p, *pool, _ptr(y))
     return y
-
-
-def _ssm(x, dt, A, B, C, D, z, dt_bias, state, lengths, softplus, step=False):
-    """A libscan_ssm."""
-    code, dev = _first(x, "x", 2 if step else 3)
-    batch, steps, dim = (x.shape[0], 1, x.shape[1]) if step else x.shape
-    kind, shape, f32 = x.dtype, x.shape, torch.float32
-    if not isinstance(A, torch.Tensor) or A.dim() != 2:
-        raise TypeError("A: expected a torch.Tensor of dim x n")
-    if not isinstance(B, torch.Tensor) or B.dim() != x.dim() + 1:
-        raise TypeError("B: expected a torch.Tensor of "
-                        + ("batch x groups x n" if step else "batch x steps x groups x n"))
-    n, groups = A.shape[1], B.shape[-2]
-    bc = (*shape[:-1], groups, n)
-    px = _arg(x, "x", kind, shape, dev)
-    pdt = _arg(dt, "dt", kind, shape, dev)
-    pz = _opt(z, "z", kind, shape, dev, False)
-    pB = _arg(B, "B", kind, bc, dev)
-    pC = _arg(C, "C", kind, bc, dev)
-    pA = _arg(A, "A", f32, (dim, n), dev, True)
-    pD = _opt(D, "D", f32, (dim,), dev)
-    pbias = _opt(dt_bias, "dt_bias", f32, (dim,), dev)
-    ps = _opt(state, "state", f32, (batch, dim, n), dev)
-    pl = _opt(lengths, "lengths", torch.int32, (batch,), dev)
-    sx, sdt, sB, sC = x.stride(), dt.stride(), B.stride(), C.stride()
-    sz = z.stride() if z is not None else (0, 0)
-    if step:
-        return _SSM.pack(code, batch, 1, dim, n, groups, int(bool(softplus)), px, sx[0], 0, pdt,
-                         sdt[0], 0, pz, sz[0], 0, pB, sB[0], 0, sB[1], pC, sC[0], 0, sC[1], pA, pD,
-                         pbias, ps, pl)
-    return _SSM.pack(code, batch, steps, dim, n, groups, int(bool(softplus)), px, sx[0], sx[1],
-                     pdt, sdt[0], sdt[1], pz, sz[0], sz[1], pB, sB[0], sB[1], sB[2], pC, sC[0],
-                     sC[1], sC[2], pA, pD, pbias, ps, pl)
 
 
 def selective_scan(x, dt, A, B, C, D=None, z=None, dt_bias=None, state=None, lengths=None,
@@ -632,11 +582,11 @@ def selective_scan(x, dt, A, B, C, D=None, z=None, dt_bias=None, state=None, len
     dt_bias: dim fp32; state: batch x dim x n fp32.  Returns (y, state_out or
     None, checkpoints or None): the last state when with_state (or state_out is
     given), and what selective_scan_backward needs when with_checkpoints."""
-    p = _ssm(x, dt, A, B, C, D, z, dt_bias, state, lengths, softplus)
+    p = _args.ssm(x, dt, A, B, C, D, z, dt_bias, state, lengths, softplus, False)
     batch, _, dim = x.shape
-    y = _into(out, x, x.shape, x.dtype)
+    y = _into(out, x)
     if with_state or state_out is not None:
-        state_out = _into(state_out, x, (batch, dim, A.shape[1]), torch.float32, "state_out")
+        state_out = _into(state_out, x, (batch, dim, A.shape[1]), True, "state_out")
     kept, need, _ = _sizes("selective_scan_bytes", p, 3)
     ckpt = torch.empty(kept // 4, dtype=torch.float32, device=x.device) if with_checkpoints \
         else None
@@ -654,12 +604,12 @@ def selective_scan_backward(dy, checkpoints, x, dt, A, B, C, D=None, z=None, dt_
     dA, dB, dC, dD or None, dz or None, ddt_bias or None, dstate or None): those
     of A, D, dt_bias and state in fp32, the last by default formed when there is
     a state."""
-    p = _ssm(x, dt, A, B, C, D, z, dt_bias, state, lengths, softplus)
-    dev, (batch, _, dim) = x.get_device(), x.shape
+    p = _args.ssm(x, dt, A, B, C, D, z, dt_bias, state, lengths, softplus, False)
+    batch, _, dim = x.shape
     kept, _, need = _sizes("selective_scan_bytes", p, 3)
-    pdy = _arg(dy, "dy", x.dtype, x.shape, dev)
-    pk = _arg(checkpoints, "checkpoints", torch.float32, (kept // 4,), dev, True)
-    pso = _opt(dstate_out, "dstate_out", torch.float32, (batch, dim, A.shape[1]), dev)
+    pdy = _strided(dy, "dy", x)
+    pk = _args.dense(checkpoints, "checkpoints", x, (kept // 4,), True)
+    pso = _args.dense(dstate_out, "dstate_out", x, (batch, dim, A.shape[1]), True)
     if with_dstate is None:
         with_dstate = state is not None
 
@@ -674,8 +624,7 @@ def selective_scan_backward(dy, checkpoints, x, dt, A, B, C, D=None, z=None, dt_
     dbias = new(dim, f32) if dt_bias is not None else None
     dstate = new((batch, dim, A.shape[1]), f32) if with_dstate else None
     buf = _scratch_for(scratch_buf, need, x)
-    _launch("selective_scan_backward", x, p, pdy or None, dy.stride(0), dy.stride(1), pk or None,
-            pso or None, _ptr(dx), _ptr(ddt), _ptr(dA), _ptr(dB), _ptr(dC), _ptr(dD), _ptr(dz),
+    _launch("selective_scan_backward", x, p, pdy, dy.stride(0), dy.stride(1), pk, pso, _ptr(dx), _ptr(ddt), _ptr(dA), _ptr(dB), _ptr(dC), _ptr(dD), _ptr(dz),
             _ptr(dbias), _ptr(dstate), _ptr(buf), buf.numel())
     return dx, ddt, dA, dB, dC, dD, dz, dbias, dstate
 
@@ -685,50 +634,11 @@ def selective_scan_step(x, dt, states, A, B, C, D=None, z=None, dt_bias=None, sl
     """One token of every row: x, dt, z: batch x dim; B, C: batch x groups x n;
     states a pool of dim x n fp32 states (row b's is number slots[b], or b),
     which move on in place.  Returns y, batch x dim."""
-    p = _ssm(x, dt, A, B, C, D, z, dt_bias, None, None, softplus, step=True)
-    tail = tuple(A.shape)
-    psl = _pool(states, x, "states", tail, slots)
-    _arg(states, "states", torch.float32, (states.shape[0], *tail), x.get_device(), True)
-    if slots is None and states.shape[0] < x.shape[0]:
-        raise ValueError("states: fewer than the rows of x")
-    y = _into(out, x, x.shape, x.dtype)
-    _launch("selective_scan_step", x, p, _ptr(states), states.shape[0], psl or None, _ptr(y))
+    p = _args.ssm(x, dt, A, B, C, D, z, dt_bias, None, None, softplus, True)
+    pool = _pool(states, x, tuple(A.shape), True, slots)
+    y = _into(out, x)
+    _launch("selective_scan_step", x, p, *pool, _ptr(y))
     return y
-
-
-def _logits(logits, history, history_len, prompt_len, repetition, presence, frequency, bias_ids,
-            bias_values, allowed, temperature):
-    """A libscan_logits."""
-    code, dev = _first(logits, "logits", 2)
-    rows, vocab = logits.shape
-    i32, f32, row = torch.int32, torch.float32, torch.Size((rows,))
-    pl = _arg(logits, "logits", logits.dtype, logits.shape, dev)
-    ph = hrow = hcols = pids = pval = nb = pal = arow = 0
-    if history is not None:
-        if not isinstance(history, torch.Tensor) or history.dim() != 2:
-            raise TypeError("history: expected a torch.Tensor of rows x tokens")
-        hcols = history.shape[1]
-        ph, hrow = _arg(history, "history", i32, (rows, hcols), dev), history.stride(0)
-    elif not (history_len is prompt_len is repetition is presence is frequency is None):
-        raise ValueError("penalties need a history")
-    if (bias_ids is None) != (bias_values is None):
-        raise ValueError("bias_ids and bias_values go together")
-    if bias_ids is not None:
-        if not isinstance(bias_ids, torch.Tensor) or bias_ids.dim() != 2:
-            raise TypeError("bias_ids: expected a torch.Tensor of rows x entries")
-        nb = bias_ids.shape[1]
-        pids = _arg(bias_ids, "bias_ids", i32, (rows, nb), dev, True)
-        pval = _arg(bias_values, "bias_values", f32, (rows, nb), dev, True)
-    if allowed is not None:
-        pal = _arg(allowed, "allowed", i32, (rows, (vocab + 31) // 32), dev)
-        arow = allowed.stride(0)
-    return _LOGITS.pack(code, rows, vocab, pl, logits.stride(0), ph, hrow, hcols,
-                        _opt(history_len, "history_len", i32, row, dev),
-                        _opt(prompt_len, "prompt_len", i32, row, dev),
-                        _opt(repetition, "repetition", f32, row, dev),
-                        _opt(presence, "presence", f32, row, dev),
-                        _opt(frequency, "frequency", f32, row, dev), pids, pval, nb, pal, arow,
-                        _opt(temperature, "temperature", f32, row, dev))
 
 
 def logits_process(logits, history=None, history_len=None, prompt_len=None, repetition=None,
@@ -743,12 +653,12 @@ def logits_process(logits, history=None, history_len=None, prompt_len=None, repe
     bias_ids (rows x entries).  allowed holds a bit per place, lowest first, in
     rows x ceil(vocab / 32) int32 words: 0 gives -infinity.  All per row.  out may
     be logits itself."""
-    p = _logits(logits, history, history_len, prompt_len, repetition, presence, frequency,
-                bias_ids, bias_values, allowed, None)
+    p = _args.logits(logits, history, history_len, prompt_len, repetition, presence, frequency,
+                     bias_ids, bias_values, allowed, None)
     if out is None:
-        out = torch.empty(logits.shape, dtype=logits.dtype, device=logits.device)
+        out = _args.empty(logits, False)
     else:
-        _arg(out, "out", logits.dtype, logits.shape, logits.get_device())
+        _strided(out, "out", logits)
     _launch("logits_process", logits, p, _ptr(out), out.stride(0))
     return out
 
@@ -759,9 +669,9 @@ def logits_probs(logits, history=None, history_len=None, prompt_len=None, repeti
     """softmax(logits_process(...) / temperature) as fp32 rows x vocab
     probabilities, what topp_sample_f32 takes.  A temperature of 0 gives the
     largest logit's places equal shares; a row with no place left is all 0."""
-    p = _logits(logits, history, history_len, prompt_len, repetition, presence, frequency,
-                bias_ids, bias_values, allowed, temperature)
-    probs = _into(out, logits, logits.shape, torch.float32)
+    p = _args.logits(logits, history, history_len, prompt_len, repetition, presence, frequency,
+                     bias_ids, bias_values, allowed, temperature)
+    probs = _into(out, logits, f32=True)
     need = _sizes("logits_scratch_bytes", p, 1)[0]
     buf = _scratch_for(scratch_buf, need, logits) if need else None
     _launch("logits_probs", logits, p, _ptr(probs), _ptr(buf),
