@@ -154,6 +154,15 @@ def call(name: str, *args):
     return st
 
 
+def address(name: str) -> int:
+    """The address of an entry point, for compiled callers."""
+    lib = _LIB or load()
+    found = lib.__dict__.setdefault("_addresses", {})
+    if name not in found:
+        found[name] = ctypes.cast(getattr(lib, name), _p).value
+    return found[name]
+
+
 def scratch_bytes(op: int, rows: int, length: int, k: int = 0) -> int:
     lib = load()
     out = _sz(0)

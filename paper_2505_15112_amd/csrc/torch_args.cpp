@@ -254,6 +254,34 @@ PyObject* empty(PyObject* const* a) {
     return THPVariable_Wrap(at::empty(like.sizes(), like.options().dtype(type)));
 }
 
+// (address of a size query of libscan.h, struct bytes, sizes): its status, then
+// the sizes
+PyObject* sizes(PyObject* const* a) {
+    void* fn = PyLong_AsVoidPtr(a[0]);
+    const char* p = PyBytes_AsString(a[1]);
+    const long n = PyLong_AsLong(a[2]);
+    if (PyErr_Occurred()) throw Raised();
+    size_t v[3] = {0, 0, 0};
+    int status;
+    if (n == 1)
+        status = ((int (*)(const void*, size_t*))fn)(p, v);
+    else
+        status = ((int (*)(const void*, size_t*, size_t*, size_t*))fn)(p, v, v + 1, v + 2);
+    PyObject* out = PyTuple_New(1 + n);
+    if (!out) throw Raised();
+    PyTuple_SET_ITEM(out, 0, PyLong_FromLong(status));
+    for (long i = 0; i < n; ++i) PyTuple_SET_ITEM(out, 1 + i, PyLong_FromSize_t(v[i]));
+    return out;
+}
+
+// (bytes, like): uninitialised memory on like's GPU
+PyObject* memory(PyObject* const* a) {
+    const int64_t n = PyLong_AsLongLong(a[0]);
+    if (PyErr_Occurred()) throw Raised();
+    return THPVariable_Wrap(
+        at::empty({n}, THPVariable_Unpack(a[1]).options().dtype(at::kByte)));
+}
+
 template <PyObject* (*F)(PyObject* const*), int N>
 PyObject* entry(PyObject*, PyObject* const* args, Py_ssize_t n) {
     if (n != N) {
@@ -272,7 +300,8 @@ PyObject* entry(PyObject*, PyObject* const* args, Py_ssize_t n) {
 
 #define ENTRY(f, n) {#f, (PyCFunction)(void (*)(void))entry<f, n>, METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {ENTRY(conv, 7),  ENTRY(ssm, 12),  ENTRY(logits, 11),
-                         ENTRY(dense, 5), ENTRY(empty, 2), {nullptr, nullptr, 0, nullptr}};
+                         ENTRY(dense, 5), ENTRY(empty, 2), ENTRY(sizes, 3),
+                         ENTRY(memory, 2), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_torch_args", nullptr, -1, methods,
                       nullptr, nullptr, nullptr, nullptr};
 

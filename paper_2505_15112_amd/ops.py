@@ -460,7 +460,7 @@ class _Args:
         module = importlib.util.module_from_spec(spec)
         spec.loader.exec_module(module)
         self.__dict__.update({k: getattr(module, k)
-                              for k in ("conv", "ssm", "logits", "dense", "empty")})
+                              for k in ("conv", "ssm", "logits", "dense", "empty", "sizes", "memory")})
         return self.__dict__[name]
 
 
@@ -480,7 +480,7 @@ def _into(out, like, shape=None, f32=False, name="out"):
 def _scratch_for(buf, nbytes, like):
     """Scratch memory of at least nbytes: the caller's, or new."""
     if buf is None:
-        return torch.empty(max(16, nbytes), dtype=torch.uint8, device=like.device)
+        return _args.memory(max(16, nbytes), like)
     _check(buf, torch.uint8, "scratch_buf")
     return buf
 
@@ -539,9 +539,11 @@ def _strided(t, name, like):
 
 
 def _sizes(cname, p, count):
-    got = [ctypes.c_size_t(0) for _ in range(count)]
-    _lib.call(cname, p, *(ctypes.byref(g) for g in got))
-    return [g.value for g in got]
+    """What a size query of libscan.h reports for a struct."""
+    status, *got = _args.sizes(_lib.address(cname), p, count)
+    if status != _lib.OK:
+        raise _lib.LibscanError(cname, status, _lib.load())
+    return got
 
 
 def _pool(states, x, tail, f32, slots):
