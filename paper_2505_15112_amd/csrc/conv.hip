@@ -1,7 +1,7 @@
 // conv.hip -- the causal depthwise convolution in front of the selective scan.
 //
 // y[t] = f(bias + sum_j w[j] x[t - (W-1) + j]) per channel, W = 2..4.  HBM bounds
-// it: a thread owns 16 bytes of channels and a run of steps, so that every
+// it: a thread owns 8 bytes of channels and a run of steps, so that every
 // input is loaded once (but for the W-1 in front of a run) and the window
 // slides through registers.
 #include "launch.hpp"
@@ -14,16 +14,19 @@ namespace ls {
 namespace {
 
 constexpr int kThreads = 256;
-constexpr int kRun = 16;      // steps a thread owns, forward
-constexpr int kBackRun = 32;  // and backward
+constexpr int kRun = 8;       // steps a thread owns, forward
+// Backward: a thread's run is W-1 steps that only open the window, and these.
+constexpr int kSteady = 28;
+constexpr int kAhead = 4;     // steps a thread loads ahead, backward
 constexpr int kBackV = 4;     // channels of a thread, backward
 constexpr int kBackSide = 32; // threads of a workgroup over channels, backward
 constexpr int kBackRuns = kThreads / kBackSide;
 
+__host__ __device__ constexpr int back_run(int width) { return kSteady + width - 1; }
 // workgroups over the steps of a row, backward (one even where there are none,
 // for the gradient of the first state)
-__host__ __device__ inline int back_runs(int64_t steps) {
-    const int per = kBackRun * kBackRuns;
+__host__ __device__ inline int back_runs(int64_t steps, int width) {
+    const int per = back_run(width) * kBackRuns;
     return steps ? (int)((steps + per - 1) / per) : 1;
 }
 
@@ -33,24 +36,30 @@ __device__ __forceinline__ int conv_len(const libscan_conv& p, int b) {
     return n < 0 ? 0 : n < (int)p.steps ? n : (int)p.steps;
 }
 
-// weight and bias of `V` channels from c0 on, of T or float
+// weight and bias of V channels from c0 on, which lie together in memory
+template <class P, int W, int V>
+__device__ __forceinline__ void load_weights_as(const P* weight, const P* b, int c0, int count,
+                                                float (&w)[W][V], float (&bias)[V]) {
+    Pack<P, V> row[W], br;
+#pragma unroll
+    for (int k = 0; k < W; ++k)
+        row[k].load(weight + (int64_t)c0 * W + k * V, count >= V ? V : count * W - k * V);
+    br.load(b + c0, b ? count : 0);
+#pragma unroll
+    for (int i = 0; i < V; ++i) {
+#pragma unroll
+        for (int j = 0; j < W; ++j) w[j][i] = to_f32(row[(i * W + j) / V].v[(i * W + j) % V]);
+        bias[i] = to_f32(br.v[i]);
+    }
+}
 template <class T, int W, int V>
 __device__ __forceinline__ void load_weights(const libscan_conv& p, int c0, int count,
                                              float (&w)[W][V], float (&bias)[V]) {
-    const bool f32 = p.weight_type == LIBSCAN_F32;
-#pragma unroll
-    for (int i = 0; i < V; ++i) {
-        const bool in = i < count;
-#pragma unroll
-        for (int j = 0; j < W; ++j) {
-            const int64_t at = (int64_t)(c0 + i) * W + j;
-            w[j][i] = !in ? 0.0f
-                          : f32 ? ((const float*)p.weight)[at] : to_f32(((const T*)p.weight)[at]);
-        }
-        bias[i] = !in || !p.bias
-                      ? 0.0f
-                      : f32 ? ((const float*)p.bias)[c0 + i] : to_f32(((const T*)p.bias)[c0 + i]);
-    }
+    if (p.weight_type == LIBSCAN_F32)
+        load_weights_as<float, W, V>((const float*)p.weight, (const float*)p.bias, c0, count, w,
+                                     bias);
+    else
+        load_weights_as<T, W, V>((const T*)p.weight, (const T*)p.bias, c0, count, w, bias);
 }
 
 // x of step t, which may lie in the first state (t >= -(W-1)), or past the end (0)
@@ -65,7 +74,7 @@ __device__ __forceinline__ void load_step(const libscan_conv& p, const T* px, co
 
 template <class T, int W>
 __global__ __launch_bounds__(kThreads) void k_conv(libscan_conv p, T* y, T* state_out) {
-    constexpr int V = 16 / sizeof(T);
+    constexpr int V = 8 / sizeof(T);
     const int dim = (int)p.dim, steps = (int)p.steps;
     const int64_t nc = (dim + V - 1) / V, nr = steps ? (steps + kRun - 1) / kRun : 1;
     const int64_t id = (int64_t)blockIdx.x * kThreads + threadIdx.x;
@@ -158,18 +167,18 @@ struct BackArgs {
 
 // Gradients.  g[t] = dy[t] f'(u[t]), u formed again; dx[t] = sum_j w[j] g[t + W-1 - j],
 // so a thread forms g of its run and of the W-1 steps behind it.
-template <class T, int W>
+template <class T, int W, bool SILU>
 __global__ __launch_bounds__(kThreads) void k_conv_back(libscan_conv p, BackArgs o) {
     constexpr int V = kBackV;
     __shared__ float s_sum[kBackRuns][W + 1][kBackSide * V];
     const int dim = (int)p.dim, steps = (int)p.steps;
     const int side = threadIdx.x % kBackSide, run = threadIdx.x / kBackSide;
     const int nc = (dim + kBackSide * V - 1) / (kBackSide * V);
-    const int nr = back_runs(steps);
+    const int nr = back_runs(steps, W);
     const int cb = blockIdx.x % nc, part = blockIdx.x / nc;  // part = b * nr + rb
     const int b = part / nr, rb = part % nr;
     const int c0 = (cb * kBackSide + side) * V, count = dim - c0, len = conv_len(p, b);
-    const int t0 = (rb * kBackRuns + run) * kBackRun;
+    const int t0 = (rb * kBackRuns + run) * back_run(W);
     const T* px = (const T*)p.x + b * p.x_batch + c0;
     const T* ps = p.state ? (const T*)p.state + (int64_t)b * (W - 1) * dim + c0 : nullptr;
     const T* pdy = (const T*)o.dy + b * o.dy_batch + c0;
@@ -183,67 +192,117 @@ __global__ __launch_bounds__(kThreads) void k_conv_back(libscan_conv p, BackArgs
 #pragma unroll
         for (int j = 0; j < W; ++j) dw[j][c] = 0.0f;
     }
-    // the gradient of input t (t >= -(W-1)) from the W outputs that read it
-    auto input_grad = [&](const float(&g)[W][V], int t, Pack<T, V>& out) {
-        Pack<T, V> so;
-        const int j0 = t - (len - (W - 1));  // its place in the last state
-        so.load(pso + (int64_t)j0 * dim, pso && j0 >= 0 && t < len ? count : 0);
-#pragma unroll
-        for (int c = 0; c < V; ++c) {
-            float v = to_f32(so.v[c]);
-#pragma unroll
-            for (int j = 0; j < W; ++j) v = __builtin_fmaf(w[j][c], g[W - 1 - j][c], v);
-            out.v[c] = from_f32<T>(t < len ? v : 0.0f);
-        }
-    };
-
     if (count > 0 && (t0 < steps || t0 == 0)) {
-        Pack<T, V> x[W];      // x[t - (W-1)] .. x[t]
+        float x[W][V];        // x[t - (W-1)] .. x[t]
         float g[W][V] = {};   // g[t - (W-1)] .. g[t]
 #pragma unroll
-        for (int j = 0; j < W - 1; ++j)
-            load_step<T, W, V>(p, px, ps, t0 - (W - 1) + j, len, count, x[j]);
-        const int end = t0 + kBackRun < steps ? t0 + kBackRun : steps;  // of this run
-#pragma unroll 4
-        for (int t = t0; t < end + W - 1; ++t) {
-            Pack<T, V> dy;
-            load_step<T, W, V>(p, px, ps, t, len, count, x[W - 1]);
-            dy.load(pdy + t * o.dy_step, t < len ? count : 0);
+        for (int j = 0; j < W - 1; ++j) {
+            Pack<T, V> v;
+            load_step<T, W, V>(p, px, ps, t0 - (W - 1) + j, len, count, v);
+#pragma unroll
+            for (int c = 0; c < V; ++c) x[j][c] = to_f32(v.v[c]);
+        }
+        auto load = [&](int t, Pack<T, V>& xt, Pack<T, V>& dy) {
+            const int has = t < len ? count : 0;
+            xt.load(px + t * p.x_step, has);
+            dy.load(pdy + t * o.dy_step, has);
+        };
+        // g of step t, and what it gives the weights
+        auto form = [&](int t, const Pack<T, V>& xt, const Pack<T, V>& dy, bool own) {
 #pragma unroll
             for (int c = 0; c < V; ++c) {
+                x[W - 1][c] = to_f32(xt.v[c]);
                 float gv = to_f32(dy.v[c]);
-                if (p.silu) {
+                if (SILU) {
                     float u = bias[c];
 #pragma unroll
-                    for (int j = 0; j < W; ++j)
-                        u = __builtin_fmaf(w[j][c], to_f32(x[j].v[c]), u);
+                    for (int j = 0; j < W; ++j) u = __builtin_fmaf(w[j][c], x[j][c], u);
                     const float sig = sigmoid(u);
-                    gv *= sig * (1.0f + u * (1.0f - sig));
+                    gv *= sig * __builtin_fmaf(u, 1.0f - sig, 1.0f);
                 }
                 g[W - 1][c] = t < len ? gv : 0.0f;
-                if (t < end) {
+                if (own) {
                     db[c] += g[W - 1][c];
 #pragma unroll
                     for (int j = 0; j < W; ++j)
-                        dw[j][c] = __builtin_fmaf(g[W - 1][c], to_f32(x[j].v[c]), dw[j][c]);
+                        dw[j][c] = __builtin_fmaf(g[W - 1][c], x[j][c], dw[j][c]);
                 }
             }
+        };
+        // the gradient of input t - (W-1), which the W outputs up to t read
+        auto gather = [&](int t, Pack<T, V>& out) {
             const int ti = t - (W - 1);
-            if (ti >= t0) {
-                Pack<T, V> out;
-                input_grad(g, ti, out);
-                out.store(pdx + (int64_t)ti * dim, count);
-            } else if (t0 == 0 && o.dstate) {
-                Pack<T, V> out;
-                input_grad(g, ti, out);
-                out.store((T*)o.dstate + ((int64_t)b * (W - 1) + t) * dim + c0, count);
+            float v[V];
+#pragma unroll
+            for (int c = 0; c < V; ++c) {
+                v[c] = w[0][c] * g[W - 1][c];
+#pragma unroll
+                for (int j = 1; j < W; ++j) v[c] = __builtin_fmaf(w[j][c], g[W - 1 - j][c], v[c]);
+            }
+            const int j0 = ti - (len - (W - 1));  // its place in the last state
+            if (pso && j0 >= 0 && ti < len) {
+                Pack<T, V> so;
+                so.load(pso + (int64_t)j0 * dim, count);
+#pragma unroll
+                for (int c = 0; c < V; ++c) v[c] += to_f32(so.v[c]);
             }
 #pragma unroll
-            for (int j = 0; j < W - 1; ++j) {
-                x[j] = x[j + 1];
+            for (int c = 0; c < V; ++c) out.v[c] = from_f32<T>(ti < len ? v[c] : 0.0f);
+        };
+        auto move = [&]() {
 #pragma unroll
-                for (int c = 0; c < V; ++c) g[j][c] = g[j + 1][c];
+            for (int j = 0; j < W - 1; ++j)
+#pragma unroll
+                for (int c = 0; c < V; ++c) {
+                    x[j][c] = x[j + 1][c];
+                    g[j][c] = g[j + 1][c];
+                }
+        };
+        auto store = [&](int t, const Pack<T, V>& out) {
+            if (t < steps) out.store(pdx + (int64_t)t * dim, count);
+        };
+
+        Pack<T, V> ox[W - 1], ody[W - 1], nx[kAhead], ndy[kAhead];
+#pragma unroll
+        for (int i = 0; i < W - 1; ++i) load(t0 + i, ox[i], ody[i]);
+#pragma unroll
+        for (int i = 0; i < kAhead; ++i) load(t0 + W - 1 + i, nx[i], ndy[i]);
+#pragma unroll
+        for (int i = 0; i < W - 1; ++i) {
+            form(t0 + i, ox[i], ody[i], true);
+            if (t0 == 0 && o.dstate) {
+                Pack<T, V> out;
+                gather(i, out);
+                out.store((T*)o.dstate + ((int64_t)b * (W - 1) + i) * dim + c0, count);
             }
+            move();
+        }
+        int t = t0 + W - 1;
+#pragma unroll 1
+        for (int k = 0; k < kSteady; k += kAhead, t += kAhead) {
+            Pack<T, V> cx[kAhead], cdy[kAhead], out[kAhead];
+#pragma unroll
+            for (int i = 0; i < kAhead; ++i) {
+                cx[i] = nx[i];
+                cdy[i] = ndy[i];
+                load(t + kAhead + i, nx[i], ndy[i]);
+            }
+#pragma unroll
+            for (int i = 0; i < kAhead; ++i) {
+                form(t + i, cx[i], cdy[i], true);
+                gather(t + i, out[i]);
+                move();
+            }
+#pragma unroll
+            for (int i = 0; i < kAhead; ++i) store(t + i - (W - 1), out[i]);
+        }
+#pragma unroll
+        for (int i = 0; i < W - 1; ++i) {  // of the run behind: not this thread's own
+            Pack<T, V> out;
+            form(t + i, nx[i], ndy[i], false);
+            gather(t + i, out);
+            store(t + i - (W - 1), out);
+            move();
         }
     }
 #pragma unroll
@@ -281,14 +340,14 @@ __global__ __launch_bounds__(kThreads) void k_conv_sum(const float* part, int64_
 }
 
 int64_t back_parts(const libscan_conv& p) {
-    return p.batch * back_runs(p.steps);
+    return p.batch * back_runs(p.steps, (int)p.width);
 }
 
 unsigned groups_of(int64_t n, int64_t per) { return (unsigned)((n + per - 1) / per); }
 
 template <class T, int W>
 hipError_t conv_as(const libscan_conv& p, void* y, void* state_out, hipStream_t s) {
-    constexpr int V = 16 / sizeof(T);
+    constexpr int V = 8 / sizeof(T);
     const int64_t nr = p.steps ? (p.steps + kRun - 1) / kRun : 1;
     const int64_t n = (p.dim + V - 1) / V * nr * p.batch;
     k_conv<T, W><<<groups_of(n, kThreads), kThreads, 0, s>>>(p, (T*)y, (T*)state_out);
@@ -310,7 +369,8 @@ hipError_t back_as(const libscan_conv& p, const BackArgs& o, float* dweight, flo
                    hipStream_t s) {
     const int64_t parts = back_parts(p);
     const int64_t nc = (p.dim + kBackSide * kBackV - 1) / (kBackSide * kBackV);
-    if (parts > 0) k_conv_back<T, W><<<(unsigned)(parts * nc), kThreads, 0, s>>>(p, o);
+    auto* back = p.silu ? k_conv_back<T, W, true> : k_conv_back<T, W, false>;
+    if (parts > 0) back<<<(unsigned)(parts * nc), kThreads, 0, s>>>(p, o);
     k_conv_sum<<<groups_of(p.dim * (W + 1), kThreads), kThreads, 0, s>>>(o.part, parts, p.dim, W,
                                                                        dweight, dbias);
     return hipGetLastError();
