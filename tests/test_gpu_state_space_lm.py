@@ -1,0 +1,63 @@
+"""The example model: its parts used together give what they give apart."""
+import importlib.util
+import os
+
+import pytest
+import torch
+
+pytestmark = pytest.mark.gpu
+
+PATH = os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "examples",
+                    "state_space_lm.py")
+
+
+@pytest.fixture(scope="module")
+def lm():
+    spec = importlib.util.spec_from_file_location("state_space_lm", PATH)
+    module = importlib.util.module_from_spec(spec)
+    spec.loader.exec_module(module)
+    return module
+
+
+def data(vocab, rows=3, steps=40):
+    g = torch.Generator(device="cuda").manual_seed(2)
+    ids = torch.randint(0, vocab, (rows, steps), generator=g, device="cuda", dtype=torch.int32)
+    return ids, torch.tensor([40, 17, 1], dtype=torch.int32, device="cuda")
+
+
+def test_tokens_one_by_one_follow_the_prompt(lm):
+    """A prompt extended token by token against the longer prompt at once, in
+    fp32 (the two sum in different orders: 1e-4 of the logits' size)."""
+    model = lm.Model(vocab=500, dim=64, dtype=torch.float32)
+    ids, lengths = data(500)
+    start = lengths - torch.tensor([7, 7, 0], dtype=torch.int32, device="cuda")
+    logits, states = model.prompt(ids, start)
+    for i in range(7):
+        nxt = ids.gather(1, (start + i).clamp(max=39)[:, None].long())[:, 0]
+        logits = model.token(nxt, states)
+    want, last = model.prompt(ids, lengths)
+    assert (logits[:2] - want[:2]).abs().max() <= 1e-4 * want.abs().max()
+    for (window, state), (w2, s2) in zip(states, last):
+        assert (window[:2] - w2[:2]).abs().max() <= 1e-4 * w2.abs().max()
+        assert (state[:2] - s2[:2]).abs().max() <= 1e-4 * s2.abs().max()
+
+
+def test_generation_repeats_and_obeys_the_grammar(lm):
+    model = lm.Model(vocab=1000, dim=64)
+    ids, lengths = data(1000)
+    allowed = torch.zeros(3, 32, dtype=torch.int32, device="cuda")
+    allowed[:, 3] = -1                      # tokens 96 .. 127 alone
+    a = lm.generate(model, ids, lengths, 10, allowed=allowed)
+    b = lm.generate(model, ids, lengths, 10, allowed=allowed)
+    assert torch.equal(a, b)
+    assert bool(((a >= 96) & (a < 128)).all())
+    # heavy penalties leave no token twice while others are there
+    c = lm.generate(model, ids, lengths, 20, allowed=allowed, temperature=0.0, frequency=1e4)
+    assert all(len(set(r)) == 20 for r in c.tolist())
+
+
+def test_training_lowers_the_loss(lm):
+    model = lm.Model(vocab=300, dim=64, dtype=torch.float32)
+    ids, lengths = data(300)
+    losses = [lm.train_step(model, ids, lengths, rate=0.2) for _ in range(8)]
+    assert losses[-1] < 0.8 * losses[0], losses
