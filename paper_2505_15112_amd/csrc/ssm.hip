@@ -19,94 +19,98 @@ namespace {
 constexpr int kTile = 32;     // steps per tile
 constexpr int kThreads = 256;
 
-template <class T, int LN, int SPL>
+// WHOLE: every row has all its steps, in whole tiles, and every workgroup all its
+// channels and states, so that nothing needs a check.
+template <class T, int LN, int SPL, bool WHOLE>
 __global__ __launch_bounds__(kThreads) void k_ssm_scan(libscan_ssm p, T* y, float* state_out,
                                                        float* ckpt, int nb) {
     using L = SsmLanes<LN, SPL>;
-    constexpr int CH = L::CH, NP = L::NP, VW = CH / 8, YS = CH + 4;
+    constexpr int CH = L::CH, NP = L::NP, TPR = kThreads / kTile, VW = CH / TPR, YS = CH + 4;
     constexpr int NBC = kTile * NP / kThreads;
-    __shared__ float2 s_du[kTile][CH];
+    __shared__ float2 s_du[kTile][CH];  // delta, delta x
     __shared__ float2 s_bc[kTile][NP];
     __shared__ float s_y[kTile][YS];
 
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     const int steps = (int)p.steps, dim = (int)p.dim, n = (int)p.n;
     const SsmBlock k = ssm_block(p, nb, CH, blockIdx.x);
-    const int len = ssm_len(p, k.b);
+    const int len = WHOLE ? steps : ssm_len(p, k.b);
+    const int lim = WHOLE ? CH : k.lim;
+    const bool gate = p.z != nullptr;
 
-    // loader: one step, VW channels
-    const int row = tid >> 3, lc = (tid & 7) * VW;
-    const int lcount = k.lim - lc;  // channels of this thread that exist (may be <= 0)
+    // loader: one step, VW channels; NBC states of B and C
+    const int row = tid / TPR, lc = (tid % TPR) * VW;
+    const int lcount = WHOLE ? VW : lim - lc;  // channels that exist (may be <= 0)
     const int64_t ch0 = k.c0 + lc;
-    const T* px = (const T*)p.x + k.b * p.x_batch + ch0;
-    const T* pdt = (const T*)p.dt + k.b * p.dt_batch + ch0;
-    const T* pz = p.z ? (const T*)p.z + k.b * p.z_batch + ch0 : nullptr;
-    const T* pB = (const T*)p.B + k.b * p.B_batch + k.g * p.B_group;
-    const T* pC = (const T*)p.C + k.b * p.C_batch + k.g * p.C_group;
-    T* py = y + ((int64_t)k.b * steps) * dim + ch0;
+    const T* px = (const T*)p.x + k.b * p.x_batch + row * p.x_step + ch0;
+    const T* pdt = (const T*)p.dt + k.b * p.dt_batch + row * p.dt_step + ch0;
+    const T* pz = (const T*)p.z + k.b * p.z_batch + row * p.z_step + ch0;
+    const int bt = tid * NBC / NP, bn = tid * NBC % NP;
+    const T* pB = (const T*)p.B + k.b * p.B_batch + k.g * p.B_group + bt * p.B_step + bn;
+    const T* pC = (const T*)p.C + k.b * p.C_batch + k.g * p.C_group + bt * p.C_step + bn;
+    T* py = y + ((int64_t)k.b * steps + row) * dim + ch0;
     float bias[VW], skip[VW];
 #pragma unroll
     for (int i = 0; i < VW; ++i) {
-        bias[i] = p.dt_bias && i < lcount ? p.dt_bias[ch0 + i] : 0.0f;
-        skip[i] = p.D && i < lcount ? p.D[ch0 + i] : 0.0f;
+        bias[i] = p.dt_bias && (WHOLE || i < lcount) ? p.dt_bias[ch0 + i] : 0.0f;
+        skip[i] = p.D && (WHOLE || i < lcount) ? p.D[ch0 + i] : 0.0f;
     }
 
     // scanner: channel wc, states n0 .. n0 + SPL
     const int wc = wave * L::CPW + L::channel(lane), n0 = L::part(lane) * SPL;
     float a2[SPL], h[SPL];
     const int64_t sbase = ((int64_t)k.b * dim + k.c0 + wc) * n + n0;
+    float* pck = ckpt + ((int64_t)k.b * ((steps + kSsmBlock - 1) / kSsmBlock) * dim + k.c0 + wc) * n +
+                 n0;
 #pragma unroll
     for (int s = 0; s < SPL; ++s) {
-        const bool in = wc < k.lim && n0 + s < n;
+        const bool in = WHOLE || (wc < lim && n0 + s < n);
         a2[s] = in ? p.A[(int64_t)(k.c0 + wc) * n + n0 + s] * kLog2e : 0.0f;
         h[s] = in && p.state ? p.state[sbase + s] : 0.0f;
     }
 
-    Pack<T, VW> rx, rdt, rz;
-    T rB[NBC], rC[NBC];
+    Pack<T, VW> nx, ndt, nz;
+    Pack<T, NBC> nB, nC;
     auto fetch = [&](int t0) {
-        const int t = t0 + row;
-        const int count = t < len ? lcount : 0;
-        rx.load(px + t * p.x_step, count);
-        rdt.load(pdt + t * p.dt_step, count);
-        rz.load(pz + t * p.z_step, pz ? count : 0);
-#pragma unroll
-        for (int i = 0; i < NBC; ++i) {
-            const int e = tid + i * kThreads, tt = t0 + e / NP, nn = e % NP;
-            const bool in = tt < len && nn < n;
-            rB[i] = in ? pB[tt * p.B_step + nn] : T(0);
-            rC[i] = in ? pC[tt * p.C_step + nn] : T(0);
-        }
+        const bool all = WHOLE || (lim == CH && n == NP && t0 + kTile <= len);
+        const int count = all ? VW : t0 + row < len ? lcount : 0;
+        const int bcount = all ? NBC : t0 + bt < len ? n - bn : 0;
+        nx.load(px + t0 * p.x_step, count);
+        ndt.load(pdt + t0 * p.dt_step, count);
+        nz.load(pz + t0 * p.z_step, gate ? count : 0);
+        nB.load(pB + t0 * p.B_step, bcount);
+        nC.load(pC + t0 * p.C_step, bcount);
     };
 
-    fetch(0);
+    if (len > 0) fetch(0);
     for (int t0 = 0; t0 < len; t0 += kTile) {
-        const bool live = t0 + row < len;
+        const bool live = WHOLE || t0 + row < len;
+        const Pack<T, VW> rx = nx, rz = nz;
+        float delta[VW];
+#pragma unroll
+        for (int i = 0; i < VW; ++i) delta[i] = to_f32(ndt.v[i]) + bias[i];
+        if (p.softplus) {
+#pragma unroll
+            for (int i = 0; i < VW; ++i) delta[i] = softplus(delta[i]);
+        }
 #pragma unroll
         for (int i = 0; i < VW; ++i) {
-            float d = to_f32(rdt.v[i]) + bias[i];
-            if (p.softplus) d = softplus(d);
-            d = live && i < lcount ? d : 0.0f;  // past the end: a = 1, b = 0
+            const float d = WHOLE || (live && i < lcount) ? delta[i] : 0.0f;  // then a = 1, b = 0
             s_du[row][lc + i] = float2{d, d * to_f32(rx.v[i])};
         }
 #pragma unroll
-        for (int i = 0; i < NBC; ++i) {
-            const int e = tid + i * kThreads;
-            s_bc[e / NP][e % NP] = float2{to_f32(rB[i]), to_f32(rC[i])};
-        }
-        const Pack<T, VW> cx = rx, cz = rz;
+        for (int i = 0; i < NBC; ++i)
+            s_bc[bt][bn + i] = float2{to_f32(nB.v[i]), to_f32(nC.v[i])};
         __syncthreads();
         if (t0 + kTile < len) fetch(t0 + kTile);
 
 #pragma unroll 1
         for (int tb = 0; tb < kTile; tb += kSsmBlock) {
-            if (ckpt && t0 + tb < len) {
-                const int64_t blk = (int64_t)k.b * ((steps + kSsmBlock - 1) / kSsmBlock) +
-                                    (t0 + tb) / kSsmBlock;
-                float* pc = ckpt + (blk * dim + k.c0 + wc) * n + n0;
+            if (ckpt && (WHOLE || t0 + tb < len)) {
+                float* pc = pck + (int64_t)((t0 + tb) / kSsmBlock) * dim * n;
 #pragma unroll
                 for (int s = 0; s < SPL; ++s)
-                    if (wc < k.lim && n0 + s < n) pc[s] = h[s];
+                    if (WHOLE || (wc < lim && n0 + s < n)) pc[s] = h[s];
             }
             float v[kSsmBlock];
 #pragma unroll
@@ -125,22 +129,26 @@ __global__ __launch_bounds__(kThreads) void k_ssm_scan(libscan_ssm p, T* y, floa
             L::sum_states(v, lane, [&](int t, float sum) { s_y[tb + t][wc] = sum; });
         }
         __syncthreads();
-        if (t0 + row < steps) {
+        if (WHOLE || t0 + row < steps) {
             Pack<T, VW> out;
+            float v[VW];
 #pragma unroll
-            for (int i = 0; i < VW; ++i) {
-                float v = s_y[row][lc + i] + skip[i] * to_f32(cx.v[i]);
-                if (pz) {
-                    const float z = to_f32(cz.v[i]);
-                    v *= z * sigmoid(z);
+            for (int i = 0; i < VW; ++i)
+                v[i] = __builtin_fmaf(skip[i], to_f32(rx.v[i]), s_y[row][lc + i]);
+            if (gate) {
+#pragma unroll
+                for (int i = 0; i < VW; ++i) {
+                    const float z = to_f32(rz.v[i]);
+                    v[i] *= z * sigmoid(z);
                 }
-                out.v[i] = from_f32<T>(live ? v : 0.0f);
             }
-            out.store(py + (int64_t)(t0 + row) * dim, lcount);
+#pragma unroll
+            for (int i = 0; i < VW; ++i) out.v[i] = from_f32<T>(live ? v[i] : 0.0f);
+            out.store(py + (int64_t)t0 * dim, lcount);
         }
     }
     // the steps past the row's tokens that no tile above has reached
-    for (int t = (len + kTile - 1) / kTile * kTile + row; t < steps; t += kTile) {
+    for (int t = (len + kTile - 1) / kTile * kTile; !WHOLE && t + row < steps; t += kTile) {
         Pack<T, VW> out;
 #pragma unroll
         for (int i = 0; i < VW; ++i) out.v[i] = T(0);
@@ -149,7 +157,7 @@ __global__ __launch_bounds__(kThreads) void k_ssm_scan(libscan_ssm p, T* y, floa
     if (state_out) {
 #pragma unroll
         for (int s = 0; s < SPL; ++s)
-            if (wc < k.lim && n0 + s < n) state_out[sbase + s] = h[s];
+            if (WHOLE || (wc < lim && n0 + s < n)) state_out[sbase + s] = h[s];
     }
 }
 
@@ -562,12 +570,14 @@ hipError_t scan_as(const libscan_ssm& p, void* y, float* state_out, float* ckpt,
                    hipStream_t stream) {
     const int nb = ssm_blocks(p, SsmLanes<LN, SPL>::CH);
     const int64_t grid = p.batch * p.groups * nb;
-    k_ssm_scan<T, LN, SPL><<<dim3((unsigned)grid), kThreads, 0, stream>>>(p, (T*)y, state_out,
-                                                                          ckpt, nb);
+    const bool whole = !p.lengths && p.steps % kTile == 0 && p.n == LN * SPL &&
+                       p.dim / p.groups % SsmLanes<LN, SPL>::CH == 0;
+    auto* scan = whole ? k_ssm_scan<T, LN, SPL, true> : k_ssm_scan<T, LN, SPL, false>;
+    scan<<<dim3((unsigned)grid), kThreads, 0, stream>>>(p, (T*)y, state_out, ckpt, nb);
     return hipGetLastError();
 }
 
-// From so many channels on, the tiles of a quad per channel fill the chip
+// From so many channels on, the tiles of eight lanes per channel fill the chip
 // without cutting rows (n <= 16).
 constexpr int64_t kTileChannels = 16384;
 
@@ -636,7 +646,7 @@ hipError_t scan_type(const libscan_ssm& p, void* y, float* state_out, float* ckp
     }
     if (p.n > 32) return scan_as<T, 16, 4>(p, y, state_out, ckpt, stream);
     if (p.n > 16) return scan_as<T, 16, 2>(p, y, state_out, ckpt, stream);
-    if (p.batch * p.dim >= kTileChannels) return scan_as<T, 4, 4>(p, y, state_out, ckpt, stream);
+    if (p.batch * p.dim >= kTileChannels) return scan_as<T, 8, 2>(p, y, state_out, ckpt, stream);
     return scan_as<T, 16, 1>(p, y, state_out, ckpt, stream);
 }
 

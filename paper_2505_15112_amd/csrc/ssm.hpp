@@ -16,7 +16,7 @@ constexpr int kSsmBlock = 16;  // steps between checkpoints
 // the lane, so the larger number of lanes lies there.
 template <int LN_, int SPL_>
 struct SsmLanes {
-    static_assert(LN_ == 4 || LN_ == 8 || LN_ == 16, "lanes of a channel");
+    static_assert(LN_ == 8 || LN_ == 16, "lanes of a channel");
     static constexpr int LN = LN_, SPL = SPL_, NP = LN * SPL, CPW = 64 / LN, CH = 4 * CPW;
     __device__ static __forceinline__ int channel(int lane) {
         return LN == 16 ? lane & 3 : lane / LN;
@@ -28,9 +28,7 @@ struct SsmLanes {
     // t.  Calls put(t, sum) for the steps whose sums end up in this lane.
     template <class F>
     __device__ static __forceinline__ void sum_states(float (&v)[kSsmBlock], int lane, F put) {
-        if constexpr (LN == 4)
-            share<0, 1>(v, lane, put);
-        else if constexpr (LN == 8)
+        if constexpr (LN == 8)
             share<2, 1, 0>(v, lane, put);
         else
             share<5, 4, 3, 2>(v, lane, put);
@@ -38,9 +36,7 @@ struct SsmLanes {
     // The same for sums over the wave's channels, of one state index.
     template <class F>
     __device__ static __forceinline__ void sum_channels(float (&v)[kSsmBlock], int lane, F put) {
-        if constexpr (LN == 4)
-            share<5, 4, 3, 2>(v, lane, put);
-        else if constexpr (LN == 8)
+        if constexpr (LN == 8)
             share<5, 4, 3>(v, lane, put);
         else
             share<0, 1>(v, lane, put);

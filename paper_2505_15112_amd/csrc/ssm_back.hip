@@ -7,7 +7,7 @@
 //   ddelta = sum_i r A + du x       dA = sum_t r delta
 //   dx = du delta + D w             ddt = ddelta softplus'(dt + dt_bias)
 // A workgroup owns CH channels of one row and walks the row backwards in
-// blocks of 16 steps, from the checkpoints that the forward pass left: h and a
+// blocks of 16 steps (staged two at a time), from the checkpoints that the forward pass left: h and a
 // of a block are formed again in registers, then the recurrence of G runs
 // through them.  Sums over a channel's states go to the block's outputs
 // through LDS; sums over channels (dB, dC) are reduced in the workgroup and
@@ -48,226 +48,265 @@ __device__ __forceinline__ void after(float v, LdsIn& p, LdsBc& q) {
     asm volatile("" : "+v"(p), "+v"(q) : "v"(v));
 }
 
-template <class T, int LN, int SPL>
+// WHOLE: every row has all its steps, in whole tiles, and every workgroup all its
+// channels and states, so that nothing needs a check.
+template <class T, int LN, int SPL, bool WHOLE>
 __global__ __launch_bounds__(kThreads) void k_ssm_back(libscan_ssm p, BackArgs o, int nb) {
     using L = SsmLanes<LN, SPL>;
-    constexpr int CH = L::CH, NP = L::NP, VW = CH / 16, YS = CH + 4;
-    constexpr int NBC = (kT * NP + kThreads - 1) / kThreads;
-    __shared__ float4 s_in[kT][CH];            // delta, delta x, w
-    __shared__ float2 s_bc[kT][NP];
-    __shared__ float s_y[kT][YS], s_du[kT][YS], s_dd[kT][YS];
-    __shared__ float2 s_g[4][kT][NP + 1];
+    constexpr int CH = L::CH, NP = L::NP, YS = CH + 4;
+    // steps that are staged together, in blocks of kT; threads to a step, channels to a thread
+    constexpr int TS = NP > 32 ? 16 : 32, SUB = TS / kT, TPR = kThreads / TS, VW = CH / TPR;
+    constexpr int NBC = TS * NP / kThreads;
+    static_assert(VW * TPR == CH && NBC * kThreads == TS * NP, "a tile is shared out evenly");
+    __shared__ float4 s_in[TS][CH];  // delta, delta x, w
+    __shared__ float2 s_bc[TS][NP];
+    __shared__ float s_y[TS][YS], s_du[TS][YS], s_dd[TS][YS];
+    __shared__ float2 s_g[4][TS][NP + 1];
 
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     const int steps = (int)p.steps, dim = (int)p.dim, n = (int)p.n, groups = (int)p.groups;
     const SsmBlock k = ssm_block(p, nb, CH, blockIdx.x);
-    const int len = ssm_len(p, k.b);
+    const int len = WHOLE ? steps : ssm_len(p, k.b);
+    const int lim = WHOLE ? CH : k.lim;
     const int blocks = (steps + kT - 1) / kT;
+    const bool gate = p.z != nullptr;
 
-    const int row = tid >> 4, lc = (tid & 15) * VW;
-    const int lcount = k.lim - lc;
+    const int row = tid / TPR, lc = (tid % TPR) * VW;
+    const int lcount = WHOLE ? VW : lim - lc;
     const int64_t ch0 = k.c0 + lc;
-    const T* px = (const T*)p.x + k.b * p.x_batch + ch0;
-    const T* pdt = (const T*)p.dt + k.b * p.dt_batch + ch0;
-    const T* pz = p.z ? (const T*)p.z + k.b * p.z_batch + ch0 : nullptr;
-    const T* pdy = (const T*)o.dy + k.b * o.dy_batch + ch0;
-    const T* pB = (const T*)p.B + k.b * p.B_batch + k.g * p.B_group;
-    const T* pC = (const T*)p.C + k.b * p.C_batch + k.g * p.C_group;
-    const int64_t obase = (int64_t)k.b * steps * dim + ch0;
+    const T* px = (const T*)p.x + k.b * p.x_batch + row * p.x_step + ch0;
+    const T* pdt = (const T*)p.dt + k.b * p.dt_batch + row * p.dt_step + ch0;
+    const T* pz = (const T*)p.z + k.b * p.z_batch + row * p.z_step + ch0;
+    const T* pdy = (const T*)o.dy + k.b * o.dy_batch + row * o.dy_step + ch0;
+    const int bt = tid * NBC / NP, bn = tid * NBC % NP;
+    const T* pB = (const T*)p.B + k.b * p.B_batch + k.g * p.B_group + bt * p.B_step + bn;
+    const T* pC = (const T*)p.C + k.b * p.C_batch + k.g * p.C_group + bt * p.C_step + bn;
+    const int64_t obase = ((int64_t)k.b * steps + row) * dim + ch0;
     float bias[VW], skip[VW], sum_d[VW], sum_bias[VW];
 #pragma unroll
     for (int i = 0; i < VW; ++i) {
-        bias[i] = p.dt_bias && i < lcount ? p.dt_bias[ch0 + i] : 0.0f;
-        skip[i] = p.D && i < lcount ? p.D[ch0 + i] : 0.0f;
+        bias[i] = p.dt_bias && (WHOLE || i < lcount) ? p.dt_bias[ch0 + i] : 0.0f;
+        skip[i] = p.D && (WHOLE || i < lcount) ? p.D[ch0 + i] : 0.0f;
         sum_d[i] = sum_bias[i] = 0.0f;
     }
 
     const int wc = wave * L::CPW + L::channel(lane), n0 = L::part(lane) * SPL;
     float a2[SPL], da[SPL], cg[SPL];  // cg: a[t+1] G[t+1] of the step that follows
     const int64_t sbase = ((int64_t)k.b * dim + k.c0 + wc) * n + n0;
+    const float* pck = o.ckpt + ((int64_t)k.b * blocks * dim + k.c0 + wc) * n + n0;
 #pragma unroll
     for (int s = 0; s < SPL; ++s) {
-        const bool in = wc < k.lim && n0 + s < n;
+        const bool in = WHOLE || (wc < lim && n0 + s < n);
         a2[s] = in ? p.A[(int64_t)(k.c0 + wc) * n + n0 + s] * kLog2e : 0.0f;
         cg[s] = in && o.dstate_out ? o.dstate_out[sbase + s] : 0.0f;
         da[s] = 0.0f;
     }
 
     // the steps past the row's tokens
-    for (int t = (len + kT - 1) / kT * kT + row; t < steps; t += kT) {
+    for (int t = (len + TS - 1) / TS * TS; !WHOLE && t + row < steps; t += TS) {
         Pack<T, VW> zero;
 #pragma unroll
         for (int i = 0; i < VW; ++i) zero.v[i] = T(0);
         const int64_t at = obase + (int64_t)t * dim;
         zero.store((T*)o.dx + at, lcount);
         zero.store((T*)o.ddt + at, lcount);
-        if (pz) zero.store((T*)o.dz + at, lcount);
+        if (gate) zero.store((T*)o.dz + at, lcount);
     }
 
-    // what a block reads, loaded while the block after it is worked on
+    // What a tile reads, loaded while the tile after it is worked on.  Tiles that
+    // lie inside the row, with all of their channels and states, need no checks.
     Pack<T, VW> nx, ndt, nz, ndy;
-    T nB[NBC], nC[NBC];
-    float nh[SPL];
-    auto fetch = [&](int blk) {
-        const int t0 = blk * kT, count = t0 + row < len ? lcount : 0;
-        nx.load(px + (t0 + row) * p.x_step, count);
-        ndt.load(pdt + (t0 + row) * p.dt_step, count);
-        nz.load(pz + (t0 + row) * p.z_step, pz ? count : 0);
-        ndy.load(pdy + (t0 + row) * o.dy_step, count);
+    Pack<T, NBC> nB, nC;
+    float nh[SUB][SPL];
+    auto fetch = [&](int t0) {
+        const bool all = WHOLE || (lim == CH && n == NP && t0 + TS <= len);
+        const int count = all ? VW : t0 + row < len ? lcount : 0;
+        const int bcount = all ? NBC : t0 + bt < len ? n - bn : 0;
+        nx.load(px + t0 * p.x_step, count);
+        ndt.load(pdt + t0 * p.dt_step, count);
+        nz.load(pz + t0 * p.z_step, gate ? count : 0);
+        ndy.load(pdy + t0 * o.dy_step, count);
+        nB.load(pB + t0 * p.B_step, bcount);
+        nC.load(pC + t0 * p.C_step, bcount);
 #pragma unroll
-        for (int i = 0; i < NBC; ++i) {
-            const int e = tid + i * kThreads, tt = e / NP, nn = e % NP;
-            const bool in = e < kT * NP && t0 + tt < len && nn < n;
-            nB[i] = in ? pB[(t0 + tt) * p.B_step + nn] : T(0);
-            nC[i] = in ? pC[(t0 + tt) * p.C_step + nn] : T(0);
+        for (int sub = 0; sub < SUB; ++sub) {
+            const float* pc = pck + ((int64_t)t0 / kT + sub) * dim * n;
+            const bool there = t0 + sub * kT < len && wc < lim;
+#pragma unroll
+            for (int s = 0; s < SPL; ++s)
+                nh[sub][s] = all || (there && n0 + s < n) ? pc[s] : 0.0f;
         }
-        const float* pc = o.ckpt + (((int64_t)k.b * blocks + blk) * dim + k.c0 + wc) * n + n0;
-#pragma unroll
-        for (int s = 0; s < SPL; ++s) nh[s] = wc < k.lim && n0 + s < n ? pc[s] : 0.0f;
     };
 
-    const int last = (len + kT - 1) / kT - 1;
+    const int last = (len + TS - 1) / TS * TS - TS;
     if (last >= 0) fetch(last);
-    for (int blk = last; blk >= 0; --blk) {
-        const int t0 = blk * kT;
-        const bool live = t0 + row < len;
+    for (int t0 = last; t0 >= 0; t0 -= TS) {
+        const bool live = WHOLE || t0 + row < len;
         const Pack<T, VW> rx = nx, rdt = ndt, rz = nz, rdy = ndy;
-        float h0[SPL];
+        float starts[SUB][SPL];
 #pragma unroll
-        for (int s = 0; s < SPL; ++s) h0[s] = nh[s];
+        for (int sub = 0; sub < SUB; ++sub)
 #pragma unroll
-        for (int i = 0; i < NBC; ++i) {
-            const int e = tid + i * kThreads;
-            if (kT * NP % kThreads == 0 || e < kT * NP)
-                s_bc[e / NP][e % NP] = float2{to_f32(nB[i]), to_f32(nC[i])};
-        }
+            for (int s = 0; s < SPL; ++s) starts[sub][s] = nh[sub][s];
+#pragma unroll
+        for (int i = 0; i < NBC; ++i)
+            s_bc[bt][bn + i] = float2{to_f32(nB.v[i]), to_f32(nC.v[i])};
         float delta[VW], w[VW];
 #pragma unroll
+        for (int i = 0; i < VW; ++i) delta[i] = to_f32(rdt.v[i]) + bias[i];
+        if (p.softplus) {
+#pragma unroll
+            for (int i = 0; i < VW; ++i) delta[i] = softplus(delta[i]);
+        }
+#pragma unroll
         for (int i = 0; i < VW; ++i) {
-            float d = to_f32(rdt.v[i]) + bias[i];
-            if (p.softplus) d = softplus(d);
-            delta[i] = live && i < lcount ? d : 0.0f;
-            const float z = to_f32(rz.v[i]);
-            w[i] = to_f32(rdy.v[i]) * (pz ? z * sigmoid(z) : 1.0f);
+            delta[i] = WHOLE || (live && i < lcount) ? delta[i] : 0.0f;  // past the end: a = 1, b = 0
+            w[i] = to_f32(rdy.v[i]);
+        }
+        if (gate) {
+#pragma unroll
+            for (int i = 0; i < VW; ++i) {
+                const float z = to_f32(rz.v[i]);
+                w[i] *= z * sigmoid(z);
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < VW; ++i)
             s_in[row][lc + i] = float4{delta[i], delta[i] * to_f32(rx.v[i]), w[i], 0.0f};
-        }
-        if (blk > 0) fetch(blk - 1);
+        if (t0 > 0) fetch(t0 - TS);
         __syncthreads();
 
-        float h[kT][SPL], a[kT][SPL];
-        LdsIn in_at = (LdsIn)&s_in[0][wc];
-        LdsBc bc_at = (LdsBc)&s_bc[0][n0];
-        {
-            float hr[SPL], v[kT];
+#pragma unroll 1
+        for (int sub = SUB - 1; sub >= 0; --sub) {
+            const int tb = sub * kT;
+            float h[kT][SPL], a[kT][SPL], h0[SPL];
 #pragma unroll
-            for (int s = 0; s < SPL; ++s) hr[s] = h0[s];
+            for (int s = 0; s < SPL; ++s) h0[s] = sub ? starts[SUB - 1][s] : starts[0][s];
+            LdsIn in_at = (LdsIn)&s_in[tb][wc];
+            LdsBc bc_at = (LdsBc)&s_bc[tb][n0];
+            {
+                float hr[SPL], v[kT];
 #pragma unroll
-            for (int t = 0; t < kT; ++t) {
-                if (t % kGroup == 0) after(hr[0], in_at, bc_at);
-                const float4 in = load_lds(in_at + t * CH);
-                float acc = 0.0f;
+                for (int s = 0; s < SPL; ++s) hr[s] = h0[s];
 #pragma unroll
-                for (int s = 0; s < SPL; ++s) {
-                    const float2 bc = load_lds(bc_at + t * NP + s);
-                    a[t][s] = exp2_fast(in.x * a2[s]);
-                    hr[s] = __builtin_fmaf(a[t][s], hr[s], in.y * bc.x);
-                    h[t][s] = hr[s];
-                    acc = __builtin_fmaf(hr[s], bc.y, acc);
+                for (int t = 0; t < kT; ++t) {
+                    if (t % kGroup == 0) after(hr[0], in_at, bc_at);
+                    const float4 in = load_lds(in_at + t * CH);
+                    float acc = 0.0f;
+#pragma unroll
+                    for (int s = 0; s < SPL; ++s) {
+                        const float2 bc = load_lds(bc_at + t * NP + s);
+                        a[t][s] = exp2_fast(in.x * a2[s]);
+                        hr[s] = __builtin_fmaf(a[t][s], hr[s], in.y * bc.x);
+                        h[t][s] = hr[s];
+                        acc = __builtin_fmaf(hr[s], bc.y, acc);
+                    }
+                    v[t] = acc;
                 }
-                v[t] = acc;
+                if (gate) L::sum_states(v, lane, [&](int t, float sum) { s_y[tb + t][wc] = sum; });
             }
-            if (pz) L::sum_states(v, lane, [&](int t, float sum) { s_y[t][wc] = sum; });
-        }
-        {
-            float vu[kT], vd[kT];
+            {
+                float vu[kT], vd[kT];
 #pragma unroll
-            for (int t = kT - 1; t >= 0; --t) {
-                if (t % kGroup == kGroup - 1) after(cg[0], in_at, bc_at);
-                const float4 in = load_lds(in_at + t * CH);
-                float du = 0.0f, dd = 0.0f;
+                for (int t = kT - 1; t >= 0; --t) {
+                    if (t % kGroup == kGroup - 1) after(cg[0], in_at, bc_at);
+                    const float4 in = load_lds(in_at + t * CH);
+                    float du = 0.0f, dd = 0.0f;
 #pragma unroll
-                for (int s = 0; s < SPL; ++s) {
-                    const float2 bc = load_lds(bc_at + t * NP + s);
-                    const float g = __builtin_fmaf(in.z, bc.y, cg[s]);
-                    du = __builtin_fmaf(g, bc.x, du);
-                    cg[s] = a[t][s] * g;
-                    const float r = cg[s] * (t ? h[t ? t - 1 : 0][s] : h0[s]);
-                    dd = __builtin_fmaf(r, a2[s], dd);
-                    da[s] = __builtin_fmaf(r, in.x, da[s]);
-                    a[t][s] = g * in.y;  // a and h of this step are done with: dB and dC
-                    h[t][s] *= in.z;
-                    // formed here and now: put off, the products hold both factors
-                    asm volatile("" : "+v"(a[t][s]), "+v"(h[t][s]));
+                    for (int s = 0; s < SPL; ++s) {
+                        const float2 bc = load_lds(bc_at + t * NP + s);
+                        const float g = __builtin_fmaf(in.z, bc.y, cg[s]);
+                        du = __builtin_fmaf(g, bc.x, du);
+                        cg[s] = a[t][s] * g;
+                        const float r = cg[s] * (t ? h[t ? t - 1 : 0][s] : h0[s]);
+                        dd = __builtin_fmaf(r, a2[s], dd);
+                        da[s] = __builtin_fmaf(r, in.x, da[s]);
+                        a[t][s] = g * in.y;  // a and h of this step are done with: dB and dC
+                        h[t][s] *= in.z;
+                        // formed here and now: put off, the products hold both factors
+                        asm volatile("" : "+v"(a[t][s]), "+v"(h[t][s]));
+                    }
+                    vu[t] = du;
+                    vd[t] = dd;
+                    asm volatile("" : "+v"(vu[t]), "+v"(vd[t]));
                 }
-                vu[t] = du;
-                vd[t] = dd;
-                asm volatile("" : "+v"(vu[t]), "+v"(vd[t]));
+                L::sum_states(vu, lane, [&](int t, float sum) { s_du[tb + t][wc] = sum; });
+                L::sum_states(vd, lane, [&](int t, float sum) { s_dd[tb + t][wc] = sum; });
             }
-            L::sum_states(vu, lane, [&](int t, float sum) { s_du[t][wc] = sum; });
-            L::sum_states(vd, lane, [&](int t, float sum) { s_dd[t][wc] = sum; });
-        }
 #pragma unroll
-        for (int s = 0; s < SPL; ++s) {
-            float v[kT], u[kT];
+            for (int s = 0; s < SPL; ++s) {
+                float v[kT], u[kT];
 #pragma unroll
-            for (int t = 0; t < kT; ++t) {
-                v[t] = a[t][s];
-                u[t] = h[t][s];
+                for (int t = 0; t < kT; ++t) {
+                    v[t] = a[t][s];
+                    u[t] = h[t][s];
+                }
+                L::sum_channels(v, lane,
+                                [&](int t, float sum) { s_g[wave][tb + t][n0 + s].x = sum; });
+                L::sum_channels(u, lane,
+                                [&](int t, float sum) { s_g[wave][tb + t][n0 + s].y = sum; });
             }
-            L::sum_channels(v, lane, [&](int t, float sum) { s_g[wave][t][n0 + s].x = sum; });
-            L::sum_channels(u, lane, [&](int t, float sum) { s_g[wave][t][n0 + s].y = sum; });
         }
         __syncthreads();
 
-        if (t0 + row < steps) {
+        if (WHOLE || t0 + row < steps) {
             Pack<T, VW> ox, odt, oz;
+            float ddt[VW];
 #pragma unroll
             for (int i = 0; i < VW; ++i) {
                 const float x = to_f32(rx.v[i]), du = s_du[row][lc + i];
-                const float v = to_f32(rdt.v[i]) + bias[i];
-                float ddt = __builtin_fmaf(du, x, s_dd[row][lc + i] * kLn2);
-                if (p.softplus) ddt *= sigmoid(v);
                 const float dx = __builtin_fmaf(du, delta[i], skip[i] * w[i]);
                 ox.v[i] = from_f32<T>(live ? dx : 0.0f);
-                odt.v[i] = from_f32<T>(live ? ddt : 0.0f);
-                if (pz) {
-                    const float z = to_f32(rz.v[i]), sig = sigmoid(z);
-                    const float yv = s_y[row][lc + i] + skip[i] * x;
-                    const float dz = to_f32(rdy.v[i]) * yv * sig * (1.0f + z * (1.0f - sig));
-                    oz.v[i] = from_f32<T>(live ? dz : 0.0f);
-                }
-                if (live && i < lcount) {
-                    sum_d[i] = __builtin_fmaf(w[i], x, sum_d[i]);
-                    sum_bias[i] += ddt;
-                }
+                ddt[i] = __builtin_fmaf(du, x, s_dd[row][lc + i] * kLn2);
+                sum_d[i] = __builtin_fmaf(w[i], x, sum_d[i]);  // both 0 past the end
             }
-            const int64_t at = obase + (int64_t)(t0 + row) * dim;
+            if (p.softplus) {
+#pragma unroll
+                for (int i = 0; i < VW; ++i) ddt[i] *= sigmoid(to_f32(rdt.v[i]) + bias[i]);
+            }
+#pragma unroll
+            for (int i = 0; i < VW; ++i) {
+                ddt[i] = WHOLE || (live && i < lcount) ? ddt[i] : 0.0f;
+                odt.v[i] = from_f32<T>(ddt[i]);
+                sum_bias[i] += ddt[i];
+            }
+            const int64_t at = obase + (int64_t)t0 * dim;
             ox.store((T*)o.dx + at, lcount);
             odt.store((T*)o.ddt + at, lcount);
-            if (pz) oz.store((T*)o.dz + at, lcount);
+            if (gate) {
+#pragma unroll
+                for (int i = 0; i < VW; ++i) {
+                    const float z = to_f32(rz.v[i]), sig = sigmoid(z);
+                    const float yv = __builtin_fmaf(skip[i], to_f32(rx.v[i]), s_y[row][lc + i]);
+                    const float dz = to_f32(rdy.v[i]) * yv * sig *
+                                     __builtin_fmaf(z, 1.0f - sig, 1.0f);
+                    oz.v[i] = from_f32<T>(live ? dz : 0.0f);
+                }
+                oz.store((T*)o.dz + at, lcount);
+            }
         }
-        for (int e = tid; e < kT * NP; e += kThreads) {
-            const int tt = e / NP, nn = e % NP;
-            if (nn < n && t0 + tt < len) {
-                float2 sum = s_g[0][tt][nn];
+#pragma unroll
+        for (int i = 0; i < NBC; ++i) {
+            if (WHOLE || (t0 + bt < len && bn + i < n)) {
+                float2 sum = s_g[0][bt][bn + i];
 #pragma unroll
                 for (int wv = 1; wv < 4; ++wv) {
-                    sum.x += s_g[wv][tt][nn].x;
-                    sum.y += s_g[wv][tt][nn].y;
+                    sum.x += s_g[wv][bt][bn + i].x;
+                    sum.y += s_g[wv][bt][bn + i].y;
                 }
-                o.part_bc[((((int64_t)k.k * p.batch + k.b) * steps + t0 + tt) * groups + k.g) * n +
-                          nn] = sum;
+                o.part_bc[((((int64_t)k.k * p.batch + k.b) * steps + t0 + bt) * groups + k.g) * n +
+                          bn + i] = sum;
             }
         }
     }
 
 #pragma unroll
     for (int s = 0; s < SPL; ++s)
-        if (wc < k.lim && n0 + s < n) {
+        if (WHOLE || (wc < lim && n0 + s < n)) {
             if (o.dstate) o.dstate[sbase + s] = cg[s];
             o.part_a[sbase + s] = da[s];
         }
-    // dD and ddt_bias: the 16 threads of each channel, in order
+    // dD and ddt_bias: the TS threads of each channel, in order
     __syncthreads();
 #pragma unroll
     for (int i = 0; i < VW; ++i) {
@@ -275,9 +314,9 @@ __global__ __launch_bounds__(kThreads) void k_ssm_back(libscan_ssm p, BackArgs o
         s_du[row][lc + i] = sum_bias[i];
     }
     __syncthreads();
-    if (tid < k.lim) {
+    if (tid < lim) {
         float d = 0.0f, e = 0.0f;
-        for (int r = 0; r < 16; ++r) {
+        for (int r = 0; r < TS; ++r) {
             d += s_y[r][tid];
             e += s_du[r][tid];
         }
@@ -340,7 +379,11 @@ size_t align16(size_t v) { return (v + 15) / 16 * 16; }
 template <class T, int LN, int SPL>
 void back_as(const libscan_ssm& p, const BackArgs& o, int nb, hipStream_t stream) {
     const int64_t grid = p.batch * p.groups * nb;
-    if (grid > 0) k_ssm_back<T, LN, SPL><<<dim3((unsigned)grid), kThreads, 0, stream>>>(p, o, nb);
+    if (grid == 0) return;
+    const bool whole = !p.lengths && p.steps % 32 == 0 && p.n == LN * SPL &&
+                       p.dim / p.groups % SsmLanes<LN, SPL>::CH == 0;
+    auto* back = whole ? k_ssm_back<T, LN, SPL, true> : k_ssm_back<T, LN, SPL, false>;
+    back<<<dim3((unsigned)grid), kThreads, 0, stream>>>(p, o, nb);
 }
 
 template <class T>
