@@ -163,23 +163,6 @@ __global__ __launch_bounds__(kThreads) void k_ssm_scan(libscan_ssm p, T* y, floa
 
 // ---------------------------------------------------------------- long rows
 
-typedef const __attribute__((address_space(4))) float* ScalarPtr;
-
-// B and C as fp32, in groups of GP states (GP of B, then GP of C; padding and the
-// steps past a row's tokens are 0), as the scanning waves read them with scalar
-// loads: one group at a time, the next one on its way while the last is used.
-template <int NP>
-struct LaneGroups {
-    static constexpr int GP = NP < 16 ? NP : 16, NG = NP / GP;
-    float v[2 * GP];
-    template <int COUNT>
-    __device__ __forceinline__ void load(ScalarPtr p) {
-        asm volatile("" : "+s"(p));  // not earlier than here
-#pragma unroll
-        for (int i = 0; i < COUNT; ++i) v[i] = p[i];
-    }
-};
-
 template <class T, int NP>
 __global__ __launch_bounds__(kThreads) void k_ssm_bc(libscan_ssm p, float* bc) {
     constexpr int GP = LaneGroups<NP>::GP;
@@ -196,89 +179,6 @@ __global__ __launch_bounds__(kThreads) void k_ssm_bc(libscan_ssm p, float* bc) {
     out[GP] = in ? to_f32(pC[nn]) : 0.0f;
 }
 
-// Waits for the scalar loads in flight, which return in no order, before new
-// ones start, and keeps the compiler from mixing the two.
-__device__ __forceinline__ void scalar_loads_done() {
-    __builtin_amdgcn_sched_barrier(0);
-    __builtin_amdgcn_s_waitcnt(0xC07F);  // lgkmcnt(0)
-    __builtin_amdgcn_sched_barrier(0);
-}
-
-// Waves of a workgroup: neighbours in channels, on the same steps, so that all
-// but the first to get there find B and C in the scalar cache.
-constexpr int kLaneWaves = 8;
-
-// The channel block and chunk of steps of a wave.
-struct LaneBlock {
-    SsmBlock k;
-    int c, t0, end, len;  // steps t0 .. end of chunk c are this wave's; end <= len
-    uint32_t lo;          // this lane's channel after k.c0; lanes past the last channel double
-                          // it, and store what it stores
-};
-__device__ __forceinline__ LaneBlock lane_block(const libscan_ssm& p, int nb, int chunk) {
-    LaneBlock r;
-    r.k = ssm_block(p, nb, kWave, blockIdx.x * kLaneWaves + uni(threadIdx.x / kWave));
-    r.c = blockIdx.y;
-    r.len = ssm_len(p, r.k.b);
-    r.t0 = r.c * chunk;
-    r.end = r.t0 + chunk < r.len ? r.t0 + chunk : r.len;
-    const int lane = threadIdx.x % kWave;
-    r.lo = (uint32_t)(lane < r.k.lim ? lane : r.k.lim - 1);
-    return r;
-}
-
-// A row of a tensor at one step after the other: the address is uniform and
-// stays in one pair of scalar registers (the empty asm keeps the compiler from
-// holding the multiples of the stride instead), the lanes add their channel.
-template <class T>
-struct StepPtr {
-    __attribute__((address_space(1))) T* p;
-    int64_t stride;
-    __device__ __forceinline__ StepPtr(T* first, int64_t step)
-        : p((__attribute__((address_space(1))) T*)first), stride(step) {}
-    __device__ __forceinline__ void next() {
-        p += stride;
-        asm("" : "+s"(p));
-    }
-};
-
-// The step sizes of COUNT steps, in the lane that owns the channel (one branch
-// for all of them: branches between the steps would keep them apart).
-template <int COUNT, class T>
-__device__ __forceinline__ void step_sizes(const libscan_ssm& p, const T (&dt)[COUNT], float bias,
-                                           float (&delta)[COUNT]) {
-#pragma unroll
-    for (int i = 0; i < COUNT; ++i) delta[i] = to_f32(dt[i]) + bias;
-    if (p.softplus) {
-#pragma unroll
-        for (int i = 0; i < COUNT; ++i) delta[i] = softplus(delta[i]);
-    }
-}
-
-constexpr int kAhead = 8;  // steps whose inputs a lane loads together
-
-// A lane's states (or rates): `have` consecutive floats, 0 after them.
-template <int NP>
-__device__ __forceinline__ void load_states(const float* p, int have, float (&v)[NP]) {
-#pragma unroll
-    for (int i = 0; i < NP; i += 4) {
-        Pack<float, 4> w;
-        w.load(p + i, have - i);
-#pragma unroll
-        for (int j = 0; j < 4; ++j) v[i + j] = w.v[j];
-    }
-}
-template <int NP>
-__device__ __forceinline__ void store_states(float* p, int have, const float (&v)[NP]) {
-#pragma unroll
-    for (int i = 0; i < NP; i += 4) {
-        Pack<float, 4> w;
-#pragma unroll
-        for (int j = 0; j < 4; ++j) w.v[j] = v[i + j];
-        w.store(p + i, have - i);
-    }
-}
-
 // The scan with a channel to a lane, all of its states in registers, and one
 // wave to a workgroup: B and C are the same for all lanes and come by scalar
 // loads, so that a step costs five vector instructions for each state (one of
@@ -293,7 +193,7 @@ __global__ __launch_bounds__(kWave * kLaneWaves) void k_ssm_lanes(libscan_ssm p,
     using Groups = LaneGroups<NP>;
     constexpr int GP = Groups::GP, NG = Groups::NG;
     if (blockIdx.x * kLaneWaves + threadIdx.x / kWave >= waves) return;
-    const LaneBlock w = lane_block(p, nb, chunk);
+    const LaneBlock w = lane_block(p, nb, chunk, blockIdx.y);
     const int b = w.k.b, c0 = w.k.c0, ch = c0 + (int)w.lo;
     const uint32_t lo = w.lo;
     const int dim = (int)p.dim, n = (int)p.n, steps = (int)p.steps;
@@ -408,7 +308,7 @@ __global__ __launch_bounds__(kWave * kLaneWaves) void k_ssm_ends(libscan_ssm p, 
     using Groups = LaneGroups<NP>;
     constexpr int GP = Groups::GP, NG = Groups::NG;
     if (blockIdx.x * kLaneWaves + threadIdx.x / kWave >= waves) return;
-    const LaneBlock w = lane_block(p, nb, chunk);
+    const LaneBlock w = lane_block(p, nb, chunk, blockIdx.y);
     const int b = w.k.b, c0 = w.k.c0, ch = c0 + (int)w.lo;
     const uint32_t lo = w.lo;
     const int dim = (int)p.dim, n = (int)p.n;
@@ -480,31 +380,31 @@ __global__ __launch_bounds__(kWave * kLaneWaves) void k_ssm_ends(libscan_ssm p, 
     sums[row] = sum;
 }
 
-// The states that the chunks start from, in the place of the ends (of which
-// the last chunk has none).
 template <int NP>
-__global__ __launch_bounds__(kThreads) void k_ssm_starts(libscan_ssm p, float* ends,
-                                                         const float* sums, int chunks) {
+__global__ __launch_bounds__(kThreads) void k_ssm_starts(libscan_ssm p, const float* init,
+                                                         float* ends, const float* sums,
+                                                         int chunks, bool backward) {
     const int64_t i = (int64_t)blockIdx.x * kThreads + threadIdx.x, rows = p.batch * p.dim;
     if (i >= rows * NP) return;
     const int64_t row = i / NP;
     const int nn = (int)(i % NP);
     const float a2 = nn < p.n ? p.A[row % p.dim * p.n + nn] * kLog2e : 0.0f;
-    float h = p.state && nn < p.n ? p.state[row * p.n + nn] : 0.0f;
+    float h = init && nn < p.n ? init[row * p.n + nn] : 0.0f;
     constexpr int kBatch = 16;  // loads in flight together
-    for (int c0 = 0; c0 < chunks; c0 += kBatch) {
+    for (int j0 = 0; j0 < chunks; j0 += kBatch) {
         float e[kBatch], s[kBatch];
 #pragma unroll
         for (int j = 0; j < kBatch; ++j) {
-            const bool in = c0 + j + 1 < chunks;
-            const int64_t at = (int64_t)(c0 + j) * rows;
+            const bool in = j0 + j + 1 < chunks;
+            const int64_t at = (int64_t)(backward ? chunks - 1 - j0 - j : j0 + j) * rows;
             e[j] = in ? ends[at * NP + i] : 0.0f;
             s[j] = in ? sums[at + row] : 0.0f;
         }
 #pragma unroll
         for (int j = 0; j < kBatch; ++j)
-            if (c0 + j < chunks) {
-                ends[(int64_t)(c0 + j) * rows * NP + i] = h;
+            if (j0 + j < chunks) {
+                const int64_t at = (int64_t)(backward ? chunks - 1 - j0 - j : j0 + j) * rows;
+                ends[at * NP + i] = h;
                 h = __builtin_fmaf(exp2_fast(s[j] * a2), h, e[j]);
             }
     }
@@ -587,20 +487,40 @@ struct LanePlan {
     int np, nb, chunk, chunks;
     size_t bc, ends, sums;  // bytes of scratch
 };
+// The time of either way in us, as measured over 1 to 16 rows of 64 to 8192 steps and
+// 70 to 4096 channels with 8 to 64 states.  The tiles walk a row at a step's
+// latency, and share SIMDs beyond 4096 channels.  The chunks have four kernels and
+// two chunks' steps to wait for, and then the vector units to keep busy.
+// E.g. n = 16, tiles against chunks: 1 x 512 x 1024 26.6 and 29.5, 1 x 1024 x 4096 51.5
+// and 51.8, 1 x 2048 x 1024 96 and 44, 1 x 8192 x 512 373 and 66, 2 x 2048 x 4096 118
+// and 124 us.
+bool chunks_pay(const libscan_ssm& p, int np) {
+    const int64_t channels = p.batch * p.dim;
+    const double over = channels > 4096 ? (double)(channels - 4096) : 0.0;
+    const double step = 0.031 + 0.00103 * (np < 16 ? 16 : np);
+    const double tiles = (double)p.steps * step * (1.0 + 6.6e-5 * over);
+    const double chunks = 14.0 + 0.9 * np + 0.36e-6 * np * (double)p.steps * (double)channels;
+    return chunks < tiles;
+}
+
 LanePlan lane_plan(const libscan_ssm& p) {
     LanePlan r{0, 0, 0, 0, 0, 0, 0};
     if (p.batch == 0 || p.dim == 0) return r;
-    const int64_t per = p.dim / p.groups;
-    if (p.steps < 64 || per < 48 || (p.n <= 16 && p.batch * p.dim >= kTileChannels)) return r;
     r.np = p.n <= 8 ? 8 : p.n <= 16 ? 16 : p.n <= 32 ? 32 : 64;
+    // (a wave of few channels of a group would leave most lanes without work)
+    if (p.steps < 64 || p.dim / p.groups < 48 || !chunks_pay(p, r.np)) {
+        r.np = 0;
+        return r;
+    }
     r.nb = ssm_blocks(p, kWave);
     const int64_t waves = p.batch * p.groups * r.nb;
     int64_t chunks = (4096 + waves - 1) / waves;  // 4 waves to each of the 1024 SIMDs
-    if (chunks > p.steps / 32) chunks = p.steps / 32;
+    // a chunk's steps pass one after the other, but more chunks are more to chain
+    const int64_t least = p.steps > 4096 ? 32 : 16;
+    if (chunks > p.steps / least) chunks = p.steps / least;
     r.chunk = (int)(((p.steps + chunks - 1) / chunks + kSsmBlock - 1) / kSsmBlock * kSsmBlock);
     r.chunks = (int)((p.steps + r.chunk - 1) / r.chunk);
-    // one more token, which the last scalar load of a row runs into
-    r.bc = (size_t)(p.batch * p.steps + 1) * p.groups * 2 * r.np * 4;
+    r.bc = ssm_bc_bytes(p, r.np);
     if (r.chunks > 1) {
         r.ends = (size_t)r.chunks * p.batch * p.dim * r.np * 4;
         r.sums = (size_t)r.chunks * p.batch * p.dim * 4;
@@ -614,17 +534,13 @@ hipError_t lanes_as(const libscan_ssm& p, const LanePlan& l, void* y, float* sta
     float* bc = (float*)scratch;
     float* ends = bc + l.bc / 4;
     float* sums = ends + l.ends / 4;
-    const int64_t words = p.batch * p.steps * p.groups * NP;
-    k_ssm_bc<T, NP><<<dim3((unsigned)((words + kThreads - 1) / kThreads)), kThreads, 0, stream>>>(
-        p, bc);
+    launch_ssm_bc(p, NP, bc, stream);
     const unsigned waves = (unsigned)(p.batch * p.groups * l.nb);
     const unsigned grid = (waves + kLaneWaves - 1) / kLaneWaves;
     if (l.chunks > 1) {
         k_ssm_ends<T, NP><<<dim3(grid, l.chunks - 1), kWave * kLaneWaves, 0, stream>>>(
             p, bc, ends, sums, l.nb, l.chunk, waves);
-        const int64_t states = p.batch * p.dim * NP;
-        k_ssm_starts<NP><<<dim3((unsigned)((states + kThreads - 1) / kThreads)), kThreads, 0,
-                           stream>>>(p, ends, sums, l.chunks);
+        launch_ssm_starts(p, NP, p.state, ends, sums, l.chunks, false, stream);
     }
     auto* scan = p.z ? k_ssm_lanes<T, NP, true> : k_ssm_lanes<T, NP, false>;
     scan<<<dim3(grid, l.chunks), kWave * kLaneWaves, 0, stream>>>(
@@ -651,6 +567,38 @@ hipError_t scan_type(const libscan_ssm& p, void* y, float* state_out, float* ckp
 }
 
 }  // namespace
+
+size_t ssm_bc_bytes(const libscan_ssm& p, int np) {
+    // one more token, which the last scalar load of a row runs into
+    return (size_t)(p.batch * p.steps + 1) * p.groups * 2 * np * 4;
+}
+
+void launch_ssm_bc(const libscan_ssm& p, int np, float* bc, hipStream_t stream) {
+    const dim3 grid((unsigned)((p.batch * p.steps * p.groups * np + kThreads - 1) / kThreads));
+    auto with = [&](auto t) {
+        using T = decltype(t);
+        auto* k = np == 8    ? k_ssm_bc<T, 8>
+                  : np == 16 ? k_ssm_bc<T, 16>
+                  : np == 32 ? k_ssm_bc<T, 32>
+                             : k_ssm_bc<T, 64>;
+        k<<<grid, kThreads, 0, stream>>>(p, bc);
+    };
+    switch (p.type) {
+        case LIBSCAN_F16: with(_Float16()); break;
+        case LIBSCAN_BF16: with(__bf16()); break;
+        default: with(float());
+    }
+}
+
+void launch_ssm_starts(const libscan_ssm& p, int np, const float* init, float* ends,
+                       const float* sums, int chunks, bool backward, hipStream_t stream) {
+    const dim3 grid((unsigned)((p.batch * p.dim * np + kThreads - 1) / kThreads));
+    auto* k = np == 8    ? k_ssm_starts<8>
+              : np == 16 ? k_ssm_starts<16>
+              : np == 32 ? k_ssm_starts<32>
+                         : k_ssm_starts<64>;
+    k<<<grid, kThreads, 0, stream>>>(p, init, ends, sums, chunks, backward);
+}
 
 size_t ssm_scratch_bytes(const libscan_ssm& p) {
     const LanePlan l = lane_plan(p);

@@ -31,10 +31,106 @@ struct BackArgs {
     void *dx, *ddt, *dz;
     float* dstate;
     float2* part_bc;  // [block of the group][batch][step][group][n] of (dB, dC)
-    float* part_a;    // [batch][dim][n]
-    float* part_d;    // [batch][dim]
-    float* part_bias; // [batch][dim]
+    float* part_a;    // [chunk][batch][dim][n]
+    float* part_d;    // [chunk][batch][dim]
+    float* part_bias; // [chunk][batch][dim]
+    // steps of a chunk (blockIdx.y) of the rows; with more than one, a[t] G[t] of the
+    // steps that follow its pieces, [piece][batch][dim][np], `split` pieces to a chunk
+    int chunk, np, split, pieces;
+    const float* starts;
 };
+
+// What a chunk gives the chunk before it from nothing behind it, and its sum of
+// delta (as k_ssm_ends in ssm.hip, backwards in time).
+template <class T, int NP>
+__global__ __launch_bounds__(kWave * kLaneWaves) void k_ssm_back_ends(libscan_ssm p, const void* dy,
+                                                                      int64_t dy_batch,
+                                                                      int64_t dy_step,
+                                                                      const float* bc_, float* ends,
+                                                                      float* sums, int nb,
+                                                                      int chunk, uint32_t waves) {
+    using Groups = LaneGroups<NP>;
+    constexpr int GP = Groups::GP, NG = Groups::NG;
+    if (blockIdx.x * kLaneWaves + threadIdx.x / kWave >= waves) return;
+    const LaneBlock w = lane_block(p, nb, chunk, blockIdx.y + 1);  // the first chunk has none before
+    const int b = w.k.b, c0 = w.k.c0, ch = c0 + (int)w.lo;
+    const uint32_t lo = w.lo;
+    const int dim = (int)p.dim, n = (int)p.n;
+    const bool gate = p.z != nullptr;
+    float a2[NP], cg[NP], sum = 0.0f;
+    load_states<NP>(p.A + (int64_t)ch * n, n, a2);
+#pragma unroll
+    for (int i = 0; i < NP; ++i) {
+        a2[i] *= kLog2e;
+        cg[i] = 0.0f;
+    }
+    if (w.t0 < w.end) {
+        const int t1 = w.end - 1;
+        const int64_t bc_step = p.groups * 2 * NP;
+        // C follows B in every group
+        ScalarPtr bc = (ScalarPtr)bc_ + (((int64_t)b * p.steps + t1) * p.groups + w.k.g) * 2 * NP + GP;
+        StepPtr<const T> pdt((const T*)p.dt + b * p.dt_batch + t1 * p.dt_step + c0, -p.dt_step);
+        StepPtr<const T> pdy((const T*)dy + b * dy_batch + t1 * dy_step + c0, -dy_step);
+        StepPtr<const T> pz(gate ? (const T*)p.z + b * p.z_batch + t1 * p.z_step + c0 : nullptr,
+                            -p.z_step);
+        const float bias = p.dt_bias ? p.dt_bias[ch] : 0.0f;
+        Groups cur;
+        cur.template load<GP>(bc);
+        T nx[kAhead], ndt[kAhead], nz[kAhead];
+        auto fetch = [&](int count) {
+#pragma unroll
+            for (int i = 0; i < kAhead; ++i) {
+                ndt[i] = nx[i] = nz[i] = T(0);
+                if (i < count) {
+                    ndt[i] = pdt.p[lo];
+                    nx[i] = pdy.p[lo];
+                    if (gate) nz[i] = pz.p[lo];
+                    pdt.next();
+                    pdy.next();
+                    if (gate) pz.next();
+                }
+            }
+        };
+        int left = w.end - w.t0;
+        fetch(left);
+        for (; left > 0; left -= kAhead) {
+            float delta[kAhead], wt[kAhead];
+            step_sizes(p, ndt, bias, delta);
+#pragma unroll
+            for (int i = 0; i < kAhead; ++i) wt[i] = to_f32(nx[i]);
+            if (gate) {
+#pragma unroll
+                for (int i = 0; i < kAhead; ++i) {
+                    const float z = to_f32(nz[i]);
+                    wt[i] *= z * sigmoid(z);
+                }
+            }
+            if (left > kAhead) fetch(left - kAhead);
+#pragma unroll
+            for (int i = 0; i < kAhead; ++i) {
+                if (i >= left) break;
+                sum += delta[i];
+#pragma unroll
+                for (int g = 0; g < NG; ++g) {
+                    scalar_loads_done();
+                    Groups next;  // of this step, or of the one before (t0 > 0: it is there)
+                    if (g + 1 == NG) bc -= bc_step;
+                    next.template load<GP>(g + 1 < NG ? bc + (g + 1) * 2 * GP : bc);
+                    __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+                    for (int j = 0; j < GP; ++j) {
+                        float& c = cg[g * GP + j];
+                        c = exp2_fast(delta[i] * a2[g * GP + j]) * __builtin_fmaf(wt[i], cur.v[j], c);
+                    }
+                    cur = next;
+                }
+            }
+        }
+    }
+    const int64_t row = ((int64_t)w.c * p.batch + b) * dim + ch;
+    store_states<NP>(ends + row * NP, NP, cg);
+    sums[row] = sum;
+}
 
 // Keeps the loads from two LDS addresses behind the computation of v: left
 // alone, the compiler loads a whole block's inputs first, into registers that
@@ -69,6 +165,13 @@ __global__ __launch_bounds__(kThreads) void k_ssm_back(libscan_ssm p, BackArgs o
     const int len = WHOLE ? steps : ssm_len(p, k.b);
     const int lim = WHOLE ? CH : k.lim;
     const int blocks = (steps + kT - 1) / kT;
+    // this workgroup's steps; those of its row's tokens
+    const int begin = blockIdx.y * o.chunk;
+    const int stop = begin + o.chunk < steps ? begin + o.chunk : steps;
+    const int end = stop < len ? stop : len;
+    const int64_t crow = (int64_t)blockIdx.y * p.batch + k.b;
+    const int piece = ((int)blockIdx.y + 1) * o.split;  // the first behind this chunk
+    const int64_t behind = (int64_t)((piece < o.pieces ? piece : o.pieces) - 1) * p.batch + k.b;
     const bool gate = p.z != nullptr;
 
     const int row = tid / TPR, lc = (tid % TPR) * VW;
@@ -98,12 +201,16 @@ __global__ __launch_bounds__(kThreads) void k_ssm_back(libscan_ssm p, BackArgs o
     for (int s = 0; s < SPL; ++s) {
         const bool in = WHOLE || (wc < lim && n0 + s < n);
         a2[s] = in ? p.A[(int64_t)(k.c0 + wc) * n + n0 + s] * kLog2e : 0.0f;
-        cg[s] = in && o.dstate_out ? o.dstate_out[sbase + s] : 0.0f;
+        if (o.starts)
+            cg[s] = in ? o.starts[(behind * dim + k.c0 + wc) * o.np + n0 + s] : 0.0f;
+        else
+            cg[s] = in && o.dstate_out ? o.dstate_out[sbase + s] : 0.0f;
         da[s] = 0.0f;
     }
 
     // the steps past the row's tokens
-    for (int t = (len + TS - 1) / TS * TS; !WHOLE && t + row < steps; t += TS) {
+    const int tail = (len + TS - 1) / TS * TS;
+    for (int t = tail > begin ? tail : begin; !WHOLE && t + row < stop; t += TS) {
         Pack<T, VW> zero;
 #pragma unroll
         for (int i = 0; i < VW; ++i) zero.v[i] = T(0);
@@ -138,9 +245,9 @@ __global__ __launch_bounds__(kThreads) void k_ssm_back(libscan_ssm p, BackArgs o
         }
     };
 
-    const int last = (len + TS - 1) / TS * TS - TS;
-    if (last >= 0) fetch(last);
-    for (int t0 = last; t0 >= 0; t0 -= TS) {
+    const int last = begin + (end - begin + TS - 1) / TS * TS - TS;  // < begin: no tokens here
+    if (last >= begin) fetch(last);
+    for (int t0 = last; t0 >= begin; t0 -= TS) {
         const bool live = WHOLE || t0 + row < len;
         const Pack<T, VW> rx = nx, rdt = ndt, rz = nz, rdy = ndy;
         float starts[SUB][SPL];
@@ -173,7 +280,7 @@ __global__ __launch_bounds__(kThreads) void k_ssm_back(libscan_ssm p, BackArgs o
 #pragma unroll
         for (int i = 0; i < VW; ++i)
             s_in[row][lc + i] = float4{delta[i], delta[i] * to_f32(rx.v[i]), w[i], 0.0f};
-        if (t0 > 0) fetch(t0 - TS);
+        if (t0 > begin) fetch(t0 - TS);
         __syncthreads();
 
 #pragma unroll 1
@@ -303,8 +410,8 @@ __global__ __launch_bounds__(kThreads) void k_ssm_back(libscan_ssm p, BackArgs o
 #pragma unroll
     for (int s = 0; s < SPL; ++s)
         if (WHOLE || (wc < lim && n0 + s < n)) {
-            if (o.dstate) o.dstate[sbase + s] = cg[s];
-            o.part_a[sbase + s] = da[s];
+            if (o.dstate && begin == 0) o.dstate[sbase + s] = cg[s];
+            o.part_a[(crow * dim + k.c0 + wc) * n + n0 + s] = da[s];
         }
     // dD and ddt_bias: the TS threads of each channel, in order
     __syncthreads();
@@ -320,8 +427,8 @@ __global__ __launch_bounds__(kThreads) void k_ssm_back(libscan_ssm p, BackArgs o
             d += s_y[r][tid];
             e += s_du[r][tid];
         }
-        o.part_d[(int64_t)k.b * dim + k.c0 + tid] = d;
-        o.part_bias[(int64_t)k.b * dim + k.c0 + tid] = e;
+        o.part_d[crow * dim + k.c0 + tid] = d;
+        o.part_bias[crow * dim + k.c0 + tid] = e;
     }
 }
 
@@ -347,7 +454,7 @@ __global__ __launch_bounds__(kThreads) void k_ssm_sum_bc(libscan_ssm p, const fl
     dC[i] = from_f32<T>(sum.y);
 }
 
-// The rows' sums of dA, dD and ddt_bias, added in order.
+// The sums of dA, dD and ddt_bias over `batch` rows (or their chunks), added in order.
 __global__ __launch_bounds__(kThreads) void k_ssm_sum_rows(int64_t batch, int64_t dim, int64_t n,
                                                            const float* part_a,
                                                            const float* part_d,
@@ -370,41 +477,113 @@ __global__ __launch_bounds__(kThreads) void k_ssm_sum_rows(int64_t batch, int64_
     }
 }
 
-// Lanes to a channel, the same for the sizes and the launch.
-int lanes(const libscan_ssm& p) { return p.n > 32 ? 16 : p.batch * p.dim >= 8192 ? 8 : 16; }
-int blocks_of(const libscan_ssm& p) { return ssm_blocks(p, 256 / lanes(p)); }
+// How a call is cut up, the same for the sizes and the launch.  Eight lanes to a
+// channel do the least work, if there are 8192 channels for them or the rows are
+// cut into chunks: until two workgroups are there for each CU (one with n > 32;
+// so many fit by their registers).  What the chunks hand on is formed by a pass
+// over smaller pieces, four waves of them to a SIMD.
+struct BackPlan {
+    int lanes, nb, chunk, chunks, np, piece, pieces;
+    size_t part_bc, part_a, part_d, bc, ends, sums;  // bytes of scratch
+};
 
 size_t align16(size_t v) { return (v + 15) / 16 * 16; }
 
+BackPlan back_plan(const libscan_ssm& p) {
+    BackPlan r{};
+    const int64_t channels = p.batch * p.dim;
+    r.np = p.n <= 8 ? 8 : p.n <= 16 ? 16 : p.n <= 32 ? 32 : 64;
+    r.lanes = p.n <= 16 ? 8 : 16;
+    r.nb = ssm_blocks(p, 256 / r.lanes);
+    r.chunks = 1;
+    r.chunk = (int)((p.steps + 31) / 32 * 32);
+    const int64_t groups = p.batch * p.groups * r.nb, fit = p.n > 32 ? 256 : 512;
+    int64_t chunks = groups > 0 ? fit / groups : 1;
+    if (chunks > p.steps / 64) chunks = p.steps / 64;
+    // Times in us of a 32-step tile: uncut, and with the CUs full.  1 x 2048 x 4096, n = 16:
+    // 270 uncut (16 lanes); 1 x 8192 x 512: 994 and 217 in chunks.
+    const double uncut = p.n > 32 ? 12.4 : p.n > 16 ? 6.3 : channels < 8192 ? 4.1 : 6.25;
+    const double full = p.n > 32 ? 12.4 : p.n > 16 ? 9.5 : 8.3;
+    const double tiles = (double)p.steps / 32;
+    if (chunks > 1 && p.dim / p.groups >= 48 &&
+        45.0 + 0.25e-6 * r.np * (double)p.steps * (double)channels + tiles / chunks * full <
+            tiles * uncut) {
+        const int64_t waves = p.batch * p.groups * ssm_blocks(p, kWave);
+        int64_t pieces = (4096 + waves - 1) / waves;
+        if (pieces > p.steps / 32) pieces = p.steps / 32;
+        r.piece = (int)(((p.steps + pieces - 1) / pieces + 31) / 32 * 32);
+        const int64_t want = (p.steps + chunks - 1) / chunks;
+        r.chunk = (int)((want + r.piece - 1) / r.piece * r.piece);
+        r.chunks = (int)((p.steps + r.chunk - 1) / r.chunk);
+        r.pieces = (int)((p.steps + r.piece - 1) / r.piece);
+    }
+    if (r.chunks == 1 && r.lanes == 8 && channels < 8192) {
+        r.lanes = 16;
+        r.nb = ssm_blocks(p, 256 / r.lanes);
+    }
+    const size_t rows = (size_t)channels;
+    r.part_bc = align16((size_t)r.nb * p.batch * p.steps * p.groups * p.n * 8);
+    r.part_a = align16(r.chunks * rows * p.n * 4);
+    r.part_d = align16(r.chunks * rows * 4);
+    if (r.chunks > 1) {
+        r.bc = align16(ssm_bc_bytes(p, r.np));
+        r.ends = align16(r.pieces * rows * r.np * 4);
+        r.sums = align16(r.pieces * rows * 4);
+    }
+    return r;
+}
+
 template <class T, int LN, int SPL>
-void back_as(const libscan_ssm& p, const BackArgs& o, int nb, hipStream_t stream) {
-    const int64_t grid = p.batch * p.groups * nb;
+void back_as(const libscan_ssm& p, const BackArgs& o, const BackPlan& l, hipStream_t stream) {
+    const int64_t grid = p.batch * p.groups * l.nb;
     if (grid == 0) return;
     const bool whole = !p.lengths && p.steps % 32 == 0 && p.n == LN * SPL &&
                        p.dim / p.groups % SsmLanes<LN, SPL>::CH == 0;
     auto* back = whole ? k_ssm_back<T, LN, SPL, true> : k_ssm_back<T, LN, SPL, false>;
-    back<<<dim3((unsigned)grid), kThreads, 0, stream>>>(p, o, nb);
+    back<<<dim3((unsigned)grid, l.chunks), kThreads, 0, stream>>>(p, o, l.nb);
 }
 
 template <class T>
-hipError_t back_type(const libscan_ssm& p, const BackArgs& o, float* dA, T* dB, T* dC, float* dD,
-                     float* ddt_bias, hipStream_t stream) {
-    const int nb = blocks_of(p);
-    const bool eight = lanes(p) == 8;
+void ends_of(const libscan_ssm& p, const BackArgs& o, const BackPlan& l, const float* bc,
+             float* ends, float* sums, hipStream_t stream) {
+    const int nb = ssm_blocks(p, kWave);
+    const unsigned waves = (unsigned)(p.batch * p.groups * nb);
+    auto* k = l.np == 8    ? k_ssm_back_ends<T, 8>
+              : l.np == 16 ? k_ssm_back_ends<T, 16>
+              : l.np == 32 ? k_ssm_back_ends<T, 32>
+                           : k_ssm_back_ends<T, 64>;
+    k<<<dim3((waves + kLaneWaves - 1) / kLaneWaves, l.pieces - 1), kWave * kLaneWaves, 0, stream>>>(
+        p, o.dy, o.dy_batch, o.dy_step, bc, ends, sums, nb, l.piece, waves);
+}
+
+template <class T>
+hipError_t back_type(const libscan_ssm& p, BackArgs o, const BackPlan& l, char* more, float* dA,
+                     T* dB, T* dC, float* dD, float* ddt_bias, hipStream_t stream) {
+    if (l.chunks > 1) {
+        float* bc = (float*)more;
+        float* ends = (float*)(more + l.bc);
+        float* sums = (float*)(more + l.bc + l.ends);
+        launch_ssm_bc(p, l.np, bc, stream);
+        ends_of<T>(p, o, l, bc, ends, sums, stream);
+        launch_ssm_starts(p, l.np, o.dstate_out, ends, sums, l.pieces, true, stream);
+        o.starts = ends;
+        o.split = l.chunk / l.piece;
+        o.pieces = l.pieces;
+    }
     if (p.n > 32)
-        back_as<T, 16, 4>(p, o, nb, stream);
+        back_as<T, 16, 4>(p, o, l, stream);
     else if (p.n > 16)
-        eight ? back_as<T, 8, 4>(p, o, nb, stream) : back_as<T, 16, 2>(p, o, nb, stream);
+        back_as<T, 16, 2>(p, o, l, stream);
     else
-        eight ? back_as<T, 8, 2>(p, o, nb, stream) : back_as<T, 16, 1>(p, o, nb, stream);
+        l.lanes == 8 ? back_as<T, 8, 2>(p, o, l, stream) : back_as<T, 16, 1>(p, o, l, stream);
     const int64_t bc = p.batch * p.steps * p.groups * p.n;
     if (bc > 0)
         k_ssm_sum_bc<T><<<dim3((unsigned)((bc + kThreads - 1) / kThreads)), kThreads, 0, stream>>>(
-            p, o.part_bc, nb, dB, dC);
+            p, o.part_bc, l.nb, dB, dC);
     const int64_t rows = p.dim * p.n;
     if (rows > 0)
         k_ssm_sum_rows<<<dim3((unsigned)((rows + kThreads - 1) / kThreads)), kThreads, 0, stream>>>(
-            p.batch, p.dim, p.n, o.part_a, o.part_d, o.part_bias, dA, dD, ddt_bias);
+            p.batch * l.chunks, p.dim, p.n, o.part_a, o.part_d, o.part_bias, dA, dD, ddt_bias);
     return hipGetLastError();
 }
 
@@ -415,33 +594,45 @@ size_t ssm_ckpt_bytes(const libscan_ssm& p) {
 }
 
 size_t ssm_back_scratch_bytes(const libscan_ssm& p) {
-    const size_t nb = blocks_of(p);
-    return align16(nb * p.batch * p.steps * p.groups * p.n * 8) +
-           align16((size_t)p.batch * p.dim * p.n * 4) + 2 * align16((size_t)p.batch * p.dim * 4);
+    const BackPlan l = back_plan(p);
+    return l.part_bc + l.part_a + 2 * l.part_d + l.bc + l.ends + l.sums;
 }
 
 hipError_t launch_ssm_back(const libscan_ssm& p, const void* dy, int64_t dy_batch, int64_t dy_step,
                            const float* ckpt, const float* dstate_out, void* dx, void* ddt,
                            float* dA, void* dB, void* dC, float* dD, void* dz, float* ddt_bias,
                            float* dstate, void* scratch, hipStream_t stream) {
-    const size_t nb = blocks_of(p);
+    const BackPlan l = back_plan(p);
     char* s = (char*)scratch;
-    BackArgs o{dy, dy_batch, dy_step, ckpt, dstate_out, dx, ddt, dz, dstate,
-               nullptr, nullptr, nullptr, nullptr};
+    BackArgs o{};
+    o.dy = dy;
+    o.dy_batch = dy_batch;
+    o.dy_step = dy_step;
+    o.ckpt = ckpt;
+    o.dstate_out = dstate_out;
+    o.dx = dx;
+    o.ddt = ddt;
+    o.dz = dz;
+    o.dstate = dstate;
     o.part_bc = (float2*)s;
-    s += align16(nb * p.batch * p.steps * p.groups * p.n * 8);
+    s += l.part_bc;
     o.part_a = (float*)s;
-    s += align16((size_t)p.batch * p.dim * p.n * 4);
+    s += l.part_a;
     o.part_d = (float*)s;
-    s += align16((size_t)p.batch * p.dim * 4);
+    s += l.part_d;
     o.part_bias = (float*)s;
+    s += l.part_d;
+    o.chunk = l.chunk;
+    o.np = l.np;
     switch (p.type) {
         case LIBSCAN_F16:
-            return back_type<_Float16>(p, o, dA, (_Float16*)dB, (_Float16*)dC, dD, ddt_bias, stream);
+            return back_type<_Float16>(p, o, l, s, dA, (_Float16*)dB, (_Float16*)dC, dD, ddt_bias,
+                                       stream);
         case LIBSCAN_BF16:
-            return back_type<__bf16>(p, o, dA, (__bf16*)dB, (__bf16*)dC, dD, ddt_bias, stream);
+            return back_type<__bf16>(p, o, l, s, dA, (__bf16*)dB, (__bf16*)dC, dD, ddt_bias,
+                                     stream);
         default:
-            return back_type<float>(p, o, dA, (float*)dB, (float*)dC, dD, ddt_bias, stream);
+            return back_type<float>(p, o, l, s, dA, (float*)dB, (float*)dC, dD, ddt_bias, stream);
     }
 }
 

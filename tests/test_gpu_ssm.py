@@ -162,6 +162,28 @@ def test_scan_long_ragged_rows(n, groups, kind):
     assert torch.equal(ops.selective_scan(**d)[0], y)
 
 
+@pytest.mark.parametrize("n,groups", [(5, 1), (16, 2), (20, 1), (64, 1)])
+def test_scan_rows_in_chunks(n, groups):
+    """Few channels and many steps: the rows are cut into chunks, forward and
+    backward.  Lengths that end chunks early, leave some empty, or are 0; the
+    same without lengths, with a first state and a gradient of the last one."""
+    steps, dim = 1537, 100
+    lengths = [1537, 0, 700, 33]
+    for case in (lengths, None):
+        rows = 4 if case else 1
+        a, dy = inputs(rows, steps, dim, n, groups, kind=F32, state=True, lengths=case)
+        d = dev(a)
+        p = ops._args.ssm(*(d[k] for k in ("x", "dt", "A", "B", "C", "D", "z", "dt_bias", "state",
+                                           "lengths")), True, False)
+        assert ops._sizes("selective_scan_bytes", p, 3)[1] > 0     # it is the chunks that run
+        for b, count in enumerate(case or []):
+            for k in ("x", "dt", "z", "B", "C"):
+                a[k][b, count:] = float("nan")
+            dy[b, count:] = float("nan")
+        check_forward(a)
+        check_backward(a, dy, dstate_out=torch.randn(rows, dim, n))
+
+
 def test_scan_wide_layout():
     """Enough channels for a quad of lanes per channel, in both directions."""
     a, dy = inputs(2, 35, 8200, 16, groups=2, kind=BF16, state=True)
