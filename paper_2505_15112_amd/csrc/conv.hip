@@ -324,15 +324,16 @@ __global__ __launch_bounds__(kThreads) void k_conv_back(libscan_conv p, BackArgs
 }
 
 // dweight and dbias: the workgroups' sums, added in order.
-__global__ __launch_bounds__(kThreads) void k_conv_sum(const float* part, int64_t parts, int64_t dim,
-                                                       int width, float* dweight, float* dbias) {
-    const int64_t i = (int64_t)blockIdx.x * kThreads + threadIdx.x;
-    if (i >= dim * (width + 1)) return;
+template <int SLICES>
+__global__ __launch_bounds__(kSumThreads) void k_conv_sum(const float* part, int64_t parts,
+                                                          int64_t dim, int width, float* dweight,
+                                                          float* dbias) {
+    const int64_t i = (int64_t)blockIdx.x * kSumOuts<SLICES> + threadIdx.x % kSumOuts<SLICES>;
+    const int64_t total = dim * (width + 1);
+    const float sum = sum_parts<SLICES>(part, i < total ? parts : 0, total, i);
+    if (threadIdx.x >= kSumOuts<SLICES> || i >= total) return;
     const int j = (int)(i / dim);
     const int64_t c = i % dim;
-    float sum = 0.0f;
-#pragma unroll 8
-    for (int64_t k = 0; k < parts; ++k) sum += part[k * (width + 1) * dim + i];
     if (j < width)
         dweight[c * width + j] = sum;
     else if (dbias)
@@ -371,8 +372,13 @@ hipError_t back_as(const libscan_conv& p, const BackArgs& o, float* dweight, flo
     const int64_t nc = (p.dim + kBackSide * kBackV - 1) / (kBackSide * kBackV);
     auto* back = p.silu ? k_conv_back<T, W, true> : k_conv_back<T, W, false>;
     if (parts > 0) back<<<(unsigned)(parts * nc), kThreads, 0, s>>>(p, o);
-    k_conv_sum<<<groups_of(p.dim * (W + 1), kThreads), kThreads, 0, s>>>(o.part, parts, p.dim, W,
-                                                                       dweight, dbias);
+    const int64_t outs = p.dim * (W + 1);
+    if (long_sum(parts))
+        k_conv_sum<8><<<groups_of(outs, kSumOuts<8>), kSumThreads, 0, s>>>(o.part, parts, p.dim, W,
+                                                                         dweight, dbias);
+    else
+        k_conv_sum<1><<<groups_of(outs, kSumOuts<1>), kSumThreads, 0, s>>>(o.part, parts, p.dim, W,
+                                                                         dweight, dbias);
     return hipGetLastError();
 }
 

@@ -121,4 +121,41 @@ __device__ __forceinline__ void share_sums(float (&v)[N], int lane) {
     if constexpr (sizeof...(REST) > 0) share_sums<K / 2, REST...>(v, lane);
 }
 
+// ------------------------------------------------ sums over partial results
+
+// A workgroup of kSumThreads adds sums of `count` parts, part[k * stride + i] over k:
+// each by SLICES threads, which take every SLICES-th part, joined in order.  The sum
+// is returned to the threads of the first slice; all threads of the workgroup
+// call.  Eight slices for long sums (of 306 parts: 38 us by one thread, 8 by eight),
+// one for short ones, which would leave the others idle.
+constexpr int kSumThreads = 256;
+template <int SLICES>
+constexpr int kSumOuts = kSumThreads / SLICES;
+inline bool long_sum(int64_t count) { return count > 16; }
+
+__device__ __forceinline__ float2 add_values(float2 a, float2 b) {
+    return float2{a.x + b.x, a.y + b.y};
+}
+__device__ __forceinline__ float add_values(float a, float b) { return a + b; }
+
+template <int SLICES, class V>
+__device__ __forceinline__ V sum_parts(const V* part, int64_t count, int64_t stride, int64_t i) {
+    constexpr int OUTS = kSumOuts<SLICES>;
+    const int out = threadIdx.x % OUTS, slice = threadIdx.x / OUTS;
+    V sum{};
+#pragma unroll 8
+    for (int64_t k = slice; k < count; k += SLICES) sum = add_values(sum, part[k * stride + i]);
+    if constexpr (SLICES > 1) {
+        __shared__ V s_part[SLICES][OUTS];
+        s_part[slice][out] = sum;
+        __syncthreads();
+        if (slice == 0) {
+#pragma unroll
+            for (int j = 1; j < SLICES; ++j) sum = add_values(sum, s_part[j][out]);
+        }
+        __syncthreads();  // before a next call writes there
+    }
+    return sum;
+}
+
 }  // namespace ls

@@ -308,8 +308,11 @@ int64_t segments(const libscan_logits& p) {
     return (p.vocab + C::kSeg - 1) / C::kSeg;
 }
 
-// Small segments where the large ones would leave CUs without work.
-bool small(const libscan_logits& p) { return p.rows * segments<Large>(p) < 256; }
+// Small segments where the large ones would leave CUs without work; for
+// probabilities only if the row takes two kernels anyway.
+bool small(const libscan_logits& p, bool probs) {
+    return p.rows * segments<Large>(p) < 256 && !(probs && p.vocab <= Large::kSeg);
+}
 
 template <class T, class C, bool NAMED>
 hipError_t process_as(const libscan_logits& p, void* out, int64_t out_row, hipStream_t s) {
@@ -339,11 +342,11 @@ hipError_t probs_as(const libscan_logits& p, float* probs, void* scratch, hipStr
 
 // f(element, cut, named) for the call's kernels
 template <class F>
-hipError_t by_kind(const libscan_logits& p, F f) {
+hipError_t by_kind(const libscan_logits& p, bool probs, F f) {
     auto named = [&](auto t, auto cut) {
         return p.history || p.biases ? f(t, cut, std::true_type()) : f(t, cut, std::false_type());
     };
-    auto cut = [&](auto t) { return small(p) ? named(t, Small()) : named(t, Large()); };
+    auto cut = [&](auto t) { return small(p, probs) ? named(t, Small()) : named(t, Large()); };
     switch (p.type) {
         case LIBSCAN_F16: return cut(_Float16());
         case LIBSCAN_BF16: return cut(__bf16());
@@ -358,16 +361,16 @@ bool logits_fit(const libscan_logits& p) {
 }
 
 size_t logits_scratch(const libscan_logits& p) {
-    const int64_t segs = small(p) ? segments<Small>(p) : segments<Large>(p);
+    const int64_t segs = small(p, true) ? segments<Small>(p) : segments<Large>(p);
     if (segs == 1) return 0;
-    const int64_t bits = !p.history && !p.biases ? 0 : small(p) ? Small::kSeg / 8 : Large::kSeg / 8;
+    const int64_t bits = !p.history && !p.biases ? 0 : small(p, true) ? Small::kSeg / 8 : Large::kSeg / 8;
     return (size_t)p.rows * segs * (8 + bits);
 }
 
 hipError_t launch_logits_process(const libscan_logits& p, void* out, int64_t out_row,
                                  hipStream_t stream) {
     if (p.rows == 0 || p.vocab == 0) return hipSuccess;
-    return by_kind(p, [&](auto t, auto cut, auto named) {
+    return by_kind(p, false, [&](auto t, auto cut, auto named) {
         return process_as<decltype(t), decltype(cut), decltype(named)::value>(p, out, out_row,
                                                                               stream);
     });
@@ -376,7 +379,7 @@ hipError_t launch_logits_process(const libscan_logits& p, void* out, int64_t out
 hipError_t launch_logits_probs(const libscan_logits& p, float* probs, void* scratch,
                                hipStream_t stream) {
     if (p.rows == 0 || p.vocab == 0) return hipSuccess;
-    return by_kind(p, [&](auto t, auto cut, auto named) {
+    return by_kind(p, true, [&](auto t, auto cut, auto named) {
         return probs_as<decltype(t), decltype(cut), decltype(named)::value>(p, probs, scratch,
                                                                             stream);
     });

@@ -495,8 +495,9 @@ struct LanePlan {
 // and 51.8, 1 x 2048 x 1024 96 and 44, 1 x 8192 x 512 373 and 66, 2 x 2048 x 4096 118
 // and 124 us.
 bool chunks_pay(const libscan_ssm& p, int np) {
-    const int64_t channels = p.batch * p.dim;
-    const double over = channels > 4096 ? (double)(channels - 4096) : 0.0;
+    // (lanes without a channel take their time all the same)
+    const int64_t channels = p.batch * p.groups * ssm_blocks(p, kWave) * kWave;
+    const double over = p.batch * p.dim > 4096 ? (double)(p.batch * p.dim - 4096) : 0.0;
     const double step = 0.031 + 0.00103 * (np < 16 ? 16 : np);
     const double tiles = (double)p.steps * step * (1.0 + 6.6e-5 * over);
     const double chunks = 14.0 + 0.9 * np + 0.36e-6 * np * (double)p.steps * (double)channels;
@@ -507,8 +508,7 @@ LanePlan lane_plan(const libscan_ssm& p) {
     LanePlan r{0, 0, 0, 0, 0, 0, 0};
     if (p.batch == 0 || p.dim == 0) return r;
     r.np = p.n <= 8 ? 8 : p.n <= 16 ? 16 : p.n <= 32 ? 32 : 64;
-    // (a wave of few channels of a group would leave most lanes without work)
-    if (p.steps < 64 || p.dim / p.groups < 48 || !chunks_pay(p, r.np)) {
+    if (p.steps < 64 || !chunks_pay(p, r.np)) {
         r.np = 0;
         return r;
     }

@@ -433,45 +433,36 @@ __global__ __launch_bounds__(kThreads) void k_ssm_back(libscan_ssm p, BackArgs o
 }
 
 // dB and dC: the workgroups' sums of a group, added in order.
-template <class T>
-__global__ __launch_bounds__(kThreads) void k_ssm_sum_bc(libscan_ssm p, const float2* part, int nb,
-                                                         T* dB, T* dC) {
+template <class T, int SLICES>
+__global__ __launch_bounds__(kSumThreads) void k_ssm_sum_bc(libscan_ssm p, const float2* part,
+                                                            int nb, T* dB, T* dC) {
     const int64_t per_step = p.groups * p.n, total = p.batch * p.steps * per_step;
-    const int64_t i = (int64_t)blockIdx.x * kThreads + threadIdx.x;
-    if (i >= total) return;
-    const int64_t bt = i / per_step;
+    const int64_t i = (int64_t)blockIdx.x * kSumOuts<SLICES> + threadIdx.x % kSumOuts<SLICES>;
+    const int64_t bt = i < total ? i / per_step : 0;
     const int b = (int)(bt / p.steps), t = (int)(bt % p.steps);
-    float2 sum{0.0f, 0.0f};
-    if (t < ssm_len(p, b)) {
-#pragma unroll 8
-        for (int k = 0; k < nb; ++k) {
-            const float2 v = part[k * total + i];
-            sum.x += v.x;
-            sum.y += v.y;
-        }
+    const bool live = i < total && t < ssm_len(p, b);
+    const float2 sum = sum_parts<SLICES>(part, live ? nb : 0, total, i);
+    if (threadIdx.x < kSumOuts<SLICES> && i < total) {
+        dB[i] = from_f32<T>(sum.x);
+        dC[i] = from_f32<T>(sum.y);
     }
-    dB[i] = from_f32<T>(sum.x);
-    dC[i] = from_f32<T>(sum.y);
 }
 
-// The sums of dA, dD and ddt_bias over `batch` rows (or their chunks), added in order.
-__global__ __launch_bounds__(kThreads) void k_ssm_sum_rows(int64_t batch, int64_t dim, int64_t n,
-                                                           const float* part_a,
-                                                           const float* part_d,
-                                                           const float* part_bias, float* dA,
-                                                           float* dD, float* ddt_bias) {
-    const int64_t i = (int64_t)blockIdx.x * kThreads + threadIdx.x;
-    if (i < dim * n) {
-        float sum = 0.0f;
-        for (int64_t b = 0; b < batch; ++b) sum += part_a[b * dim * n + i];
-        dA[i] = sum;
-    }
-    if (i < dim) {
-        float d = 0.0f, e = 0.0f;
-        for (int64_t b = 0; b < batch; ++b) {
-            d += part_d[b * dim + i];
-            e += part_bias[b * dim + i];
-        }
+// The sums of dA, dD and ddt_bias over `rows` rows (or their chunks), added in order.
+template <int SLICES>
+__global__ __launch_bounds__(kSumThreads) void k_ssm_sum_rows(int64_t rows, int64_t dim, int64_t n,
+                                                              const float* part_a,
+                                                              const float* part_d,
+                                                              const float* part_bias, float* dA,
+                                                              float* dD, float* ddt_bias) {
+    const int64_t i = (int64_t)blockIdx.x * kSumOuts<SLICES> + threadIdx.x % kSumOuts<SLICES>;
+    const bool first = threadIdx.x < kSumOuts<SLICES>;
+    const float a = sum_parts<SLICES>(part_a, i < dim * n ? rows : 0, dim * n, i);
+    if (first && i < dim * n) dA[i] = a;
+    if ((int64_t)blockIdx.x * kSumOuts<SLICES> >= dim) return;  // the whole workgroup
+    const float d = sum_parts<SLICES>(part_d, i < dim ? rows : 0, dim, i);
+    const float e = sum_parts<SLICES>(part_bias, i < dim ? rows : 0, dim, i);
+    if (first && i < dim) {
         if (dD) dD[i] = d;
         if (ddt_bias) ddt_bias[i] = e;
     }
@@ -505,10 +496,10 @@ BackPlan back_plan(const libscan_ssm& p) {
     const double uncut = p.n > 32 ? 12.4 : p.n > 16 ? 6.3 : channels < 8192 ? 4.1 : 6.25;
     const double full = p.n > 32 ? 12.4 : p.n > 16 ? 9.5 : 8.3;
     const double tiles = (double)p.steps / 32;
-    if (chunks > 1 && p.dim / p.groups >= 48 &&
-        45.0 + 0.25e-6 * r.np * (double)p.steps * (double)channels + tiles / chunks * full <
+    const int64_t waves = p.batch * p.groups * ssm_blocks(p, kWave);
+    if (chunks > 1 &&
+        45.0 + 0.25e-6 * r.np * (double)p.steps * (double)(waves * kWave) + tiles / chunks * full <
             tiles * uncut) {
-        const int64_t waves = p.batch * p.groups * ssm_blocks(p, kWave);
         int64_t pieces = (4096 + waves - 1) / waves;
         if (pieces > p.steps / 32) pieces = p.steps / 32;
         r.piece = (int)(((p.steps + pieces - 1) / pieces + 31) / 32 * 32);
@@ -577,13 +568,20 @@ hipError_t back_type(const libscan_ssm& p, BackArgs o, const BackPlan& l, char* 
     else
         l.lanes == 8 ? back_as<T, 8, 2>(p, o, l, stream) : back_as<T, 16, 1>(p, o, l, stream);
     const int64_t bc = p.batch * p.steps * p.groups * p.n;
-    if (bc > 0)
-        k_ssm_sum_bc<T><<<dim3((unsigned)((bc + kThreads - 1) / kThreads)), kThreads, 0, stream>>>(
-            p, o.part_bc, l.nb, dB, dC);
-    const int64_t rows = p.dim * p.n;
-    if (rows > 0)
-        k_ssm_sum_rows<<<dim3((unsigned)((rows + kThreads - 1) / kThreads)), kThreads, 0, stream>>>(
-            p.batch * l.chunks, p.dim, p.n, o.part_a, o.part_d, o.part_bias, dA, dD, ddt_bias);
+    auto grid = [](int64_t outs, int per) { return dim3((unsigned)((outs + per - 1) / per)); };
+    if (bc > 0 && long_sum(l.nb))
+        k_ssm_sum_bc<T, 8><<<grid(bc, kSumOuts<8>), kSumThreads, 0, stream>>>(p, o.part_bc, l.nb,
+                                                                              dB, dC);
+    else if (bc > 0)
+        k_ssm_sum_bc<T, 1><<<grid(bc, kSumOuts<1>), kSumThreads, 0, stream>>>(p, o.part_bc, l.nb,
+                                                                              dB, dC);
+    const int64_t outs = p.dim * p.n, rows = p.batch * l.chunks;
+    if (outs > 0 && long_sum(rows))
+        k_ssm_sum_rows<8><<<grid(outs, kSumOuts<8>), kSumThreads, 0, stream>>>(
+            rows, p.dim, p.n, o.part_a, o.part_d, o.part_bias, dA, dD, ddt_bias);
+    else if (outs > 0)
+        k_ssm_sum_rows<1><<<grid(outs, kSumOuts<1>), kSumThreads, 0, stream>>>(
+            rows, p.dim, p.n, o.part_a, o.part_d, o.part_bias, dA, dD, ddt_bias);
     return hipGetLastError();
 }
 

@@ -254,6 +254,14 @@ PyObject* empty(PyObject* const* a) {
     return THPVariable_Wrap(at::empty(like.sizes(), like.options().dtype(type)));
 }
 
+// (count, like): a new fp32 vector on like's GPU
+PyObject* floats(PyObject* const* a) {
+    const int64_t n = PyLong_AsLongLong(a[0]);
+    if (PyErr_Occurred()) throw Raised();
+    return THPVariable_Wrap(
+        at::empty({n}, THPVariable_Unpack(a[1]).options().dtype(at::kFloat)));
+}
+
 // (address of a size query of libscan.h, struct bytes, sizes): its status, then
 // the sizes
 PyObject* sizes(PyObject* const* a) {
@@ -301,7 +309,7 @@ PyObject* entry(PyObject*, PyObject* const* args, Py_ssize_t n) {
 #define ENTRY(f, n) {#f, (PyCFunction)(void (*)(void))entry<f, n>, METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {ENTRY(conv, 7),  ENTRY(ssm, 12),  ENTRY(logits, 11),
                          ENTRY(dense, 5), ENTRY(empty, 2), ENTRY(sizes, 3),
-                         ENTRY(memory, 2), {nullptr, nullptr, 0, nullptr}};
+                         ENTRY(memory, 2), ENTRY(floats, 2), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_torch_args", nullptr, -1, methods,
                       nullptr, nullptr, nullptr, nullptr};
 

@@ -460,7 +460,7 @@ class _Args:
         module = importlib.util.module_from_spec(spec)
         spec.loader.exec_module(module)
         self.__dict__.update({k: getattr(module, k)
-                              for k in ("conv", "ssm", "logits", "dense", "empty", "sizes", "memory")})
+                              for k in ("conv", "ssm", "logits", "dense", "empty", "sizes", "memory", "floats")})
         return self.__dict__[name]
 
 
@@ -511,11 +511,11 @@ def causal_conv_backward(dy, x, weight, bias=None, state=None, lengths=None, sil
     pdy = _strided(dy, "dy", x)
     pso = _args.dense(dstate_out, "dstate_out", x, (batch, width - 1, dim), False)
     dx = _args.empty(x, False)
-    dweight = torch.empty((dim, width), dtype=torch.float32, device=x.device)
-    dbias = dweight.new_empty(dim) if bias is not None else None
+    dweight = _args.empty(weight, True)
+    dbias = _args.empty(bias, True) if bias is not None else None
     if with_dstate is None:
         with_dstate = state is not None
-    dstate = x.new_empty((batch, width - 1, dim)) if with_dstate else None
+    dstate = _into(None, x, (batch, width - 1, dim)) if with_dstate else None
     need = _sizes("causal_conv_scratch_bytes", p, 1)[0]
     buf = _scratch_for(scratch_buf, need, x)
     _launch("causal_conv_backward", x, p, pdy, dy.stride(0), dy.stride(1), pso, _ptr(dx),
@@ -590,8 +590,7 @@ def selective_scan(x, dt, A, B, C, D=None, z=None, dt_bias=None, state=None, len
     if with_state or state_out is not None:
         state_out = _into(state_out, x, (batch, dim, A.shape[1]), True, "state_out")
     kept, need, _ = _sizes("selective_scan_bytes", p, 3)
-    ckpt = torch.empty(kept // 4, dtype=torch.float32, device=x.device) if with_checkpoints \
-        else None
+    ckpt = _args.floats(kept // 4, x) if with_checkpoints else None
     buf = _scratch_for(scratch_buf, need, x) if need else None
     _launch("selective_scan", x, p, _ptr(y), _ptr(state_out), _ptr(ckpt), _ptr(buf),
             buf.numel() if buf is not None else 0)
@@ -615,16 +614,12 @@ def selective_scan_backward(dy, checkpoints, x, dt, A, B, C, D=None, z=None, dt_
     if with_dstate is None:
         with_dstate = state is not None
 
-    def new(shape, dtype):
-        return torch.empty(shape, dtype=dtype, device=x.device)
-
-    f32 = torch.float32
-    dx, ddt = new(x.shape, x.dtype), new(x.shape, x.dtype)
-    dA, dB, dC = new(A.shape, f32), new(B.shape, x.dtype), new(B.shape, x.dtype)
-    dD = new(dim, f32) if D is not None else None
-    dz = new(x.shape, x.dtype) if z is not None else None
-    dbias = new(dim, f32) if dt_bias is not None else None
-    dstate = new((batch, dim, A.shape[1]), f32) if with_dstate else None
+    new = _args.empty
+    dx, ddt, dA, dB, dC = new(x, False), new(x, False), new(A, True), new(B, False), new(B, False)
+    dD = new(D, True) if D is not None else None
+    dz = new(x, False) if z is not None else None
+    dbias = new(dt_bias, True) if dt_bias is not None else None
+    dstate = _into(None, x, (batch, dim, A.shape[1]), True) if with_dstate else None
     buf = _scratch_for(scratch_buf, need, x)
     _launch("selective_scan_backward", x, p, pdy, dy.stride(0), dy.stride(1), pk, pso, _ptr(dx), _ptr(ddt), _ptr(dA), _ptr(dB), _ptr(dC), _ptr(dD), _ptr(dz),
             _ptr(dbias), _ptr(dstate), _ptr(buf), buf.numel())
