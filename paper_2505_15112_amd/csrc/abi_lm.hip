@@ -76,9 +76,10 @@ int check_conv(const libscan_conv* p) {
     if (p->width < 2 || p->width > 4) return LIBSCAN_EINVAL;
     const int r = check_sizes(p->batch, p->steps, p->dim);
     if (r != LIBSCAN_OK) return r;
-    // forward blocks own 16 steps of at least 1024 channels or many rows
-    if ((__int128)p->batch * (p->steps / 16 + 1) * (p->dim / 4 + 1) / 256 >= kMaxBlocks ||
-        (__int128)p->batch * (p->steps / 256 + 1) * (p->dim / 128 + 1) >= kMaxBlocks)
+    // forward threads own 8 steps of at least two channels, backward workgroups at
+    // least 224 steps of 128
+    if ((__int128)p->batch * (p->steps / 8 + 1) * (p->dim / 2 + 1) / 256 >= kMaxBlocks ||
+        (__int128)p->batch * (p->steps / 224 + 1) * (p->dim / 128 + 1) >= kMaxBlocks)
         return LIBSCAN_ERANGE;
     return LIBSCAN_OK;
 }
@@ -92,8 +93,12 @@ int check_ssm(const libscan_ssm* p) {
     const int r = check_sizes(p->batch, p->steps, p->dim);
     if (r != LIBSCAN_OK) return r;
     if (p->dim % p->groups) return LIBSCAN_EINVAL;
+    // workgroups of at least 16 channels, of 32 sums of dB, dC or dA, of 256 states
+    const int64_t np = p->n <= 8 ? 8 : p->n <= 16 ? 16 : p->n <= 32 ? 32 : 64;
     if ((__int128)p->batch * p->groups * (p->dim / p->groups / 16 + 1) >= kMaxBlocks ||
-        (__int128)p->batch * p->steps * p->groups * p->n / 256 >= kMaxBlocks)
+        (__int128)p->batch * p->steps * p->groups * np / 32 >= kMaxBlocks ||
+        (__int128)p->dim * np / 32 >= kMaxBlocks ||
+        (__int128)p->batch * p->dim * np / 256 >= kMaxBlocks)
         return LIBSCAN_ERANGE;
     return LIBSCAN_OK;
 }
