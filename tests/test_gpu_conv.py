@@ -70,6 +70,14 @@ def test_conv_and_gradients(size, width, kind, wkind):
     check(x, w, bias, state, dy)
 
 
+@pytest.mark.parametrize("kind,wkind", [(F32, F32), (BF16, F32), (BF16, BF16)])
+def test_conv_gradients_over_many_rows(kind, wkind):
+    """Sums over many workgroups, whole ones and others."""
+    for size in ((9, 500, 40), (24, 248, 128)):
+        x, w, bias, state, dy = inputs(*size, 4, kind, wkind)
+        check(x, w, bias, state, dy)
+
+
 @pytest.mark.parametrize("silu", [True, False])
 @pytest.mark.parametrize("bias", [True, False])
 def test_conv_without_parts(silu, bias):

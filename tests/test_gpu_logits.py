@@ -93,6 +93,16 @@ def test_many_rows():
     check(inputs(700, 300, F16, hist=20, biases=3, grammar=True))
 
 
+@pytest.mark.parametrize("rows,vocab", [(40, 60000), (129, 16387), (300, 8193)])
+@pytest.mark.parametrize("named", [True, False])
+@pytest.mark.parametrize("kind", [F32, F16, BF16])
+def test_many_long_rows(rows, vocab, named, kind):
+    """Rows of several segments, enough of them for the wide workgroups."""
+    a = (inputs(rows, vocab, kind, hist=60, biases=9, grammar=True) if named
+         else inputs(rows, vocab, kind))
+    check(a, torch.linspace(0.3, 1.5, rows))
+
+
 def test_rows_that_the_mask_leaves_empty():
     a = inputs(4, 20000, F32, grammar=True)
     a["allowed"][1] = 0

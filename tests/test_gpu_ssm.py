@@ -443,3 +443,17 @@ def test_refusals():
     with pytest.raises(ValueError):             # fewer states than rows
         ops.selective_scan_step(d["x"][:, 0], d["dt"][:, 0], d["state"][:1], d["A"], d["B"][:, 0],
                                 d["C"][:, 0])
+
+
+@pytest.mark.parametrize("size", [(2, 32, 32, 16, 1), (3, 64, 64, 16, 2), (1, 32, 32, 32, 1),
+                                  (2, 64, 64, 32, 2), (1, 32, 32, 64, 1), (2, 32, 64, 64, 2),
+                                  (4, 32, 4096, 16, 2), (1, 1024, 64, 16, 1), (1, 768, 64, 32, 2),
+                                  (1, 512, 32, 64, 1)])
+@pytest.mark.parametrize("kind", [F32, F16, BF16])
+def test_scan_whole_tiles(size, kind):
+    """Steps, channels and states that leave no tile in part filled."""
+    for state in (False, True):
+        a, dy = inputs(*size, kind=kind, state=state)
+        check_forward(a)
+    check_backward(a, dy, dstate_out=torch.randn(size[0], size[2], size[3],
+                                                 generator=torch.Generator().manual_seed(4)))
