@@ -469,14 +469,18 @@ __global__ __launch_bounds__(kSumThreads) void k_ssm_sum_rows(int64_t rows, int6
 }
 
 // How a call is cut up, the same for the sizes and the launch.  Eight lanes to a
-// channel do the least work, if there are 8192 channels for them or the rows are
+// channel do the least work, if there are 16384 channels for them or the rows are
 // cut into chunks: until two workgroups are there for each CU (one with n > 32;
-// so many fit by their registers).  What the chunks hand on is formed by a pass
-// over smaller pieces, four waves of them to a SIMD.
+// so many fit by their registers).  Uncut rows of 2048 steps, n = 16, with eight
+// lanes and with sixteen: 8192 channels 391 and 350 us, 12288 525 and 458, 16384
+// 539 and 654.  What the chunks hand on is formed by a pass over smaller pieces,
+// four waves of them to a SIMD.
 struct BackPlan {
     int lanes, nb, chunk, chunks, np, piece, pieces;
     size_t part_bc, part_a, part_d, bc, ends, sums;  // bytes of scratch
 };
+
+constexpr int64_t kWideLanes = 16384;
 
 size_t align16(size_t v) { return (v + 15) / 16 * 16; }
 
@@ -491,9 +495,11 @@ BackPlan back_plan(const libscan_ssm& p) {
     const int64_t groups = p.batch * p.groups * r.nb, fit = p.n > 32 ? 256 : 512;
     int64_t chunks = groups > 0 ? fit / groups : 1;
     if (chunks > p.steps / 64) chunks = p.steps / 64;
-    // Times in us of a 32-step tile: uncut, and with the CUs full.  1 x 2048 x 4096, n = 16:
-    // 270 uncut (16 lanes); 1 x 8192 x 512: 994 and 217 in chunks.
-    const double uncut = p.n > 32 ? 12.4 : p.n > 16 ? 6.3 : channels < 8192 ? 4.1 : 6.25;
+    // Times in us of a 32-step tile: uncut, and with the CUs full.  n = 16, uncut and in
+    // chunks: 1 x 2048 x 4096 271 and 191, 2 x 2048 x 4096 350 and 345, 1 x 8192 x 512 994
+    // and 149; n = 64, 1 x 8192 x 512: 2945 and 490.
+    const double share = channels > 4096 ? 3.5e-4 * (double)(channels - 4096) : 0.0;
+    const double uncut = p.n > 32 ? 12.4 : p.n > 16 ? 6.3 : channels < kWideLanes ? 4.1 + share : 8.3;
     const double full = p.n > 32 ? 12.4 : p.n > 16 ? 9.5 : 8.3;
     const double tiles = (double)p.steps / 32;
     const int64_t waves = p.batch * p.groups * ssm_blocks(p, kWave);
@@ -508,7 +514,7 @@ BackPlan back_plan(const libscan_ssm& p) {
         r.chunks = (int)((p.steps + r.chunk - 1) / r.chunk);
         r.pieces = (int)((p.steps + r.piece - 1) / r.piece);
     }
-    if (r.chunks == 1 && r.lanes == 8 && channels < 8192) {
+    if (r.chunks == 1 && r.lanes == 8 && channels < kWideLanes) {
         r.lanes = 16;
         r.nb = ssm_blocks(p, 256 / r.lanes);
     }
