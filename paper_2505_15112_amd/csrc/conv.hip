@@ -3,7 +3,8 @@
 // y[t] = f(bias + sum_j w[j] x[t - (W-1) + j]) per channel, W = 2..4.  HBM bounds
 // it: a thread owns 8 bytes of channels and a run of steps, so that every
 // input is loaded once (but for the W-1 in front of a run) and the window
-// slides through registers.
+// slides through registers.  The window is the inputs themselves, in their type;
+// sums and the weights' gradients are fp32, and a result is rounded once.
 #include "launch.hpp"
 #include "lm.hpp"
 
@@ -72,6 +73,10 @@ __device__ __forceinline__ void load_step(const libscan_conv& p, const T* px, co
         v.load(ps + (t + W - 1) * p.dim, ps ? count : 0);
 }
 
+// bf16, W = 4: 1 x 2048 x 4096 in 12 us, 4 x 2048 x 4096 in 35 us (134 MB: 3.9 TB/s).
+// Runs of 4, 8 and 16 steps by 8 and 16 bytes of channels were measured: longer
+// runs and wider threads leave too few waves, shorter runs load the W-1 inputs in
+// front of them too often.
 template <class T, int W>
 __global__ __launch_bounds__(kThreads) void k_conv(libscan_conv p, T* y, T* state_out) {
     constexpr int V = 8 / sizeof(T);
@@ -117,7 +122,7 @@ __global__ __launch_bounds__(kThreads) void k_conv(libscan_conv p, T* y, T* stat
     }
 }
 
-// One token against the pool.
+// One token against the pool: 64 rows of 4096 channels in 4 us, launch and latency.
 template <class T, int W>
 __global__ __launch_bounds__(kThreads) void k_conv_step(libscan_conv p, T* states,
                                                         int64_t n_states, const int32_t* slots,
@@ -166,7 +171,9 @@ struct BackArgs {
 };
 
 // Gradients.  g[t] = dy[t] f'(u[t]), u formed again; dx[t] = sum_j w[j] g[t + W-1 - j],
-// so a thread forms g of its run and of the W-1 steps behind it.
+// so a thread forms g of its run and of the W-1 steps behind it.  4 x 2048 x 4096,
+// bf16, W = 4: 55 us for 201 MB, 3.7 TB/s; the inner loop has no branches (73 us
+// with them), and loads kAhead steps ahead of what it uses.
 template <class T, int W, bool SILU>
 __global__ __launch_bounds__(kThreads) void k_conv_back(libscan_conv p, BackArgs o) {
     constexpr int V = kBackV;
@@ -323,7 +330,7 @@ __global__ __launch_bounds__(kThreads) void k_conv_back(libscan_conv p, BackArgs
     }
 }
 
-// dweight and dbias: the workgroups' sums, added in order.
+// dweight and dbias: the workgroups' sums, added in order: 5 us for 4096 channels.
 template <int SLICES>
 __global__ __launch_bounds__(kSumThreads) void k_conv_sum(const float* part, int64_t parts,
                                                           int64_t dim, int width, float* dweight,

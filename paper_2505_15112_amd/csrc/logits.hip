@@ -8,7 +8,13 @@
 // Rows longer than a segment take two kernels for probabilities.  The first
 // finds the segments' maxima and sums, and leaves the named tokens' logits in
 // their places of the output and the bits in scratch memory; the second has
-// nothing to count and only streams.
+// nothing to count and only streams.  Logits are fp32 from the load to the one
+// rounding of the result; shares and sums are fp32.
+//
+// HBM bounds large calls: 300 x 200003 fp32 with everything on, processed, 92 us
+// (487 MB, 5.3 TB/s); 128 x 131072 bf16 to probabilities with 2048 seen tokens a
+// row, 20 + 23 us (34 MB, then 101 MB), where the first kernel waits for its
+// counting.  One row of 131072: 5.3 + 3.7 us, launch and latency.
 #include "launch.hpp"
 #include "lm.hpp"
 
@@ -20,7 +26,9 @@ namespace {
 
 constexpr int kV = 8;  // consecutive places of a thread
 // Workgroups of so many threads, each with so many groups of kV places.  A few
-// rows are cut into small segments, to have more than a handful of workgroups.
+// rows are cut into small segments, to have more than a handful of workgroups:
+// one row of 131072 with 777 seen tokens takes 9.0 us of kernels in small segments
+// and 11.0 in large ones; 64 such rows of bf16 24 and 22.
 template <int THREADS, int PER>
 struct Cut {
     static constexpr int kThreads = THREADS, kPer = PER, kSeg = THREADS * PER * kV;

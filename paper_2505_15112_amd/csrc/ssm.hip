@@ -2,12 +2,17 @@
 //
 // h[t] = a[t] h[t-1] + b[t] per channel and state index, a = exp(delta A),
 // b = delta x B; y = sum over the state index of C h, plus D x, times
-// silu(z).  A workgroup owns CH channels of one row and walks the row in tiles
-// of 32 steps.  What depends on step and channel alone (softplus, delta x) is
-// computed once per tile by threads that own 16 bytes of channels, and goes
-// through LDS to the lanes that own (channel, state) pairs; their sums over
-// the state index go back the same way to be gated and stored.  The states
-// stay in registers for the whole row.
+// silu(z).  One exponential and four multiply-adds for every step, channel and
+// state, against 2 n of them to the bytes of one x: the vector units bound a
+// scan (4 waves to a SIMD: 10.5 ns for the five instructions of a wave), not
+// HBM.  States, sums and step sizes are fp32 whatever the type of the inputs;
+// y is rounded once.  exp(delta A) is 2^(delta (A log2 e)), A scaled once.
+//
+// Two ways to cut a call up (lane_plan says which, from measured times):
+// tiles (k_ssm_scan), one kernel that walks every row from end to end with a
+// channel's states shared out over lanes, for rows that fill the chip or are
+// short; and chunks (k_ssm_bc, k_ssm_ends, k_ssm_starts, k_ssm_lanes) with a
+// channel to a lane, for few long rows, whose steps are the latency.
 #include "launch.hpp"
 #include "lm.hpp"
 #include "ssm.hpp"
@@ -19,8 +24,18 @@ namespace {
 constexpr int kTile = 32;     // steps per tile
 constexpr int kThreads = 256;
 
+// The tiles.  A workgroup owns CH channels of one row and walks the row in tiles
+// of 32 steps.  What depends on step and channel alone (softplus, delta x) is
+// computed once per tile by threads that own 16 bytes of channels, and goes
+// through LDS to the lanes that own (channel, state) pairs; their sums over
+// the state index are shared out over the lanes of a channel, 16 steps at a
+// time, and go back the same way to be gated and stored.  The states stay in
+// registers for the whole row.
 // WHOLE: every row has all its steps, in whole tiles, and every workgroup all its
-// channels and states, so that nothing needs a check.
+// channels and states, so that nothing needs a check.  n = 16, with and without
+// the checks: 4 x 2048 x 4096 169 and 184 us, 1 x 2048 x 4096 98 and 116; four
+// lanes to a channel took a third longer on the first, for want of waves.
+// Ragged 16 x 501 x 4096: 95 us.
 template <class T, int LN, int SPL, bool WHOLE>
 __global__ __launch_bounds__(kThreads) void k_ssm_scan(libscan_ssm p, T* y, float* state_out,
                                                        float* ckpt, int nb) {
@@ -163,6 +178,8 @@ __global__ __launch_bounds__(kThreads) void k_ssm_scan(libscan_ssm p, T* y, floa
 
 // ---------------------------------------------------------------- long rows
 
+// B and C of the whole call for k_ssm_lanes and k_ssm_ends, which read them with
+// scalar loads and thus in fp32: 1 x 4096 tokens, n = 16: 5 us, launch and latency.
 template <class T, int NP>
 __global__ __launch_bounds__(kThreads) void k_ssm_bc(libscan_ssm p, float* bc) {
     constexpr int GP = LaneGroups<NP>::GP;
@@ -179,12 +196,14 @@ __global__ __launch_bounds__(kThreads) void k_ssm_bc(libscan_ssm p, float* bc) {
     out[GP] = in ? to_f32(pC[nn]) : 0.0f;
 }
 
-// The scan with a channel to a lane, all of its states in registers, and one
-// wave to a workgroup: B and C are the same for all lanes and come by scalar
-// loads, so that a step costs five vector instructions for each state (one of
-// them the exponential) and nothing goes through LDS.  Rows are cut into
-// chunks until the waves fill the chip; `starts` (NULL for one chunk) holds
-// the states that the chunks start from.
+// The scan with a channel to a lane and all of its states in registers: B and C
+// are the same for all lanes and come by scalar loads, so that a step costs five
+// vector instructions for each state (one of them the exponential) and nothing
+// goes through LDS.  Rows are cut into chunks until the waves fill the chip;
+// `starts` (NULL for one chunk) holds the states that the chunks start from.
+// 1 x 4096 x 4096, n = 16, 64 chunks: 72 us, against 43 for those instructions
+// alone; the rest is the softplus, the gate and each step's wait for its scalar
+// loads.  1 x 16389 x 2048: 150 us against 86.
 template <class T, int NP, bool GATE>
 __global__ __launch_bounds__(kWave * kLaneWaves) void k_ssm_lanes(libscan_ssm p, const float* bc_,
                                                      const float* starts, T* y, float* state_out,
@@ -300,7 +319,9 @@ __global__ __launch_bounds__(kWave * kLaneWaves) void k_ssm_lanes(libscan_ssm p,
 }
 
 // What a chunk does to any state it starts from: its decay exp(A sum delta) and
-// the state it ends in from zero.
+// the state it ends in from zero.  1 x 4096 x 4096: 54 us; the price of the
+// chunks, and with them still less than one walk over the row (tiles: 192 us
+// for the call, chunks 128).
 template <class T, int NP>
 __global__ __launch_bounds__(kWave * kLaneWaves) void k_ssm_ends(libscan_ssm p, const float* bc_, float* ends,
                                                     float* sums, int nb, int chunk,
@@ -380,6 +401,8 @@ __global__ __launch_bounds__(kWave * kLaneWaves) void k_ssm_ends(libscan_ssm p, 
     sums[row] = sum;
 }
 
+// Chains the chunks: a thread owns a (channel, state) pair and goes through the
+// ends in order, 16 loads in flight.  1 x 4096 x 4096, n = 16, 64 chunks: 11 us.
 template <int NP>
 __global__ __launch_bounds__(kThreads) void k_ssm_starts(libscan_ssm p, const float* init,
                                                          float* ends, const float* sums,
@@ -411,7 +434,9 @@ __global__ __launch_bounds__(kThreads) void k_ssm_starts(libscan_ssm p, const fl
 }
 
 // One token.  A quad of lanes owns a channel's states, four at a time: the
-// states, read and written once, are all the traffic that counts.
+// states, read and written once, are all the traffic that counts.  128 rows of
+// 5120 channels, n = 16: 20 us for 88 MB, 4.4 TB/s; one row of 2048: 4 us, launch
+// and the latency of two dependent loads.
 template <class T>
 __global__ __launch_bounds__(kThreads) void k_ssm_step(libscan_ssm p, float* states,
                                                        int64_t n_states, const int32_t* slots,
@@ -477,8 +502,10 @@ hipError_t scan_as(const libscan_ssm& p, void* y, float* state_out, float* ckpt,
     return hipGetLastError();
 }
 
-// From so many channels on, the tiles of eight lanes per channel fill the chip
-// without cutting rows (n <= 16).
+// From so many channels on, eight lanes to a channel in the tiles (n <= 16) are
+// enough waves for the chip, and share sums over fewer lanes; below, sixteen.
+// Eight and sixteen, rows of 2048 steps: 8192 channels 135 and 118 us, 12288 168
+// and 148, 16384 169 and 184; 32768 of 512 steps 75 and 89.
 constexpr int64_t kTileChannels = 16384;
 
 // How a call is cut up: `np` states to a lane and chunks of `chunk` steps.  np = 0:
