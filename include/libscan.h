@@ -552,9 +552,9 @@ int logits_process(const libscan_logits* p, void* out, int64_t out_row, void* st
 /* probs: rows x vocab fp32, dense: softmax of the processed logits divided by the
  * row's temperature, as topp_sample_f32 takes it.  A temperature of 0 is the
  * limit: equal shares for the places of the largest logit; a negative one turns
- * the logits over.  Places at -infinity
- * get 0; so does a row that has no others.  A NaN or +infinity elsewhere (but
- * for +infinity at temperature 0) makes every place above -infinity NaN.
+ * the logits over (+infinity is then a place without a share).  Places at
+ * -infinity get 0; so does a row that has no others.  A NaN, or +infinity at a
+ * temperature above 0, makes every place above -infinity NaN.
  * Scratch: logits_scratch_bytes (a host function). */
 int logits_probs(const libscan_logits* p, float* probs, void* scratch, size_t scratch_bytes,
                  void* stream);

@@ -153,6 +153,14 @@ def test_low_masks_of_half_types():
                         "equal")
 
 
+@pytest.mark.parametrize("vocab", [900, 20001])
+def test_negative_temperature(vocab):
+    """The least likely places first; masked and empty ones stay without a share."""
+    a = inputs(3, vocab, F32, hist=20, grammar=True)
+    a["logits"][1, 5:90] = R.NEG_INF
+    check(a, torch.tensor([-1.0, -0.7, -2.0]))
+
+
 def test_temperature_zero_shares_ties():
     a = inputs(2, 10000, F32)
     a["logits"][0, [3, 9000]] = 50.0
