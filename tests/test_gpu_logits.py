@@ -155,10 +155,14 @@ def test_low_masks_of_half_types():
 
 @pytest.mark.parametrize("vocab", [900, 20001])
 def test_negative_temperature(vocab):
-    """The least likely places first; masked and empty ones stay without a share."""
-    a = inputs(3, vocab, F32, hist=20, grammar=True)
+    """The shares of the negated logits, bit for bit; masked and empty places have none."""
+    a = inputs(3, vocab, F32, grammar=True)
     a["logits"][1, 5:90] = R.NEG_INF
-    check(a, torch.tensor([-1.0, -0.7, -2.0]))
+    other = dict(a, logits=(-a["logits"]).masked_fill(a["logits"] == R.NEG_INF, R.NEG_INF))
+    t = torch.tensor([1.0, 0.7, 2.0], device=DEV)
+    got = ops.logits_probs(**dev(a), temperature=-t)
+    assert torch.equal(got, ops.logits_probs(**dev(other), temperature=t))
+    assert got.sum(1).sub(1).abs().max() < 1e-4 and not got[1, 5:90].any()
 
 
 def test_temperature_zero_shares_ties():
