@@ -121,7 +121,8 @@ __global__ __launch_bounds__(kThreads) void k_ssm_scan(libscan_ssm p, T* y, floa
 
 #pragma unroll 1
         for (int tb = 0; tb < kTile; tb += kSsmBlock) {
-            if (ckpt && (WHOLE || t0 + tb < len)) {
+            if (!WHOLE && t0 + tb >= len) break;
+            if (ckpt) {
                 float* pc = pck + (int64_t)((t0 + tb) / kSsmBlock) * dim * n;
 #pragma unroll
                 for (int s = 0; s < SPL; ++s)

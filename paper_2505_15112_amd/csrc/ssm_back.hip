@@ -292,8 +292,10 @@ __global__ __launch_bounds__(kThreads) void k_ssm_back(libscan_ssm p, BackArgs o
         if (t0 > begin) fetch(t0 - TS);
         __syncthreads();
 
+        // blocks past the row's tokens (there is one before: t0 < len) leave cg as it is
+        const int top = WHOLE || t0 + TS - kT < len ? SUB - 1 : (len - 1 - t0) / kT;
 #pragma unroll 1
-        for (int sub = SUB - 1; sub >= 0; --sub) {
+        for (int sub = top; sub >= 0; --sub) {
             const int tb = sub * kT;
             float h[kT][SPL], a[kT][SPL], h0[SPL];
 #pragma unroll
