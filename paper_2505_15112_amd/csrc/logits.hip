@@ -206,9 +206,10 @@ __global__ __launch_bounds__(C::kThreads) void k_logits(libscan_logits p, T* out
 
     // Shares are e^((l - m) / temperature) for the row's largest logit m: the
     // difference first, as a logit times 1 / temperature may overflow (rows masked
-    // by the type's lowest value).  A negative temperature turns the logits over.
-    const float slope = kLog2e / temp, scale = __builtin_fabsf(slope);
-    const bool greedy = scale == -kNegInf, flip = slope < 0.0f, odd = greedy || scale == 0.0f;
+    // by the type's lowest value).  A negative temperature turns the logits over;
+    // -0.0, whose slope is -infinity, is not one.
+    const float scale = __builtin_fabsf(kLog2e / temp);
+    const bool greedy = scale == -kNegInf, flip = temp < 0.0f, odd = greedy || scale == 0.0f;
     const bool masked = bits != nullptr || size < C::kSeg;
     float v[kPer][kV];
     float top = kNegInf;

@@ -251,3 +251,16 @@ def test_refusals():
     with pytest.raises(_lib.LibscanError):  # too little scratch
         ops.logits_probs(torch.zeros(2, 50000, device=DEV),
                          scratch_buf=torch.empty(16, dtype=torch.uint8, device=DEV))
+
+
+@pytest.mark.parametrize("vocab", [900, 20001])
+@pytest.mark.parametrize("masked", [False, True])
+def test_temperature_of_negative_zero(vocab, masked):
+    """-0.0 is 0: the largest logit's places, as for +0.0."""
+    a = inputs(3, vocab, F32, hist=20, grammar=masked)
+    a["logits"][1, [4, 800]] = 60.0
+    zero = torch.zeros(3)
+    got = ops.logits_probs(**dev(a), temperature=(-zero).to(DEV)).cpu()
+    assert torch.equal(got, ops.logits_probs(**dev(a), temperature=zero.to(DEV)).cpu())
+    want = R.probs(ref(a)[0], zero)
+    assert ((got - want).abs() <= 2.0**-23 * want).all()
