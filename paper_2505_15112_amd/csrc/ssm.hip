@@ -404,6 +404,9 @@ __global__ __launch_bounds__(kWave * kLaneWaves) void k_ssm_ends(libscan_ssm p, 
 
 // Chains the chunks: a thread owns a (channel, state) pair and goes through the
 // ends in order, 16 loads in flight.  1 x 4096 x 4096, n = 16, 64 chunks: 11 us.
+// A whole chunk's decay 2^v may be beyond fp32 where h 2^v is not (of h = 0 nothing
+// grows): then h 2^(v/2) 2^(v/2), with finite factors.  Only then, as it is one more
+// multiplication after the other for every chunk (1 x 4096 x 2048, 128 chunks: 1.3 us).
 template <int NP>
 __global__ __launch_bounds__(kThreads) void k_ssm_starts(libscan_ssm p, const float* init,
                                                          float* ends, const float* sums,
@@ -416,21 +419,33 @@ __global__ __launch_bounds__(kThreads) void k_ssm_starts(libscan_ssm p, const fl
     float h = init && nn < p.n ? init[row * p.n + nn] : 0.0f;
     constexpr int kBatch = 16;  // loads in flight together
     for (int j0 = 0; j0 < chunks; j0 += kBatch) {
-        float e[kBatch], s[kBatch];
+        float e[kBatch], v[kBatch];
+        bool beyond = false;
 #pragma unroll
         for (int j = 0; j < kBatch; ++j) {
             const bool in = j0 + j + 1 < chunks;
             const int64_t at = (int64_t)(backward ? chunks - 1 - j0 - j : j0 + j) * rows;
             e[j] = in ? ends[at * NP + i] : 0.0f;
-            s[j] = in ? sums[at + row] : 0.0f;
+            v[j] = (in ? sums[at + row] : 0.0f) * a2;
+            beyond |= v[j] >= 127.0f;
         }
+        auto chain = [&](auto decayed) {
 #pragma unroll
-        for (int j = 0; j < kBatch; ++j)
-            if (j0 + j < chunks) {
-                const int64_t at = (int64_t)(backward ? chunks - 1 - j0 - j : j0 + j) * rows;
-                ends[at * NP + i] = h;
-                h = __builtin_fmaf(exp2_fast(s[j] * a2), h, e[j]);
-            }
+            for (int j = 0; j < kBatch; ++j)
+                if (j0 + j < chunks) {
+                    const int64_t at = (int64_t)(backward ? chunks - 1 - j0 - j : j0 + j) * rows;
+                    ends[at * NP + i] = h;
+                    h = decayed(v[j], e[j]);
+                }
+        };
+        if (__any(beyond))
+            chain([&](float v, float e) {
+                float half = exp2_fast(0.5f * v);
+                half = half > __FLT_MAX__ ? __FLT_MAX__ : half;
+                return __builtin_fmaf(half, half * h, e);
+            });
+        else
+            chain([&](float v, float e) { return __builtin_fmaf(exp2_fast(v), h, e); });
     }
 }
 

@@ -457,3 +457,50 @@ def test_scan_whole_tiles(size, kind):
         check_forward(a)
     check_backward(a, dy, dstate_out=torch.randn(size[0], size[2], size[3],
                                                  generator=torch.Generator().manual_seed(4)))
+
+
+# ---------------------------------------------------------------- edges
+
+def cut(a):
+    """Whether the call's rows are cut into chunks: (forward, backward)."""
+    p = ops._args.ssm(*(dev(a)[k] for k in ("x", "dt", "A", "B", "C", "D", "z", "dt_bias", "state",
+                                            "lengths")), True, False)
+    (batch, steps, dim), (groups, n) = a["x"].shape, a["B"].shape[2:]
+    _, forward, backward = ops._sizes("selective_scan_bytes", p, 3)
+    per = 32 if n <= 16 and batch * dim >= 16384 else 16  # channels of a workgroup, uncut
+    parts = -(-dim // groups // per)
+    whole = sum((v + 15) // 16 * 16 for v in (parts * batch * steps * groups * n * 8,
+                                               batch * dim * n * 4, batch * dim * 4, batch * dim * 4))
+    return forward > 0, backward != whole
+
+
+@pytest.mark.parametrize("first", [False, True])
+def test_chunks_of_growing_systems(first):
+    """Negative step sizes: the decay over a chunk is beyond fp32, the states are
+    not, as nothing (or next to nothing) is there to grow.  Forwards over the
+    first steps, backwards over the last."""
+    a, dy = inputs(1, 1537, 100, 16, skip=True, bias=False, state=True)
+    assert cut(a) == (True, True)
+    a["A"] = torch.full((100, 16), -8.0)
+    a["A"][:, ::2] = -6.0
+    a["dt"] = torch.full_like(a["dt"], 0.05)
+    so = None
+    if first:                       # a small start grows by e^112 in 40 steps
+        a["state"] *= 1e-30
+        a["dt"][:, :40] = -0.35
+        a["x"][:, :38] = 0
+        check_forward(a, softplus=False)
+        a, dy = inputs(1, 1537, 100, 16, skip=True, bias=False, state=True)
+        a["A"] = torch.full((100, 16), -8.0)
+        a["dt"] = torch.full_like(a["dt"], 0.05)
+        a["dt"][:, 1472:1512] = -0.35
+        a["x"][:, 1400:] = 0
+        dy[:, 1400:] = 0
+        so = torch.randn(1, 100, 16, generator=torch.Generator().manual_seed(6)) * 1e-30
+    else:                           # from nothing, by e^179 in 64
+        a["state"] = None
+        a["dt"][:, :64] = -0.35
+        a["x"][:, :62] = 0
+        dy[:, 10:] = 0
+        check_forward(a, softplus=False)
+    check_backward(a, dy, dstate_out=so, softplus=False)
