@@ -36,13 +36,16 @@ constexpr int kThreads = 256;
 // the checks: 4 x 2048 x 4096 169 and 184 us, 1 x 2048 x 4096 98 and 116; four
 // lanes to a channel took a third longer on the first, for want of waves.
 // Ragged 16 x 501 x 4096: 95 us.
-template <class T, int LN, int SPL, bool WHOLE>
+// Lanes whose states are padding read a delta and x of 0 (column CH): an infinite one
+// would make infinity times 0 of the padding's B, and NaN of the channel's sum.  PART:
+// some lane's states are padding in part (n is no multiple of SPL), and are held at 0.
+template <class T, int LN, int SPL, bool WHOLE, bool PART>
 __global__ __launch_bounds__(kThreads) void k_ssm_scan(libscan_ssm p, T* y, float* state_out,
                                                        float* ckpt, int nb) {
     using L = SsmLanes<LN, SPL>;
     constexpr int CH = L::CH, NP = L::NP, TPR = kThreads / kTile, VW = CH / TPR, YS = CH + 4;
     constexpr int NBC = kTile * NP / kThreads;
-    __shared__ float2 s_du[kTile][CH];  // delta, delta x
+    __shared__ float2 s_du[kTile][WHOLE ? CH : CH + 2];  // delta, delta x
     __shared__ float2 s_bc[kTile][NP];
     __shared__ float s_y[kTile][YS];
 
@@ -73,6 +76,8 @@ __global__ __launch_bounds__(kThreads) void k_ssm_scan(libscan_ssm p, T* y, floa
 
     // scanner: channel wc, states n0 .. n0 + SPL
     const int wc = wave * L::CPW + L::channel(lane), n0 = L::part(lane) * SPL;
+    const int from = WHOLE || n0 < n ? wc : CH;
+    if (!WHOLE && tid < kTile) s_du[tid][CH] = float2{0.0f, 0.0f};
     float a2[SPL], h[SPL];
     const int64_t sbase = ((int64_t)k.b * dim + k.c0 + wc) * n + n0;
     float* pck = ckpt + ((int64_t)k.b * ((steps + kSsmBlock - 1) / kSsmBlock) * dim + k.c0 + wc) * n +
@@ -131,13 +136,14 @@ __global__ __launch_bounds__(kThreads) void k_ssm_scan(libscan_ssm p, T* y, floa
             float v[kSsmBlock];
 #pragma unroll
             for (int t = 0; t < kSsmBlock; ++t) {
-                const float2 du = s_du[tb + t][wc];
+                const float2 du = s_du[tb + t][from];
                 float acc = 0.0f;
 #pragma unroll
                 for (int s = 0; s < SPL; ++s) {
                     const float2 bc = s_bc[tb + t][n0 + s];
                     const float a = exp2_fast(du.x * a2[s]);
                     h[s] = __builtin_fmaf(a, h[s], du.y * bc.x);
+                    if (PART && s && n0 + s >= n) h[s] = 0.0f;
                     acc = __builtin_fmaf(h[s], bc.y, acc);
                 }
                 v[t] = acc;
@@ -205,7 +211,9 @@ __global__ __launch_bounds__(kThreads) void k_ssm_bc(libscan_ssm p, float* bc) {
 // 1 x 4096 x 4096, n = 16, 64 chunks: 72 us, against 43 for those instructions
 // alone; the rest is the softplus, the gate and each step's wait for its scalar
 // loads.  1 x 16389 x 2048: 150 us against 86.
-template <class T, int NP, bool GATE>
+// PAD: n < NP, and the states past n (n > NP / 2 but for 8) are held at 0 or left out,
+// four at a time: an infinite delta or x would make NaN of them, and of y.
+template <class T, int NP, bool GATE, bool PAD>
 __global__ __launch_bounds__(kWave * kLaneWaves) void k_ssm_lanes(libscan_ssm p, const float* bc_,
                                                      const float* starts, T* y, float* state_out,
                                                      float* ckpt, int nb, int chunk,
@@ -230,7 +238,7 @@ __global__ __launch_bounds__(kWave * kLaneWaves) void k_ssm_lanes(libscan_ssm p,
     {
         const float* from = starts ? starts + ((int64_t)w.c * p.batch * dim + row) * NP
                                    : p.state ? p.state + row * n : nullptr;
-        const int have = starts ? NP : p.state ? n : 0;
+        const int have = starts || p.state ? n : 0;
         load_states<NP>(p.A + (int64_t)ch * n, n, a2);
         load_states<NP>(from, have, h);
 #pragma unroll
@@ -250,10 +258,16 @@ __global__ __launch_bounds__(kWave * kLaneWaves) void k_ssm_lanes(libscan_ssm p,
             next.template load<2 * GP>(g + 1 < NG ? bc + (g + 1) * 2 * GP : bc);
             __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-            for (int i = 0; i < GP; ++i) {
-                float& hi = h[g * GP + i];
-                hi = __builtin_fmaf(exp2_fast(delta * a2[g * GP + i]), hi, u * cur.v[i]);
-                acc[i & 1] = __builtin_fmaf(hi, cur.v[GP + i], acc[i & 1]);
+            for (int i0 = 0; i0 < GP; i0 += 4) {
+                const int s0 = g * GP + i0;
+                if (PAD && s0 >= NP / 2 && s0 >= n) break;
+#pragma unroll
+                for (int i = i0; i < i0 + 4; ++i) {
+                    float& hi = h[g * GP + i];
+                    hi = __builtin_fmaf(exp2_fast(delta * a2[g * GP + i]), hi, u * cur.v[i]);
+                    if (PAD && (NP == 8 || s0 >= NP / 2) && g * GP + i >= n) hi = 0.0f;
+                    acc[i & 1] = __builtin_fmaf(hi, cur.v[GP + i], acc[i & 1]);
+                }
             }
             cur = next;
         }
@@ -490,7 +504,7 @@ __global__ __launch_bounds__(kThreads) void k_ssm_step(libscan_ssm p, float* sta
         for (int i = 0; i < 4; ++i) {
             h.v[i] = __builtin_fmaf(exp2_fast(delta * (a.v[i] * kLog2e)), h.v[i],
                                     u * to_f32(B.v[i]));
-            acc = __builtin_fmaf(h.v[i], to_f32(C.v[i]), acc);
+            if (i0 + i < n) acc = __builtin_fmaf(h.v[i], to_f32(C.v[i]), acc);
         }
         h.store(ph + i0, n - i0);
     }
@@ -513,7 +527,9 @@ hipError_t scan_as(const libscan_ssm& p, void* y, float* state_out, float* ckpt,
     const int64_t grid = p.batch * p.groups * nb;
     const bool whole = !p.lengths && p.steps % kTile == 0 && p.n == LN * SPL &&
                        p.dim / p.groups % SsmLanes<LN, SPL>::CH == 0;
-    auto* scan = whole ? k_ssm_scan<T, LN, SPL, true> : k_ssm_scan<T, LN, SPL, false>;
+    auto* scan = whole       ? k_ssm_scan<T, LN, SPL, true, false>
+                 : p.n % SPL ? k_ssm_scan<T, LN, SPL, false, (SPL > 1)>
+                             : k_ssm_scan<T, LN, SPL, false, false>;
     scan<<<dim3((unsigned)grid), kThreads, 0, stream>>>(p, (T*)y, state_out, ckpt, nb);
     return hipGetLastError();
 }
@@ -585,7 +601,8 @@ hipError_t lanes_as(const libscan_ssm& p, const LanePlan& l, void* y, float* sta
             p, bc, ends, sums, l.nb, l.chunk, waves);
         launch_ssm_starts(p, NP, p.state, ends, sums, l.chunks, false, stream);
     }
-    auto* scan = p.z ? k_ssm_lanes<T, NP, true> : k_ssm_lanes<T, NP, false>;
+    auto* scan = p.n == NP ? p.z ? k_ssm_lanes<T, NP, true, false> : k_ssm_lanes<T, NP, false, false>
+                           : p.z ? k_ssm_lanes<T, NP, true, true> : k_ssm_lanes<T, NP, false, true>;
     scan<<<dim3(grid, l.chunks), kWave * kLaneWaves, 0, stream>>>(
         p, bc, l.chunks > 1 ? ends : nullptr, (T*)y, state_out, ckpt, l.nb, l.chunk,
         waves);

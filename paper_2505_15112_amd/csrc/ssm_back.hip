@@ -155,7 +155,10 @@ __device__ __forceinline__ void after(float v, LdsIn& p, LdsBc& q) {
 // the whole call: 541 us, with the checks 601; 16 steps staged at a time instead of
 // 32 took 35 us more, four lanes to a channel (one wave to a SIMD for want of
 // registers) 200 more.
-template <class T, int LN, int SPL, bool WHOLE>
+// Lanes whose channel or states are padding read zeros alone (column CH of s_in, NP on
+// of s_bc), so that no infinity there meets a 0 and no NaN the sums.  PART: some lane's
+// states are padding in part (n is no multiple of SPL), and are held at 0.
+template <class T, int LN, int SPL, bool WHOLE, bool PART>
 __global__ __launch_bounds__(kThreads) void k_ssm_back(libscan_ssm p, BackArgs o, int nb) {
     using L = SsmLanes<LN, SPL>;
     constexpr int CH = L::CH, NP = L::NP, YS = CH + 4;
@@ -163,8 +166,9 @@ __global__ __launch_bounds__(kThreads) void k_ssm_back(libscan_ssm p, BackArgs o
     constexpr int TS = NP > 32 ? 16 : 32, SUB = TS / kT, TPR = kThreads / TS, VW = CH / TPR;
     constexpr int NBC = TS * NP / kThreads;
     static_assert(VW * TPR == CH && NBC * kThreads == TS * NP, "a tile is shared out evenly");
-    __shared__ float4 s_in[TS][CH];  // delta, delta x, w
-    __shared__ float2 s_bc[TS][NP];
+    constexpr int INS = WHOLE ? CH : CH + 1, BCS = WHOLE ? NP : NP + (SPL > 2 ? SPL : 2);
+    __shared__ float4 s_in[TS][INS];  // delta, delta x, w
+    __shared__ float2 s_bc[TS][BCS];
     __shared__ float s_y[TS][YS], s_du[TS][YS], s_dd[TS][YS];
     __shared__ float2 s_g[4][TS][NP + 1];
 
@@ -203,6 +207,12 @@ __global__ __launch_bounds__(kThreads) void k_ssm_back(libscan_ssm p, BackArgs o
     }
 
     const int wc = wave * L::CPW + L::channel(lane), n0 = L::part(lane) * SPL;
+    const bool used = WHOLE || (wc < lim && n0 < n);
+    if (!WHOLE && tid < TS) {
+        s_in[tid][CH] = float4{0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+        for (int s = 0; s < SPL; ++s) s_bc[tid][NP + s] = float2{0.0f, 0.0f};
+    }
     float a2[SPL], da[SPL], cg[SPL];  // cg: a[t+1] G[t+1] of the step that follows
     const int64_t sbase = ((int64_t)k.b * dim + k.c0 + wc) * n + n0;
     const float* pck = o.ckpt + ((int64_t)k.b * blocks * dim + k.c0 + wc) * n + n0;
@@ -300,8 +310,8 @@ __global__ __launch_bounds__(kThreads) void k_ssm_back(libscan_ssm p, BackArgs o
             float h[kT][SPL], a[kT][SPL], h0[SPL];
 #pragma unroll
             for (int s = 0; s < SPL; ++s) h0[s] = sub ? starts[SUB - 1][s] : starts[0][s];
-            LdsIn in_at = (LdsIn)&s_in[tb][wc];
-            LdsBc bc_at = (LdsBc)&s_bc[tb][n0];
+            LdsIn in_at = (LdsIn)&s_in[tb][WHOLE || used ? wc : CH];
+            LdsBc bc_at = (LdsBc)&s_bc[tb][WHOLE || used ? n0 : NP];
             {
                 float hr[SPL], v[kT];
 #pragma unroll
@@ -309,13 +319,14 @@ __global__ __launch_bounds__(kThreads) void k_ssm_back(libscan_ssm p, BackArgs o
 #pragma unroll
                 for (int t = 0; t < kT; ++t) {
                     if (t % kGroup == 0) after(hr[0], in_at, bc_at);
-                    const float4 in = load_lds(in_at + t * CH);
+                    const float4 in = load_lds(in_at + t * INS);
                     float acc = 0.0f;
 #pragma unroll
                     for (int s = 0; s < SPL; ++s) {
-                        const float2 bc = load_lds(bc_at + t * NP + s);
+                        const float2 bc = load_lds(bc_at + t * BCS + s);
                         a[t][s] = exp2_fast(in.x * a2[s]);
                         hr[s] = __builtin_fmaf(a[t][s], hr[s], in.y * bc.x);
+                        if (PART && s && n0 + s >= n) a[t][s] = hr[s] = 0.0f;
                         h[t][s] = hr[s];
                         acc = __builtin_fmaf(hr[s], bc.y, acc);
                     }
@@ -328,12 +339,13 @@ __global__ __launch_bounds__(kThreads) void k_ssm_back(libscan_ssm p, BackArgs o
 #pragma unroll
                 for (int t = kT - 1; t >= 0; --t) {
                     if (t % kGroup == kGroup - 1) after(cg[0], in_at, bc_at);
-                    const float4 in = load_lds(in_at + t * CH);
+                    const float4 in = load_lds(in_at + t * INS);
                     float du = 0.0f, dd = 0.0f;
 #pragma unroll
                     for (int s = 0; s < SPL; ++s) {
-                        const float2 bc = load_lds(bc_at + t * NP + s);
-                        const float g = __builtin_fmaf(in.z, bc.y, cg[s]);
+                        const float2 bc = load_lds(bc_at + t * BCS + s);
+                        float g = __builtin_fmaf(in.z, bc.y, cg[s]);
+                        if (PART && s && n0 + s >= n) g = 0.0f;
                         du = __builtin_fmaf(g, bc.x, du);
                         cg[s] = a[t][s] * g;
                         const float r = cg[s] * (t ? h[t ? t - 1 : 0][s] : h0[s]);
@@ -551,7 +563,9 @@ void back_as(const libscan_ssm& p, const BackArgs& o, const BackPlan& l, hipStre
     if (grid == 0) return;
     const bool whole = !p.lengths && p.steps % 32 == 0 && p.n == LN * SPL &&
                        p.dim / p.groups % SsmLanes<LN, SPL>::CH == 0;
-    auto* back = whole ? k_ssm_back<T, LN, SPL, true> : k_ssm_back<T, LN, SPL, false>;
+    auto* back = whole       ? k_ssm_back<T, LN, SPL, true, false>
+                 : p.n % SPL ? k_ssm_back<T, LN, SPL, false, (SPL > 1)>
+                             : k_ssm_back<T, LN, SPL, false, false>;
     back<<<dim3((unsigned)grid, l.chunks), kThreads, 0, stream>>>(p, o, l.nb);
 }
 

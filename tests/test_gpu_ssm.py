@@ -504,3 +504,83 @@ def test_chunks_of_growing_systems(first):
         dy[:, 10:] = 0
         check_forward(a, softplus=False)
     check_backward(a, dy, dstate_out=so, softplus=False)
+
+
+def assert_same(got, ref, mag, c, what):
+    """NaN where the definition has NaN, its infinities, and the bounds elsewhere."""
+    g = got.detach().cpu().double()
+    assert torch.equal(g.isnan(), ref.isnan()), \
+        f"{what}: NaN at {(g.isnan() != ref.isnan()).nonzero()[:3].tolist()}"
+    assert torch.equal(g[ref.isinf()], ref[ref.isinf()]), what
+    odd = ~ref.isfinite()
+    R.assert_within(got.detach().cpu().masked_fill(odd, 0), ref.masked_fill(odd, 0),
+                    mag.masked_fill(~mag.isfinite(), 0), c, what)
+
+
+def check_same(a, dy=None, softplus=True, dstate_out=None):
+    """The call against the definition where inputs may be infinite or NaN."""
+    batch, steps, dim = a["x"].shape
+    d = dev(a)
+    announce("selective_scan", tuple(a["x"].shape), tuple(a["B"].shape), a["x"].dtype)
+    y, last, kept = ops.selective_scan(**d, softplus=softplus, with_state=True,
+                                       with_checkpoints=True)
+    more = dict(softplus_on=softplus)
+    if dy is not None:
+        more.update(dy=dy.double(),
+                    dstate_out=dstate_out.double() if dstate_out is not None else None)
+    ref = R.scan(**ref_args(a), **more)
+    mag = R.scan(**ref_args(a), **more, absolute=True)
+    assert_same(y, ref["y"], mag["y"], 4 * (steps + 32), "y")
+    assert_same(last, ref["state"], mag["state"], 4 * (steps + 32), "state")
+    if dy is None:
+        return
+    got = ops.selective_scan_backward(
+        dy.to(DEV), kept, **d, softplus=softplus, with_dstate=True,
+        dstate_out=dstate_out.to(DEV) if dstate_out is not None else None)
+    for name, g in zip(NAMES, got):
+        extra = dim + batch * steps if name in ("dA", "dB", "dC", "dD", "ddt_bias") else 0
+        assert_same(g, ref[name], mag[name], 8 * (steps + 32) + extra, name)
+
+
+def positive(*size, **kw):
+    """Inputs whose products are all positive, so that infinities do not cancel."""
+    a, dy = inputs(*size, state=True, **kw)
+    for k in ("x", "B", "C", "D", "z", "state"):
+        a[k] = a[k].abs() + 0.1
+    a["A"] = -(a["A"].abs() * 0.02 + 0.01)
+    return a, dy.abs() + 0.1
+
+
+PADDED = [(2, 20, 40, 1, 1), (1, 35, 34, 5, 2), (1, 20, 17, 7, 1), (1, 33, 20, 16, 1),
+          (2, 18, 40, 17, 1), (1, 20, 33, 33, 1), (1, 17, 20, 62, 1), (1, 18, 16400, 5, 1),
+          (1, 18, 16400, 8, 2), (1, 801, 40, 3, 1), (1, 801, 40, 11, 2), (1, 801, 33, 20, 1),
+          (1, 801, 20, 50, 1)]
+
+
+@pytest.mark.parametrize("size", PADDED)
+def test_infinities_where_states_or_channels_do_not_fill_the_lanes(size):
+    """An infinite input, step size, gradient or C gives the infinities that the
+    definition has, whatever n and the channels are padded to."""
+    a, _ = positive(*size)
+    if size[1] > 800:
+        assert cut(a) == (True, True)
+    a["x"][0, 5, 3] = a["dt"][0, 9, 12] = float("inf")
+    check_same(a)
+    a, dy = positive(*size)
+    dy[0, 6, 3] = float("inf")
+    check_same(a, dy)
+    a, dy = positive(*size)
+    a["C"][0, 7, 0, 0] = float("inf")
+    check_same(a, dy)
+
+
+@pytest.mark.parametrize("n", [1, 3, 8, 18, 64])
+def test_step_infinities(n):
+    a, _ = positive(2, 1, 40, n)
+    a["x"][0, 0, 3] = a["dt"][1, 0, 9] = float("inf")
+    d = dev(a)
+    y = ops.selective_scan_step(d["x"][:, 0], d["dt"][:, 0], d["state"], d["A"], d["B"][:, 0],
+                                d["C"][:, 0], D=d["D"], z=d["z"][:, 0], dt_bias=d["dt_bias"])
+    ref, mag = R.scan(**ref_args(a)), R.scan(**ref_args(a), absolute=True)
+    assert_same(y, ref["y"][:, 0], mag["y"][:, 0], 4 * 33, "y")
+    assert_same(d["state"], ref["state"], mag["state"], 4 * 33, "state")
