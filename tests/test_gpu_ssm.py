@@ -584,3 +584,27 @@ def test_step_infinities(n):
     ref, mag = R.scan(**ref_args(a)), R.scan(**ref_args(a), absolute=True)
     assert_same(y, ref["y"][:, 0], mag["y"][:, 0], 4 * 33, "y")
     assert_same(d["state"], ref["state"], mag["state"], 4 * 33, "state")
+
+
+@pytest.mark.parametrize("size", [(1, 20, 40, 16, 1), (2, 33, 20, 20, 2), (1, 5, 34, 64, 1),
+                                  (1, 18, 16400, 16, 1), (1, 801, 40, 16, 1)])
+@pytest.mark.parametrize("ragged", [False, True])
+def test_nothing_follows_a_rows_last_token(size, ragged):
+    """A NaN or an infinity in the last token's x is in none of the gradients that
+    it has no part in (A's among them)."""
+    batch, steps = size[:2]
+    count = steps - 3 if ragged else steps
+    a, dy = positive(*size, lengths=[count] * batch if ragged else None)
+    a["x"][0, count - 1, 3] = float("nan")
+    a["x"][0, count - 1, 5] = float("inf")
+    check_same(a, dy, dstate_out=torch.rand(
+        batch, *a["A"].shape, generator=torch.Generator().manual_seed(9)))
+
+
+@pytest.mark.parametrize("size", PADDED)
+def test_an_infinite_state_beyond_the_last_token(size):
+    """An infinity in B stays in the states to the end; steps that are not the row's
+    have no part in the gradients."""
+    a, dy = positive(*size)
+    a["B"][0, 7, 0, 0] = float("inf")
+    check_same(a, dy)
