@@ -335,7 +335,7 @@ __global__ __launch_bounds__(kThreads) void k_ssm_back(libscan_ssm p, BackArgs o
                 if (gate) L::sum_states(v, lane, [&](int t, float sum) { s_y[tb + t][wc] = sum; });
             }
             // A block that the row ends in has steps past it, which leave cg as it is and
-            // must not multiply their delta of 0 with a state that is infinite by then.
+            // must not multiply their delta of 0 with a state or a gradient that is infinite.
             const int left = len - t0 - tb;
             {
                 float vu[kT], vd[kT];
@@ -351,9 +351,8 @@ __global__ __launch_bounds__(kThreads) void k_ssm_back(libscan_ssm p, BackArgs o
                         if (PART && s && n0 + s >= n) g = 0.0f;
                         du = __builtin_fmaf(g, bc.x, du);
                         cg[s] = a[t][s] * g;
-                        float before = t ? h[t ? t - 1 : 0][s] : h0[s];
-                        if (!WHOLE && t >= left) before = 0.0f;
-                        const float r = cg[s] * before;
+                        float r = cg[s] * (t ? h[t ? t - 1 : 0][s] : h0[s]);
+                        if (!WHOLE && t >= left) r = 0.0f;
                         dd = __builtin_fmaf(r, a2[s], dd);
                         da[s] = __builtin_fmaf(r, in.x, da[s]);
                         a[t][s] = g * in.y;  // a and h of this step are done with: dB and dC

@@ -608,3 +608,12 @@ def test_an_infinite_state_beyond_the_last_token(size):
     a, dy = positive(*size)
     a["B"][0, 7, 0, 0] = float("inf")
     check_same(a, dy)
+
+
+@pytest.mark.parametrize("size", PADDED)
+def test_an_infinite_gradient_of_the_last_state(size):
+    """It comes in before the steps that are not the row's, and passes them by."""
+    a, dy = positive(*size)
+    so = torch.rand(size[0], *a["A"].shape, generator=torch.Generator().manual_seed(9))
+    so[0, 3, 0] = float("inf")
+    check_same(a, dy, dstate_out=so)
