@@ -202,10 +202,12 @@ __global__ __launch_bounds__(kThreads) void k_conv_back(libscan_conv p, BackArgs
     if (count > 0 && (t0 < steps || t0 == 0)) {
         float x[W][V];        // x[t - (W-1)] .. x[t]
         float g[W][V] = {};   // g[t - (W-1)] .. g[t]
+        // (no output of an empty row reads its first state)
+        const int open = len > 0 ? count : 0;
 #pragma unroll
         for (int j = 0; j < W - 1; ++j) {
             Pack<T, V> v;
-            load_step<T, W, V>(p, px, ps, t0 - (W - 1) + j, len, count, v);
+            load_step<T, W, V>(p, px, ps, t0 - (W - 1) + j, len, open, v);
 #pragma unroll
             for (int c = 0; c < V; ++c) x[j][c] = to_f32(v.v[c]);
         }
@@ -228,11 +230,15 @@ __global__ __launch_bounds__(kThreads) void k_conv_back(libscan_conv p, BackArgs
                     gv *= sig * __builtin_fmaf(u, 1.0f - sig, 1.0f);
                 }
                 g[W - 1][c] = t < len ? gv : 0.0f;
+                // Past the row's end g is 0, and inputs that are infinite or NaN must not meet
+                // it.  (With the silu they have made NaN of the last outputs' g already, and
+                // with it of all that they could spoil.)
                 if (own) {
                     db[c] += g[W - 1][c];
 #pragma unroll
                     for (int j = 0; j < W; ++j)
-                        dw[j][c] = __builtin_fmaf(g[W - 1][c], x[j][c], dw[j][c]);
+                        dw[j][c] = __builtin_fmaf(g[W - 1][c], SILU || t < len ? x[j][c] : 0.0f,
+                                                  dw[j][c]);
                 }
             }
         };

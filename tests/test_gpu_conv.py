@@ -187,3 +187,39 @@ def test_refusals():
         ops.causal_conv(x, w, state=state, state_out=state)
     with pytest.raises(ValueError):
         ops.causal_conv_step(x[:, 0], state[:1], w)
+
+
+def check_dweight(x, w, b, state, dy, lengths=None, silu=True):
+    n = torch.tensor(lengths, dtype=torch.int32) if lengths is not None else None
+    xd, wd, bd, sd, dyd = to(x, w, b, state, dy)
+    announce("causal_conv_backward", tuple(x.shape), tuple(w.shape), x.dtype)
+    got = ops.causal_conv_backward(dyd, xd, wd, bd, state=sd,
+                                   lengths=n.to(DEV) if n is not None else None, silu=silu)[1]
+    args = (dy.double(), *dbl(x, w, b, state), n, silu)
+    want, mag = R.conv_back(*args)[1], R.conv_back(*args, absolute=True)[1]
+    g, odd = got.cpu(), ~want.isfinite()
+    assert torch.equal(g.isnan(), want.isnan()) and torch.equal(g[odd & ~want.isnan()].double(),
+                                                                 want[odd & ~want.isnan()])
+    R.assert_within(g.masked_fill(odd, 0), want.masked_fill(odd, 0),
+                    mag.masked_fill(~mag.isfinite(), 0), 24 + x.shape[0] * x.shape[1], "dweight")
+
+
+@pytest.mark.parametrize("width", [2, 3, 4])
+@pytest.mark.parametrize("value", [float("nan"), float("inf")])
+def test_conv_weights_that_a_last_input_does_not_meet(width, value):
+    """The last input meets the last weight only; an infinity or NaN there is in no
+    other weight's gradient."""
+    for lengths in (None, [40, 17]):
+        x, w, b, state, dy = inputs(2, 40, 37, width, F32, state=True)
+        x[0, 39, 5] = value
+        x[1, 16 if lengths else 39, 8] = value
+        check_dweight(x, w, b, state, dy, lengths, silu=False)
+
+
+@pytest.mark.parametrize("silu", [True, False])
+def test_conv_weights_and_a_row_without_tokens(silu):
+    """What the first state of an empty row holds is in no weight's gradient."""
+    x, w, b, state, dy = inputs(3, 40, 37, 4, BF16, state=True)
+    state[1] = float("nan")
+    state[2] = float("inf")
+    check_dweight(x, w, b, state, dy, [40, 0, -2], silu)
