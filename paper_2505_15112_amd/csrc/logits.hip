@@ -115,7 +115,7 @@ __device__ __forceinline__ void note_named(const libscan_logits& p, const T* px,
     });
     __syncthreads();
     if (n > 0) {
-        const float rep = p.repetition ? p.repetition[row] : 1.0f, inv_rep = 1.0f / rep;
+        const float rep = p.repetition ? p.repetition[row] : 1.0f;
         const float pres = p.presence ? p.presence[row] : 0.0f;
         const float freq = p.frequency ? p.frequency[row] : 0.0f;
         each_id<C>(ids, n, first_ids, [&](int, int id) {
@@ -123,7 +123,7 @@ __device__ __forceinline__ void note_named(const libscan_logits& p, const T* px,
             if (at < (uint32_t)size && !(atomicOr(&s.named[at >> 5], bit) & bit)) {
                 const uint32_t c = s.word[at];
                 float l = to_f32(px[at]);
-                l *= l > 0.0f ? inv_rep : rep;
+                l = l > 0.0f ? l / rep : l * rep;
                 if (c) l = l - (float)c * freq - pres;
                 s.word[at] = as_u32(l);
             }

@@ -264,3 +264,15 @@ def test_temperature_of_negative_zero(vocab, masked):
     assert torch.equal(got, ops.logits_probs(**dev(a), temperature=zero.to(DEV)).cpu())
     want = R.probs(ref(a)[0], zero)
     assert ((got - want).abs() <= 2.0**-23 * want).all()
+
+
+@pytest.mark.parametrize("vocab", [3000, 20001])
+def test_repetition_divides(vocab):
+    """Seen tokens alone: one rounding, that of l / repetition or l * repetition."""
+    x = inputs(3, vocab, F32)["logits"]
+    x[2] *= 1e-30
+    rep = torch.tensor([1.1, 0.7, 1e-39])  # the last one's reciprocal is beyond fp32
+    got = ops.logits_process(x.to(DEV), history=torch.arange(vocab).int().expand(3, -1).to(DEV),
+                             prompt_len=torch.full((3,), vocab).int().to(DEV),
+                             repetition=rep.to(DEV)).cpu()
+    assert torch.equal(got, torch.where(x > 0, x / rep[:, None], x * rep[:, None]))
