@@ -276,3 +276,49 @@ def test_repetition_divides(vocab):
                              prompt_len=torch.full((3,), vocab).int().to(DEV),
                              repetition=rep.to(DEV)).cpu()
     assert torch.equal(got, torch.where(x > 0, x / rep[:, None], x * rep[:, None]))
+
+
+@pytest.mark.parametrize("vocab,biases", [(40, 700), (5000, 4000), (20001, 3001)])
+@pytest.mark.parametrize("hist", [0, 300])
+def test_biases_that_repeat_add_up_in_the_lists_order(vocab, biases, hist):
+    """Single-precision additions one by one, so the same bits."""
+    a = inputs(2, vocab, F32, hist=hist)
+    base = ops.logits_process(**dev(a)).cpu() if hist else a["logits"]
+    g = torch.Generator().manual_seed(3)
+    ids = torch.randint(-1, vocab + 1, (2, biases), generator=g).int()
+    ids[1, ::3] = 7                     # one id in a third of the list
+    ids[0, biases // 2:] = ids[0, :biases - biases // 2].clone()
+    values = torch.randn(2, biases, generator=g) * 3
+    got = ops.logits_process(**dev(dict(a, bias_ids=ids, bias_values=values))).cpu()
+    want = base.clone().numpy()
+    for r in range(2):
+        for tok, v in zip(ids[r].tolist(), values[r].numpy()):
+            if 0 <= tok < vocab:
+                want[r, tok] += v
+    assert torch.equal(got, torch.from_numpy(want))
+
+
+def test_repeated_biases_take_no_quadratic_time():
+    """A long list with every id twice, or one id alone, against one without
+    repeats: a few walks over the list, where a search for each entry's repeats
+    took 1600 times as long (50 times are room for noise)."""
+    g = torch.Generator(device=DEV).manual_seed(1)
+    x = torch.randn(1, 131072, device=DEV, generator=g)
+    once = torch.randperm(131072, device=DEV, generator=g)[None, :16384].int().contiguous()
+    twice = torch.cat((once[:, :8192], once[:, :8192]), 1)
+    values = torch.randn(1, 16384, device=DEV, generator=g)
+
+    def time(ids):
+        ops.logits_process(x, bias_ids=ids, bias_values=values)
+        each = []
+        for _ in range(5):
+            a, b = (torch.cuda.Event(enable_timing=True) for _ in range(2))
+            a.record()
+            ops.logits_process(x, bias_ids=ids, bias_values=values)
+            b.record()
+            torch.cuda.synchronize()
+            each.append(a.elapsed_time(b))
+        return sorted(each)[2]
+
+    limit = 50 * time(once)
+    assert time(twice) < limit and time(torch.full_like(once, 77)) < limit
