@@ -8,7 +8,8 @@ with LS_ADVERSARIAL_DELAYS (pseudo-random pauses before every inter-workgroup
 protocol step) for the adversarial-scheduling tests; it binds its own symbols
 (-Bsymbolic) so that it can be loaded beside libscan.so.  csrc/torch_args.cpp,
 which checks torch tensors for the binding, becomes _torch_args.so (host code,
-against torch's headers).
+against torch's headers), which only the binding needs: it is left out where torch
+is not installed, and an error in it is raised when the libraries are linked.
 """
 import concurrent.futures as cf
 import glob
@@ -93,9 +94,13 @@ def build(verbose: bool = False) -> str:
     with cf.ThreadPoolExecutor(max_workers=min(8, len(jobs) + 1)) as ex:
         args = ex.submit(_torch_args, verbose)
         objs = list(ex.map(lambda j: _compile(j[0], verbose, j[1], j[2]), jobs))
-    args.result()
     _link(objs[:len(srcs)], LIB, verbose)
     _link(objs[len(srcs):], LIB_ADV, verbose, ("-Wl,-Bsymbolic",))
+    try:
+        args.result()
+    except ImportError as e:
+        print(f"{LIB} is built; without torch ({e}) the binding's {os.path.basename(LIB_ARGS)} "
+              "is not", file=sys.stderr)
     return LIB
 
 
