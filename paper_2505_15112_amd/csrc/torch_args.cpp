@@ -10,6 +10,7 @@
 #include <Python.h>
 
 #include <ATen/ATen.h>
+#include <c10/core/GradMode.h>
 #include <torch/csrc/autograd/python_variable.h>
 
 #include <sstream>
@@ -101,6 +102,20 @@ T* address(PyObject* o, const char* name, at::ScalarType type, at::IntArrayRef s
     return o == Py_None ? nullptr : (T*)operand(o, name, type, shape, on, dense).data_ptr();
 }
 
+// Says that the call records no graph, if one of its first n arguments (tensors or
+// None by now) would have it recorded.
+void no_graph(PyObject* const* a, int n, const char* instead) {
+    if (!c10::GradMode::is_enabled()) return;
+    for (int i = 0; i < n; ++i) {
+        if (a[i] == Py_None || !THPVariable_Unpack(a[i]).requires_grad()) continue;
+        const std::string s = std::string("an argument requires gradients, but no autograd graph "
+                                          "is recorded here: ") + instead;
+        // (the caller of the binding's function)
+        if (PyErr_WarnEx(PyExc_UserWarning, s.c_str(), 2) < 0) throw Raised();
+        return;
+    }
+}
+
 bool truth(PyObject* o) {
     const int v = PyObject_IsTrue(o);
     if (v < 0) throw Raised();
@@ -136,6 +151,7 @@ PyObject* conv(PyObject* const* a) {
     p.bias = address(a[2], "bias", w.scalar_type(), {p.dim}, x, true);
     p.state = address(a[3], "state", kind, {p.batch, p.width - 1, p.dim}, x, true);
     p.lengths = address<int32_t>(a[4], "lengths", at::kInt, {p.batch}, x, true);
+    no_graph(a, 5, step ? "a step has no gradients" : "causal_conv_backward forms the gradients");
     return packed(p);
 }
 
@@ -183,6 +199,8 @@ PyObject* ssm(PyObject* const* a) {
     p.dt_bias = address<float>(a[7], "dt_bias", at::kFloat, {p.dim}, x, true);
     p.state = address<float>(a[8], "state", at::kFloat, {p.batch, p.dim, p.n}, x, true);
     p.lengths = address<int32_t>(a[9], "lengths", at::kInt, {p.batch}, x, true);
+    no_graph(a, 10, step ? "a step has no gradients"
+                         : "selective_scan_backward forms the gradients");
     return packed(p);
 }
 
@@ -224,6 +242,7 @@ PyObject* logits(PyObject* const* a) {
         p.allowed_row = al.stride(0);
     }
     p.temperature = address<float>(a[10], "temperature", at::kFloat, {p.rows}, x, true);
+    no_graph(a, 11, "processed logits have no gradients");
     return packed(p);
 }
 

@@ -447,6 +447,10 @@ def topk_rows_f32(x, k, largest=True, values_out=None, idx_out=None, ws=None, sc
 
 
 # ---------------------------------------------------------------- language model operators
+#
+# None of these records an autograd graph; where an argument would have it recorded,
+# a UserWarning says so.  A torch.autograd.Function that calls an operator and its
+# *_backward is what training takes (examples/state_space_lm.py has one for each).
 
 class _Args:
     """The compiled checks of torch_args.cpp, loaded at the first use: conv, ssm and

@@ -61,3 +61,42 @@ def test_training_lowers_the_loss(lm):
     ids, lengths = data(300)
     losses = [lm.train_step(model, ids, lengths, rate=0.2) for _ in range(8)]
     assert losses[-1] < 0.8 * losses[0], losses
+
+
+def test_a_graph_that_is_not_recorded_is_said_so(lm):
+    """Arguments that require gradients: a warning that names the caller's line, and
+    none where no graph is wanted, or the call is a Function's."""
+    import warnings
+
+    from paper_2505_15112_amd import ops
+    x, w = torch.randn(2, 5, 8, device="cuda"), torch.randn(8, 4, device="cuda")
+    A, B = -torch.rand(8, 4, device="cuda"), torch.randn(2, 5, 1, 4, device="cuda")
+    pool, window = torch.zeros(2, 8, 4, device="cuda"), torch.zeros(2, 3, 8, device="cuda")
+
+    def calls(x, w, A):
+        return [(lambda: ops.causal_conv(x, w), "causal_conv_backward"),
+                (lambda: ops.selective_scan(x, x, A, B, B), "selective_scan_backward"),
+                (lambda: ops.causal_conv_step(x[:, 0], window, w), "no gradients"),
+                (lambda: ops.selective_scan_step(x[:, 0], x[:, 0], pool, A, B[:, 0], B[:, 0]),
+                 "no gradients"),
+                (lambda: ops.logits_process(x[0]), "no gradients"),
+                (lambda: ops.logits_probs(x[0]), "no gradients")]
+
+    leaf = x.clone().requires_grad_()
+    for call, what in calls(leaf, w, A):
+        with pytest.warns(UserWarning, match=what) as said:
+            call()
+        assert said[0].filename == __file__
+    with pytest.warns(UserWarning, match="causal_conv_backward"):
+        ops.causal_conv(x, w.clone().requires_grad_())
+    with pytest.warns(UserWarning, match="selective_scan_backward"):
+        ops.selective_scan(x, x, A.clone().requires_grad_(), B, B)
+    with warnings.catch_warnings():
+        warnings.simplefilter("error")
+        for call, _ in calls(x, w, A):
+            call()
+        with torch.no_grad():
+            for call, _ in calls(leaf, w, A):
+                call()
+        ids, lengths = data(50)
+        lm.train_step(lm.Model(vocab=50, dim=64), ids, lengths)
