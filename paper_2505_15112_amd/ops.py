@@ -560,8 +560,6 @@ def _pool(states, x, tail, f32, slots):
         if count < x.shape[0]:
             raise ValueError("states: fewer than the rows of x")
         return ps, count, None
-    if slots.dtype != torch.int32:
-        raise TypeError(f"slots: expected torch.int32, got {slots.dtype}")
     _check(slots, torch.int32, "slots", (1,))
     if slots.shape[0] != x.shape[0] or slots.get_device() != x.get_device():
         raise ValueError("slots: expected one for each row of x, on its GPU")

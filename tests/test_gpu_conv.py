@@ -223,3 +223,14 @@ def test_conv_weights_and_a_row_without_tokens(silu):
     state[1] = float("nan")
     state[2] = float("inf")
     check_dweight(x, w, b, state, dy, [40, 0, -2], silu)
+
+
+def test_step_refuses_slots_that_are_no_tensor():
+    x, w, _, state, _ = to(*inputs(2, 1, 8, 4, F32, state=True))
+    for slots in ([0, 1], 1, torch.zeros(2, dtype=torch.int64, device=DEV)):
+        with pytest.raises(TypeError, match="slots"):
+            ops.causal_conv_step(x[:, 0], state, w, slots=slots)
+    for slots in (torch.zeros(2, dtype=torch.int32),
+                  torch.zeros(3, dtype=torch.int32, device=DEV)):
+        with pytest.raises(ValueError, match="slots"):
+            ops.causal_conv_step(x[:, 0], state, w, slots=slots)
