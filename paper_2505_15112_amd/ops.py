@@ -486,6 +486,8 @@ def _scratch_for(buf, nbytes, like):
     if buf is None:
         return _args.memory(max(16, nbytes), like)
     _check(buf, torch.uint8, "scratch_buf")
+    if buf.get_device() != like.get_device():
+        raise ValueError(f"scratch_buf: expected memory on the operands' GPU, got {buf.device}")
     return buf
 
 

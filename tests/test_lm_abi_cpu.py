@@ -202,3 +202,19 @@ def test_binding_needs_gpu_tensors():
         ops.logits_process([1.0])
     with pytest.raises(TypeError, match="float32, float16 or bfloat16"):
         ops.logits_process(torch.zeros(2, 10, dtype=torch.float64))
+
+
+def test_scratch_of_another_gpu_is_refused(monkeypatch):
+    """(Stand-ins: a kernel of one GPU must not get memory of another.)"""
+    class On:
+        def __init__(self, i):
+            self.i, self.device = i, f"cuda:{i}"
+
+        def get_device(self):
+            return self.i
+
+    monkeypatch.setattr(ops, "_check", lambda *a, **k: None)
+    here, there = On(0), On(1)
+    assert ops._scratch_for(here, 16, On(0)) is here
+    with pytest.raises(ValueError, match="scratch_buf"):
+        ops._scratch_for(there, 16, On(0))
