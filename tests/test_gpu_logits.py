@@ -322,3 +322,17 @@ def test_repeated_biases_take_no_quadratic_time():
 
     limit = 50 * time(once)
     assert time(twice) < limit and time(torch.full_like(once, 77)) < limit
+
+
+@pytest.mark.parametrize("rows,vocab", [(1, 200003), (4, 600001)])
+@pytest.mark.parametrize("named", [True, False])
+def test_rows_of_more_than_64_segments(rows, vocab, named):
+    """More segments than a wave has lanes, small ones and large ones: the maximum
+    and most of the sum beyond the first 64, and among them."""
+    a = (inputs(rows, vocab, BF16, hist=60, biases=9, grammar=True) if named
+         else inputs(rows, vocab, BF16))
+    for at in (vocab - 3, 5):
+        a["logits"][:, at] = 25.0
+        if named:
+            a["allowed"][:, at // 32] = -1
+        check(a, torch.linspace(0.5, 1.5, rows))

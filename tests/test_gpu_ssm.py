@@ -617,3 +617,66 @@ def test_an_infinite_gradient_of_the_last_state(size):
     so = torch.rand(size[0], *a["A"].shape, generator=torch.Generator().manual_seed(9))
     so[0, 3, 0] = float("inf")
     check_same(a, dy, dstate_out=so)
+
+
+CHUNKED = [  # gate, skip, bias, softplus, ragged
+    (True, True, True, True, True), (False, True, True, True, True), (True, False, False, True, False),
+    (False, False, True, False, True), (True, True, False, False, False),
+    (False, True, False, True, False),
+]
+
+
+@pytest.mark.parametrize("n,groups", [(1, 1), (8, 1), (16, 2), (20, 1), (50, 2), (64, 1)])
+@pytest.mark.parametrize("kind", [F32, F16, BF16])
+def test_chunks_without_parts(n, groups, kind):
+    """Rows that are cut, with and without a gate, D, a bias, the softplus and
+    lengths, against the definition."""
+    steps = 801 if n <= 32 else 1201
+    i = [1, 8, 16, 20, 50, 64].index(n) + 2 * [F32, F16, BF16].index(kind)
+    for gate, skip, bias, softplus, ragged in (CHUNKED[i % 6], CHUNKED[(i + 3) % 6]):
+        lengths = [steps, 0, 33, 500] if ragged else None
+        rows = 4 if ragged else 2
+        a, dy = inputs(rows, steps, 70, n, groups, kind=kind, gate=gate, skip=skip, bias=bias,
+                       state=ragged, lengths=lengths)
+        if not softplus:
+            a["dt"] = a["dt"].abs() * 0.2
+            a["dt_bias"] = a["dt_bias"].abs() * 0.1 if bias else None
+        assert cut(a) == (True, True)
+        for b, count in enumerate(lengths or []):
+            for k in ("x", "dt", "z", "B", "C"):
+                if a[k] is not None:
+                    a[k][b, count:] = float("nan")
+            dy[b, count:] = float("nan")
+        check_forward(a, softplus)
+        so = torch.randn(rows, 70, n, generator=torch.Generator().manual_seed(8))
+        check_backward(a, dy, dstate_out=so, softplus=softplus)
+
+
+@pytest.mark.parametrize("n,groups", [(16, 1), (20, 2), (64, 1)])
+@pytest.mark.parametrize("kind", [F32, BF16])
+def test_chunks_of_strided_rows(n, groups, kind):
+    """Cut rows on slices of wider tensors, time before batch, off 16 bytes, and
+    one row's inputs for several (stride 0), against the definition."""
+    a, dy = inputs(3, 801, 34, n, groups, kind=kind, state=True)
+    a["dt"] = a["dt"][:1].expand(3, 801, 34)
+    assert cut(a) == (True, True)
+    ref, mag = (R.scan(**ref_args(a), dy=dy.double(), absolute=v) for v in (False, True))
+    d = dev(a)
+    wide = torch.full((801, 3, 3 * 34 + 1), float("nan"), dtype=kind, device=DEV)
+    views = [wide[:, :, 1 + 34 * i:35 + 34 * i].transpose(0, 1) for i in range(3)]
+    for v, t in zip(views, (a["x"], a["z"], dy)):
+        v.copy_(t)
+    both = torch.full((3, 801, 1 + 2 * groups * n), float("nan"), dtype=kind, device=DEV)
+    for i, k in enumerate("BC"):
+        v = both[:, :, 1 + i * groups * n:1 + (i + 1) * groups * n].unflatten(2, (groups, n))
+        v.copy_(d[k])
+        d[k] = v
+    d["x"], d["z"] = views[:2]
+    d["dt"] = a["dt"][:1].to(DEV).expand(3, 801, 34)
+    y, last, kept = ops.selective_scan(**d, with_state=True, with_checkpoints=True)
+    R.assert_within(y, ref["y"], mag["y"], 4 * 833, "y")
+    R.assert_within(last, ref["state"], mag["state"], 4 * 833, "state")
+    got = ops.selective_scan_backward(views[2], kept, **d)
+    for name, g in zip(NAMES, got):
+        extra = 34 + 3 * 801 if name in ("dA", "dB", "dC", "dD", "ddt_bias") else 0
+        R.assert_within(g, ref[name], mag[name], 8 * 833 + extra, name)
