@@ -20,6 +20,9 @@ from paper_2505_15112_amd import ops  # noqa: E402
 
 
 class Conv(torch.autograd.Function):
+    """ops.causal_conv on rows that start from nothing (no first state, which
+    causal_conv_backward has a gradient for)."""
+
     @staticmethod
     def forward(ctx, x, weight, bias, lengths):
         y, _ = ops.causal_conv(x, weight, bias, lengths=lengths)
@@ -35,6 +38,8 @@ class Conv(torch.autograd.Function):
 
 
 class Scan(torch.autograd.Function):
+    """ops.selective_scan on rows that start from nothing, as Conv."""
+
     @staticmethod
     def forward(ctx, x, dt, A, B, C, D, z, dt_bias, lengths):
         y, _, kept = ops.selective_scan(x, dt, A, B, C, D=D, z=z, dt_bias=dt_bias,

@@ -484,7 +484,15 @@ typedef struct {
 } libscan_ssm;
 
 /* Bytes of the checkpoints that selective_scan hands to its gradient, and of
- * the scratch of either.  Host function; only the sizes in *p are read. */
+ * the scratch of either.  Host function; only the sizes in *p are read.
+ * checkpoints: batch * ceil(steps / 16) * dim * n * 4.  scratch: 0, or for rows cut into
+ * chunks (up to 4096 waves of 64 channels in all) 8 bytes for each token, group and
+ * state of n rounded up to 8, 16, 32 or 64, and 4 for each chunk, channel and state.
+ * backward_scratch: the partial sums of dB and dC, 8 bytes for each token, group and
+ * state times the ceil(dim / groups / 16) workgroups of a group (32 channels, not 16,
+ * where n <= 16 and batch * dim >= 16384, or the rows are cut): n / 2 or n / 4 bytes
+ * for each token and channel, 32 at n = 64, where all of bf16's x, dt, z and dy are 8;
+ * and 4 for each chunk, channel and state, with what the chunks need as above. */
 int selective_scan_bytes(const libscan_ssm* p, size_t* checkpoints, size_t* scratch,
                          size_t* backward_scratch);
 
@@ -514,7 +522,7 @@ int selective_scan_step(const libscan_ssm* p, float* states, int64_t n_states,
 /* Logits before a sampler.  logits: rows x vocab, row stride logits_row.  In this
  * order, per row:
  *  - every token id that history[0 .. history_len) holds: l > 0 ? l / repetition :
- *    l * repetition;
+ *    l * repetition (one rounding);
  *  - every id that history[prompt_len .. history_len) holds c > 0 times:
  *    l -= c * frequency + presence;
  *  - every entry of bias_ids (rows x biases): l += its value (several entries of
@@ -554,7 +562,8 @@ int logits_process(const libscan_logits* p, void* out, int64_t out_row, void* st
  * limit: equal shares for the places of the largest logit; a negative one turns
  * the logits over (+infinity is then a place without a share).  Places at
  * -infinity get 0; so does a row that has no others.  A NaN, or +infinity at a
- * temperature above 0, makes every place above -infinity NaN.
+ * temperature above 0, makes every place above -infinity NaN.  -0.0 is 0.  A share
+ * below 2^-126 may be 0.
  * Scratch: logits_scratch_bytes (a host function). */
 int logits_probs(const libscan_logits* p, float* probs, void* scratch, size_t scratch_bytes,
                  void* stream);

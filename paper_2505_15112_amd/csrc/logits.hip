@@ -11,10 +11,10 @@
 // nothing to count and only streams.  Logits are fp32 from the load to the one
 // rounding of the result; shares and sums are fp32.
 //
-// HBM bounds large calls: 300 x 200003 fp32 with everything on, processed, 92 us
-// (487 MB, 5.3 TB/s); 128 x 131072 bf16 to probabilities with 2048 seen tokens a
-// row, 20 + 23 us (34 MB, then 101 MB), where the first kernel waits for its
-// counting.  One row of 131072: 5.3 + 3.7 us, launch and latency.
+// HBM bounds large calls: 300 x 200003 fp32 with everything on, processed, 94 us
+// (487 MB, 5.2 TB/s); 128 x 131072 bf16 to probabilities with 2048 seen tokens a
+// row, 21 + 24 us (34 MB, then 101 MB), where the first kernel waits for its
+// counting.  One row of 131072: 5.6 + 3.7 us, launch and latency.
 #include "launch.hpp"
 #include "lm.hpp"
 

@@ -209,15 +209,18 @@ __global__ __launch_bounds__(kThreads) void k_ssm_bc(libscan_ssm p, float* bc) {
 // goes through LDS.  Rows are cut into chunks until the waves fill the chip;
 // `starts` (NULL for one chunk) holds the states that the chunks start from.
 // 1 x 4096 x 4096, n = 16, 64 chunks: 72 us, against 43 for those instructions
-// alone; the rest is the softplus, the gate and each step's wait for its scalar
-// loads.  1 x 16389 x 2048: 150 us against 86.
+// alone.  A step issues 113 vector instructions, not those 80 (the softplus, the gate,
+// types and addresses are the others), and the vector units are busy for 76 % of the
+// time; the scalar loads are not what they wait for (with the loads taken out it was
+// no faster).  1 x 16389 x 2048: 149 us against 86.
 // PAD: n < NP, and the states past n (n > NP / 2 but for 8) are held at 0 or left out,
 // four at a time: an infinite delta or x would make NaN of them, and of y.
 template <class T, int NP, bool GATE, bool PAD>
 __global__ __launch_bounds__(kWave * kLaneWaves) void k_ssm_lanes(libscan_ssm p, const float* bc_,
-                                                     const float* starts, T* y, float* state_out,
-                                                     float* ckpt, int nb, int chunk,
-                                                                uint32_t waves) {
+                                                                  const float* starts, T* y,
+                                                                  float* state_out, float* ckpt,
+                                                                  int nb, int chunk,
+                                                                  uint32_t waves) {
     using Groups = LaneGroups<NP>;
     constexpr int GP = Groups::GP, NG = Groups::NG;
     if (blockIdx.x * kLaneWaves + threadIdx.x / kWave >= waves) return;
@@ -338,9 +341,9 @@ __global__ __launch_bounds__(kWave * kLaneWaves) void k_ssm_lanes(libscan_ssm p,
 // chunks, and with them still less than one walk over the row (tiles: 192 us
 // for the call, chunks 128).
 template <class T, int NP>
-__global__ __launch_bounds__(kWave * kLaneWaves) void k_ssm_ends(libscan_ssm p, const float* bc_, float* ends,
-                                                    float* sums, int nb, int chunk,
-                                                                uint32_t waves) {
+__global__ __launch_bounds__(kWave * kLaneWaves) void k_ssm_ends(libscan_ssm p, const float* bc_,
+                                                                 float* ends, float* sums, int nb,
+                                                                 int chunk, uint32_t waves) {
     using Groups = LaneGroups<NP>;
     constexpr int GP = Groups::GP, NG = Groups::NG;
     if (blockIdx.x * kLaneWaves + threadIdx.x / kWave >= waves) return;
@@ -549,7 +552,9 @@ struct LanePlan {
 // The time of either way in us, as measured over 1 to 16 rows of 64 to 8192 steps and
 // 70 to 4096 channels with 8 to 64 states.  The tiles walk a row at a step's
 // latency, and share SIMDs beyond 4096 channels.  The chunks have four kernels and
-// two chunks' steps to wait for, and then the vector units to keep busy.
+// two chunks' steps to wait for, and then the vector units to keep busy (a call that
+// fills the chip with one chunk has two of them, and is rated the same).  Other sizes
+// go by the same two lines.
 // E.g. n = 16, tiles against chunks: 1 x 512 x 1024 26.6 and 29.5, 1 x 1024 x 4096 51.5
 // and 51.8, 1 x 2048 x 1024 96 and 44, 1 x 8192 x 512 373 and 66, 2 x 2048 x 4096 118
 // and 124 us.

@@ -460,7 +460,7 @@ __global__ __launch_bounds__(kThreads) void k_ssm_back(libscan_ssm p, BackArgs o
 }
 
 // dB and dC: the workgroups' sums of a group, added in order (eight threads to an
-// output from 16 parts on).  4 x 2048 x 4096, n = 16, 128 parts: 24 us for 134 MB.
+// output from 17 parts on).  4 x 2048 x 4096, n = 16, 128 parts: 24 us for 134 MB.
 template <class T, int SLICES>
 __global__ __launch_bounds__(kSumThreads) void k_ssm_sum_bc(libscan_ssm p, const float2* part,
                                                             int nb, T* dB, T* dC) {
@@ -523,9 +523,10 @@ BackPlan back_plan(const libscan_ssm& p) {
     const int64_t groups = p.batch * p.groups * r.nb, fit = p.n > 32 ? 256 : 512;
     int64_t chunks = groups > 0 ? fit / groups : 1;
     if (chunks > p.steps / 64) chunks = p.steps / 64;
-    // Times in us of a 32-step tile: uncut, and with the CUs full.  n = 16, uncut and in
-    // chunks: 1 x 2048 x 4096 271 and 191, 2 x 2048 x 4096 350 and 345, 1 x 8192 x 512 994
-    // and 149; n = 64, 1 x 8192 x 512: 2945 and 490.
+    // Times in us of a 32-step tile: uncut, and with the CUs full, as measured for 1 to 16
+    // rows of 128 to 8192 steps (other sizes go by the same lines).  The whole call, n =
+    // 16, uncut and in chunks: 1 x 2048 x 4096 271 and 186, 2 x 2048 x 4096 350 and 345,
+    // 1 x 8192 x 512 1005 and 131; n = 64, 1 x 8192 x 512: 2848 and 480.
     const double share = channels > 4096 ? 3.5e-4 * (double)(channels - 4096) : 0.0;
     const double uncut = p.n > 32   ? 12.4
                          : p.n > 16 ? 6.3

@@ -463,8 +463,8 @@ class _Args:
         spec = importlib.util.spec_from_file_location("_torch_args", path)
         module = importlib.util.module_from_spec(spec)
         spec.loader.exec_module(module)
-        self.__dict__.update({k: getattr(module, k)
-                              for k in ("conv", "ssm", "logits", "dense", "empty", "sizes", "memory", "floats")})
+        names = ("conv", "ssm", "logits", "dense", "empty", "sizes", "memory", "floats")
+        self.__dict__.update({k: getattr(module, k) for k in names})
         return self.__dict__[name]
 
 
@@ -608,7 +608,8 @@ def selective_scan_backward(dy, checkpoints, x, dt, A, B, C, D=None, z=None, dt_
     of its last state), with its inputs and its checkpoints.  Returns (dx, ddt,
     dA, dB, dC, dD or None, dz or None, ddt_bias or None, dstate or None): those
     of A, D, dt_bias and state in fp32, the last by default formed when there is
-    a state."""
+    a state.  The scratch holds partial sums of dB and dC, up to n / 2 bytes for each
+    token and channel (include/libscan.h, selective_scan_bytes)."""
     p = _args.ssm(x, dt, A, B, C, D, z, dt_bias, state, lengths, softplus, False)
     batch, _, dim = x.shape
     kept, _, need = _sizes("selective_scan_bytes", p, 3)
@@ -625,8 +626,9 @@ def selective_scan_backward(dy, checkpoints, x, dt, A, B, C, D=None, z=None, dt_
     dbias = new(dt_bias, True) if dt_bias is not None else None
     dstate = _into(None, x, (batch, dim, A.shape[1]), True) if with_dstate else None
     buf = _scratch_for(scratch_buf, need, x)
-    _launch("selective_scan_backward", x, p, pdy, dy.stride(0), dy.stride(1), pk, pso, _ptr(dx), _ptr(ddt), _ptr(dA), _ptr(dB), _ptr(dC), _ptr(dD), _ptr(dz),
-            _ptr(dbias), _ptr(dstate), _ptr(buf), buf.numel())
+    _launch("selective_scan_backward", x, p, pdy, dy.stride(0), dy.stride(1), pk, pso, _ptr(dx),
+            _ptr(ddt), _ptr(dA), _ptr(dB), _ptr(dC), _ptr(dD), _ptr(dz), _ptr(dbias),
+            _ptr(dstate), _ptr(buf), buf.numel())
     return dx, ddt, dA, dB, dC, dD, dz, dbias, dstate
 
 
