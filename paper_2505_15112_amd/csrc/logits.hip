@@ -159,6 +159,12 @@ __device__ __forceinline__ void note_named(const libscan_logits& p, const T* px,
     const bool repeats = s.repeats;
     if (n > 0) {
         const float rep = p.repetition ? p.repetition[row] : 1.0f;
+        // l / rep, rounded once, as the product with the reciprocal in 64 bits: it is off by
+        // at most 2^-52 of the quotient, and a normal quotient of 24-bit numbers at least 2^-49
+        // of itself from where the rounding to 24 bits turns.  (19 rows of 3185 places
+        // with 7381 tokens: a division for each token 14.7 us, this 13.4, a product with the
+        // rounded reciprocal, which rounds twice, 12.7.)
+        const double inv_rep = 1.0 / (double)rep;
         const float pres = p.presence ? p.presence[row] : 0.0f;
         const float freq = p.frequency ? p.frequency[row] : 0.0f;
         each_id<C>(ids, n, first_ids, [&](int, int id) {
@@ -166,7 +172,7 @@ __device__ __forceinline__ void note_named(const libscan_logits& p, const T* px,
             if (at < (uint32_t)size && !(atomicOr(&s.named[at >> 5], bit) & bit)) {
                 const uint32_t c = s.word[at];
                 float l = to_f32(px[at]);
-                l = l > 0.0f ? l / rep : l * rep;
+                l = l > 0.0f ? (float)((double)l * inv_rep) : l * rep;
                 if (c) l = l - (float)c * freq - pres;
                 s.word[at] = as_u32(l);
             }

@@ -336,3 +336,24 @@ def test_rows_of_more_than_64_segments(rows, vocab, named):
         if named:
             a["allowed"][:, at // 32] = -1
         check(a, torch.linspace(0.5, 1.5, rows))
+
+
+def test_repetition_divides_at_its_ends():
+    """Penalties and logits from the smallest to the largest, 0, infinities and NaN: the
+    quotient's bits (results below the normal range aside)."""
+    g = torch.Generator().manual_seed(5)
+    rep = torch.cat((torch.tensor([0.0, 1e-45, 1e-39, 2.0**-126, 2.0**-125, 1.0, 3.0, 2.0**126,
+                                   3.4e38, float("inf"), float("nan")]),
+                     torch.exp2(torch.rand(53, generator=g) * 250 - 125),
+                     torch.rand(192, generator=g) + 0.5))
+    x = torch.exp2(torch.rand(len(rep), 4001, generator=g) * 250 - 125)
+    x[:, ::2] = torch.rand(len(rep), 2001, generator=g) * 8
+    x[:, :4] = torch.tensor([0.0, float("inf"), 3.4e38, 1e-38])
+    rows, vocab = x.shape
+    got = ops.logits_process(x.to(DEV), history=torch.arange(vocab).int().expand(rows, -1).to(DEV),
+                             prompt_len=torch.full((rows,), vocab).int().to(DEV),
+                             repetition=rep.to(DEV)).cpu()
+    want = torch.where(x > 0, x / rep[:, None], x * rep[:, None])
+    assert torch.equal(got.isnan(), want.isnan())
+    normal = (want >= 2.0**-126) | (want == 0)
+    assert normal.double().mean() > 0.7 and torch.equal(got[normal], want[normal])
