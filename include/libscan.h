@@ -396,7 +396,8 @@ int libscan_scratch_bytes(int op, int64_t rows, int64_t len, int64_t k, size_t* 
 /* ------------------------------------------------------------------------
  * Language model operators: the first-order linear recurrence of selective
  * state space layers (a prefix scan with h_t = a_t h_{t-1} + b_t in the place
- * of the sum, Section 2), the short causal convolution in front of it, and
+ * of the sum, Section 2) and of linear attention (the same with matrices for
+ * states), the short causal convolution in front of it, layer norm, and
  * the logits' processing in front of topp_sample_f32 and topk_rows_f32
  * (Section 5).  They are described by structs whose fields are all 8 bytes
  * wide (strides in elements).  Rules shared by all of them:
@@ -518,6 +519,85 @@ int selective_scan_backward(const libscan_ssm* p, const void* dy, int64_t dy_bat
  * dim); the pool states (n_states x dim x n, dense fp32) move on in place. */
 int selective_scan_step(const libscan_ssm* p, float* states, int64_t n_states,
                         const int32_t* slots, void* y, void* stream);
+
+/* Linear attention with a decay for each head: per row b and head h, with group
+ * g = h / (heads / groups), a state S of dk x dv,
+ *   S[t] = exp(log_decay[t,h]) S[t-1] + k[t,g] v[t,h]^T
+ *   y[t,h] = scale * q[t,g] S[t]
+ * q, k: batch x steps x groups x dk; v, y: batch x steps x heads x dv, with unit
+ * stride over the last dimension.  log_decay: fp32, batch x steps x heads with
+ * unit stride over heads, or (fixed != 0) heads, one for all tokens; 0 keeps the
+ * state, -infinity clears it.  state (nullable: zeros): batch x heads x dk x dv,
+ * dense fp32.  1 <= dk, dv <= 256, heads a multiple of groups. */
+typedef struct {
+    int64_t type, batch, steps, heads, groups, dk, dv, fixed;
+    const void* q;
+    int64_t q_batch, q_step, q_head;
+    const void* k;
+    int64_t k_batch, k_step, k_head;
+    const void* v;
+    int64_t v_batch, v_step, v_head;
+    const float* log_decay;
+    int64_t decay_batch, decay_step;
+    double scale;
+    const float* state;
+    const int32_t* lengths;
+} libscan_attend;
+
+/* Scratch bytes of linear_attention and of its gradients.  Host function; only the
+ * sizes in *p are read. */
+int linear_attention_bytes(const libscan_attend* p, size_t* scratch, size_t* backward_scratch);
+
+/* y: batch x steps x heads x dv; state_out (nullable): batch x heads x dk x dv fp32,
+ * the last state. */
+int linear_attention(const libscan_attend* p, void* y, float* state_out, void* scratch,
+                     size_t scratch_bytes, void* stream);
+
+/* Gradients for dy (batch x steps x heads x dv, strides dy_batch, dy_step, dy_head)
+ * and dstate_out (nullable, batch x heads x dk x dv fp32: the gradient of the last
+ * state), from the same *p: dq, dk (of the groups), dv, of `type`; dlog_decay (of
+ * log_decay's shape: 0 where the decay is -infinity) and dstate (nullable: batch x
+ * heads x dk x dv), fp32.  Sums run in a fixed order. */
+int linear_attention_backward(const libscan_attend* p, const void* dy, int64_t dy_batch,
+                              int64_t dy_step, int64_t dy_head, const float* dstate_out, void* dq,
+                              void* dk, void* dv, float* dlog_decay, float* dstate, void* scratch,
+                              size_t scratch_bytes, void* stream);
+
+/* One token of every row (steps = 1; p->state and p->lengths NULL): y (batch x heads x
+ * dv); the pool states (n_states x heads x dk x dv, dense fp32) move on in place. */
+int linear_attention_step(const libscan_attend* p, float* states, int64_t n_states,
+                          const int32_t* slots, void* y, void* stream);
+
+/* Layer norm: y = (x - mean) / sqrt(var + eps) * weight + bias over each of `groups`
+ * groups of dim / groups neighbouring channels (var with divisor dim / groups).  With
+ * residual, x is first replaced by x + residual, rounded to `type`.  x, residual
+ * (nullable): batch x steps x dim; weight, bias (nullable): dim, dense, of
+ * `weight_type` (type or LIBSCAN_F32).  dim a multiple of groups; eps >= 0. */
+typedef struct {
+    int64_t type, weight_type, batch, steps, dim, groups;
+    double eps;
+    const void* x;
+    int64_t x_batch, x_step;
+    const void* residual;
+    int64_t residual_batch, residual_step;
+    const void* weight;
+    const void* bias;
+} libscan_norm;
+
+/* y: batch x steps x dim; sum (nullable): x + residual, likewise; stats (nullable):
+ * batch x steps x groups x 2 fp32, mean and 1 / sqrt(var + eps). */
+int layer_norm(const libscan_norm* p, void* y, void* sum, float* stats, void* stream);
+
+/* Gradients for dy and dsum (nullable), batch x steps x dim, where p->x is what was
+ * normalised (the sum, where there was a residual; p->residual NULL) and stats what
+ * layer_norm gave: dx (the gradient of both x and residual, dsum added), batch x steps
+ * x dim of `type`; dweight, dbias (nullable): dim, fp32.  Sums run in a fixed order.
+ * Scratch: what layer_norm_scratch_bytes reports (a host function). */
+int layer_norm_backward(const libscan_norm* p, const void* dy, int64_t dy_batch, int64_t dy_step,
+                        const void* dsum, int64_t dsum_batch, int64_t dsum_step,
+                        const float* stats, void* dx, float* dweight, float* dbias, void* scratch,
+                        size_t scratch_bytes, void* stream);
+int layer_norm_scratch_bytes(const libscan_norm* p, size_t* bytes);
 
 /* Logits before a sampler.  logits: rows x vocab, row stride logits_row.  In this
  * order, per row:

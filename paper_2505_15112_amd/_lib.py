@@ -71,6 +71,14 @@ SIGNATURES = {
     "selective_scan": (_int, [_struct, _p, _p, _p, _p, _sz, _p]),
     "selective_scan_backward": (_int, [_struct, _p, _i64, _i64] + [_p] * 12 + [_sz, _p]),
     "selective_scan_step": (_int, [_struct, _p, _i64, _p, _p, _p]),
+    "linear_attention_bytes": (_int, [_struct, ctypes.POINTER(_sz), ctypes.POINTER(_sz)]),
+    "linear_attention": (_int, [_struct, _p, _p, _p, _sz, _p]),
+    "linear_attention_backward": (_int, [_struct, _p] + [_i64] * 3 + [_p] * 7 + [_sz, _p]),
+    "linear_attention_step": (_int, [_struct, _p, _i64, _p, _p, _p]),
+    "layer_norm": (_int, [_struct, _p, _p, _p, _p]),
+    "layer_norm_scratch_bytes": (_int, [_struct, ctypes.POINTER(_sz)]),
+    "layer_norm_backward": (_int, [_struct, _p, _i64, _i64, _p, _i64, _i64] + [_p] * 5
+                            + [_sz, _p]),
     "logits_process": (_int, [_struct, _p, _i64, _p]),
     "logits_probs": (_int, [_struct, _p, _p, _sz, _p]),
     "logits_scratch_bytes": (_int, [_struct, ctypes.POINTER(_sz)]),

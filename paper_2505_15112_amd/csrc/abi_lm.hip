@@ -133,6 +133,47 @@ int check_logits(const libscan_logits* p) {
     return LIBSCAN_OK;
 }
 
+int check_attend(const libscan_attend* p) {
+    if (!p || !known(p->type)) return LIBSCAN_EINVAL;
+    if (p->dk < 1 || p->dv < 1 || p->heads < 0 || p->groups < 1) return LIBSCAN_EINVAL;
+    if (p->dk > 256 || p->dv > 256 || p->heads > (1 << 16)) return LIBSCAN_ERANGE;
+    const int r = check_sizes(p->batch, p->steps, p->heads * (p->dk > p->dv ? p->dk : p->dv));
+    if (r != LIBSCAN_OK) return r;
+    if (p->heads % p->groups) return LIBSCAN_EINVAL;
+    // workgroups of at least 16 columns of a row's head, of 256 shared gradients
+    if ((__int128)p->batch * p->heads * 16 >= kMaxBlocks ||
+        (__int128)p->batch * p->steps * p->groups * p->dk / 256 >= kMaxBlocks)
+        return LIBSCAN_ERANGE;
+    return LIBSCAN_OK;
+}
+
+// The spans of the attention's inputs; false if one that is needed is missing.
+constexpr int kAttendInputs = 6;
+bool attend_inputs(const libscan_attend* p, Span (&in)[kAttendInputs]) {
+    const int64_t es = elem(p->type), b = p->batch, t = p->steps, h = p->heads, g = p->groups;
+    if (b * t * h && (!p->q || !p->k || !p->v || !p->log_decay)) return false;
+    in[0] = strided(p->q, es, b, p->q_batch, t, p->q_step, g, p->q_head, p->dk);
+    in[1] = strided(p->k, es, b, p->k_batch, t, p->k_step, g, p->k_head, p->dk);
+    in[2] = strided(p->v, es, b, p->v_batch, t, p->v_step, h, p->v_head, p->dv);
+    in[3] = p->fixed ? dense(p->log_decay, h, 4)
+                     : strided(p->log_decay, 4, b, p->decay_batch, t, p->decay_step, 1, 0, h);
+    in[4] = dense(p->state, b * h * p->dk * p->dv, 4);
+    in[5] = dense(p->lengths, b, 4);
+    return true;
+}
+
+int check_norm(const libscan_norm* p) {
+    if (!p || !known(p->type)) return LIBSCAN_EINVAL;
+    if (p->weight_type != p->type && p->weight_type != LIBSCAN_F32) return LIBSCAN_EINVAL;
+    if (p->groups < 1 || !(p->eps >= 0.0)) return LIBSCAN_EINVAL;
+    const int r = check_sizes(p->batch, p->steps, p->dim);
+    if (r != LIBSCAN_OK) return r;
+    if (p->dim % p->groups) return LIBSCAN_EINVAL;
+    // a workgroup to a row's group at most
+    if ((__int128)p->batch * p->steps * p->groups >= kMaxBlocks) return LIBSCAN_ERANGE;
+    return LIBSCAN_OK;
+}
+
 constexpr int kLogitsInputs = 11;
 bool logits_inputs(const libscan_logits* p, Span (&in)[kLogitsInputs]) {
     const int64_t r = p->rows, v = p->vocab;
@@ -298,6 +339,127 @@ int selective_scan_step(const libscan_ssm* p, float* states, int64_t n_states,
                         dense(states, n_states * p->dim * p->n, 4)};
     if (!sound(in, out)) return LIBSCAN_EINVAL;
     return hip_status(ls::launch_ssm_step(*p, states, n_states, slots, y, (hipStream_t)stream));
+}
+
+int linear_attention_bytes(const libscan_attend* p, size_t* scratch, size_t* backward_scratch) {
+    const int r = check_attend(p);
+    if (r != LIBSCAN_OK) return r;
+    if (scratch) *scratch = ls::attend_scratch_bytes(*p);
+    if (backward_scratch) *backward_scratch = ls::attend_back_scratch_bytes(*p);
+    return LIBSCAN_OK;
+}
+
+int linear_attention(const libscan_attend* p, void* y, float* state_out, void* scratch,
+                     size_t scratch_bytes, void* stream) {
+    const int r = check_attend(p);
+    if (r != LIBSCAN_OK) return r;
+    const int64_t values = p->batch * p->steps * p->heads * p->dv;
+    Span in[kAttendInputs];
+    if (!attend_inputs(p, in) || (values && !y)) return LIBSCAN_EINVAL;
+    const size_t need = ls::attend_scratch_bytes(*p);
+    const Span out[] = {dense(y, values, elem(p->type)),
+                        dense(state_out, p->batch * p->heads * p->dk * p->dv, 4),
+                        dense(scratch, (int64_t)need, 1)};
+    if (!sound(in, out)) return LIBSCAN_EINVAL;
+    const int s = check_scratch(scratch, scratch_bytes, need);
+    if (s != LIBSCAN_OK) return s;
+    return hip_status(ls::launch_attend(*p, y, state_out, scratch, (hipStream_t)stream));
+}
+
+int linear_attention_backward(const libscan_attend* p, const void* dy, int64_t dy_batch,
+                              int64_t dy_step, int64_t dy_head, const float* dstate_out, void* dq,
+                              void* dk, void* dv, float* dlog_decay, float* dstate, void* scratch,
+                              size_t scratch_bytes, void* stream) {
+    const int r = check_attend(p);
+    if (r != LIBSCAN_OK) return r;
+    const int64_t es = elem(p->type), b = p->batch, t = p->steps, h = p->heads;
+    const int64_t states = b * h * p->dk * p->dv, shared = b * t * p->groups * p->dk;
+    Span in[kAttendInputs + 2];
+    Span(&first)[kAttendInputs] = (Span(&)[kAttendInputs])in;
+    if (!attend_inputs(p, first)) return LIBSCAN_EINVAL;
+    if (b * t * h && (!dy || !dq || !dk || !dv)) return LIBSCAN_EINVAL;
+    if ((p->fixed ? h : b * t * h) && !dlog_decay) return LIBSCAN_EINVAL;
+    const size_t need = ls::attend_back_scratch_bytes(*p);
+    in[kAttendInputs] = strided(dy, es, b, dy_batch, t, dy_step, h, dy_head, p->dv);
+    in[kAttendInputs + 1] = dense(dstate_out, states, 4);
+    const Span out[] = {dense(dq, shared, es), dense(dk, shared, es),
+                        dense(dv, b * t * h * p->dv, es),
+                        dense(dlog_decay, p->fixed ? h : b * t * h, 4), dense(dstate, states, 4),
+                        dense(scratch, (int64_t)need, 1)};
+    if (!sound(in, out)) return LIBSCAN_EINVAL;
+    const int s = check_scratch(scratch, scratch_bytes, need);
+    if (s != LIBSCAN_OK) return s;
+    return hip_status(ls::launch_attend_back(*p, dy, dy_batch, dy_step, dy_head, dstate_out, dq, dk,
+                                             dv, dlog_decay, dstate, scratch,
+                                             (hipStream_t)stream));
+}
+
+int linear_attention_step(const libscan_attend* p, float* states, int64_t n_states,
+                          const int32_t* slots, void* y, void* stream) {
+    const int r = check_attend(p);
+    if (r != LIBSCAN_OK) return r;
+    if (p->steps != 1 || p->state || p->lengths || n_states < 0) return LIBSCAN_EINVAL;
+    if (p->batch == 0 || p->heads == 0) return LIBSCAN_OK;
+    Span in[kAttendInputs];
+    if (!attend_inputs(p, in) || !y || (n_states && !states)) return LIBSCAN_EINVAL;
+    const int64_t each = p->heads * p->dk * p->dv;
+    if (n_states > kMaxSpan / (each * 4)) return LIBSCAN_ERANGE;
+    in[4] = dense(slots, p->batch, 4);
+    const Span out[] = {dense(y, p->batch * p->heads * p->dv, elem(p->type)),
+                        dense(states, n_states * each, 4)};
+    if (!sound(in, out)) return LIBSCAN_EINVAL;
+    return hip_status(ls::launch_attend_step(*p, states, n_states, slots, y, (hipStream_t)stream));
+}
+
+int layer_norm(const libscan_norm* p, void* y, void* sum, float* stats, void* stream) {
+    const int r = check_norm(p);
+    if (r != LIBSCAN_OK) return r;
+    const int64_t es = elem(p->type), ws = elem(p->weight_type), rows = p->batch * p->steps;
+    if (rows * p->dim && (!p->x || !y)) return LIBSCAN_EINVAL;
+    const Span in[] = {strided(p->x, es, p->batch, p->x_batch, p->steps, p->x_step, 1, 0, p->dim),
+                       p->residual ? strided(p->residual, es, p->batch, p->residual_batch, p->steps,
+                                             p->residual_step, 1, 0, p->dim)
+                                   : Span{nullptr, 0},
+                       dense(p->weight, p->dim, ws), dense(p->bias, p->dim, ws)};
+    const Span out[] = {dense(y, rows * p->dim, es), dense(sum, rows * p->dim, es),
+                        dense(stats, rows * p->groups * 2, 4)};
+    if (!sound(in, out)) return LIBSCAN_EINVAL;
+    return hip_status(ls::launch_norm(*p, y, sum, stats, (hipStream_t)stream));
+}
+
+int layer_norm_scratch_bytes(const libscan_norm* p, size_t* bytes) {
+    const int r = check_norm(p);
+    if (r != LIBSCAN_OK) return r;
+    if (!bytes) return LIBSCAN_EINVAL;
+    *bytes = ls::norm_scratch_bytes(*p);
+    return LIBSCAN_OK;
+}
+
+int layer_norm_backward(const libscan_norm* p, const void* dy, int64_t dy_batch, int64_t dy_step,
+                        const void* dsum, int64_t dsum_batch, int64_t dsum_step,
+                        const float* stats, void* dx, float* dweight, float* dbias, void* scratch,
+                        size_t scratch_bytes, void* stream) {
+    const int r = check_norm(p);
+    if (r != LIBSCAN_OK) return r;
+    if (p->residual) return LIBSCAN_EINVAL;
+    const int64_t es = elem(p->type), ws = elem(p->weight_type), rows = p->batch * p->steps;
+    if (rows * p->dim && (!p->x || !dy || !stats || !dx)) return LIBSCAN_EINVAL;
+    const size_t need = ls::norm_scratch_bytes(*p);
+    const Span in[] = {strided(p->x, es, p->batch, p->x_batch, p->steps, p->x_step, 1, 0, p->dim),
+                       strided(dy, es, p->batch, dy_batch, p->steps, dy_step, 1, 0, p->dim),
+                       dsum ? strided(dsum, es, p->batch, dsum_batch, p->steps, dsum_step, 1, 0,
+                                      p->dim)
+                            : Span{nullptr, 0},
+                       dense(p->weight, p->dim, ws), dense(p->bias, p->dim, ws),
+                       dense(stats, rows * p->groups * 2, 4)};
+    const Span out[] = {dense(dx, rows * p->dim, es), dense(dweight, p->dim, 4),
+                        dense(dbias, p->dim, 4), dense(scratch, (int64_t)need, 1)};
+    if (!sound(in, out)) return LIBSCAN_EINVAL;
+    const int s = check_scratch(scratch, scratch_bytes, need);
+    if (s != LIBSCAN_OK) return s;
+    return hip_status(ls::launch_norm_back(*p, dy, dy_batch, dy_step, dsum, dsum_batch, dsum_step,
+                                           stats, dx, dweight, dbias, scratch,
+                                           (hipStream_t)stream));
 }
 
 int logits_process(const libscan_logits* p, void* out, int64_t out_row, void* stream) {

@@ -1,0 +1,66 @@
+// attend.hpp -- linear attention as one operator used four times.
+//
+// With D[i,j] = e^(g[j+1] + .. + g[i]) for j <= i, the output is
+//   o[i] = sum over j <= i of D[i,j] (q[i] . k[j]) v[j],
+// which a state S[i] = e^g[i] S[i-1] + k[i] v[i]^T carries: o[i] = q[i] S[i].
+// Its gradients are the same sum with the operands in other places: dq = (do,
+// v, k); and backwards in time, where step j decays by the next token's g,
+// dk = (v, do, q) and dv = (k, q, do).  A Walk is one of them.
+#pragma once
+
+#include "../../include/libscan.h"
+#include "lm.hpp"
+
+namespace ls {
+
+// An operand of batch x steps x some heads x width: head h of the walk reads
+// head h / share of it.
+struct WalkSide {
+    const void* p;
+    int64_t batch, step, head;
+    int share;
+};
+
+// States of every row and head, element (r, c) of number i at p[i * dk * dv + r * row +
+// c * col].
+struct WalkState {
+    float* p;
+    int64_t row, col;
+};
+
+struct Walk {
+    int batch, steps, heads, dk, dv;
+    bool reverse;
+    WalkSide q, k, v;  // q and k of width dk, v of dv
+    const float* g;    // log decays, [batch, step, head]
+    int64_t g_batch, g_step;
+    float inner, outer;  // factors of k v^T, and of the output
+    WalkState first, last;  // nullable
+    const int32_t* lengths;
+    // Output: batch x steps x heads x dv, dense; fp32 where `wide`.  With `dots`
+    // (batch x steps x heads for each block of columns), the sums of the output
+    // times e, before it is rounded.
+    void* out;
+    bool wide;
+    WalkSide e;
+    float* dots;
+};
+
+__device__ __forceinline__ int walk_len(const Walk& w, int b) {
+    if (!w.lengths) return w.steps;
+    const int n = w.lengths[b];
+    return n < 0 ? 0 : n < w.steps ? n : w.steps;
+}
+
+// The token at a place of the walk, and that place's decay.  Places at and behind
+// `len` are the tokens there, whose outputs are 0.
+__device__ __forceinline__ int walk_token(const Walk& w, int place, int len) {
+    return w.reverse && place < len ? len - 1 - place : place;
+}
+__device__ __forceinline__ float walk_decay(const Walk& w, int b, int h, int place, int len) {
+    if (place >= len || (w.reverse && place == 0)) return 0.0f;
+    const int t = w.reverse ? len - place : place;
+    return w.g[b * w.g_batch + t * w.g_step + h];
+}
+
+}  // namespace ls

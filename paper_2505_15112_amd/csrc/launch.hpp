@@ -132,6 +132,25 @@ hipError_t launch_ssm_back(const libscan_ssm& p, const void* dy, int64_t dy_batc
                            float* dA, void* dB, void* dC, float* dD, void* dz, float* ddt_bias,
                            float* dstate, void* scratch, hipStream_t stream);
 
+size_t attend_scratch_bytes(const libscan_attend& p);
+size_t attend_back_scratch_bytes(const libscan_attend& p);
+hipError_t launch_attend(const libscan_attend& p, void* y, float* state_out, void* scratch,
+                         hipStream_t stream);
+hipError_t launch_attend_back(const libscan_attend& p, const void* dy, int64_t dy_batch,
+                              int64_t dy_step, int64_t dy_head, const float* dstate_out, void* dq,
+                              void* dk, void* dv, float* dlog_decay, float* dstate, void* scratch,
+                              hipStream_t stream);
+hipError_t launch_attend_step(const libscan_attend& p, float* states, int64_t n_states,
+                              const int32_t* slots, void* y, hipStream_t stream);
+
+hipError_t launch_norm(const libscan_norm& p, void* y, void* sum, float* stats,
+                       hipStream_t stream);
+size_t norm_scratch_bytes(const libscan_norm& p);
+hipError_t launch_norm_back(const libscan_norm& p, const void* dy, int64_t dy_batch,
+                            int64_t dy_step, const void* dsum, int64_t dsum_batch,
+                            int64_t dsum_step, const float* stats, void* dx, float* dweight,
+                            float* dbias, void* scratch, hipStream_t stream);
+
 bool logits_fit(const libscan_logits& p);  // one launch holds the rows' segments
 size_t logits_scratch(const libscan_logits& p);
 hipError_t launch_logits_process(const libscan_logits& p, void* out, int64_t out_row,

@@ -13,6 +13,7 @@
 #include <c10/core/GradMode.h>
 #include <torch/csrc/autograd/python_variable.h>
 
+#include <cmath>
 #include <sstream>
 
 #include "../../include/libscan.h"
@@ -204,6 +205,106 @@ PyObject* ssm(PyObject* const* a) {
     return packed(p);
 }
 
+double real(PyObject* o) {
+    const double v = PyFloat_AsDouble(o);
+    if (v == -1.0 && PyErr_Occurred()) throw Raised();
+    return v;
+}
+
+// (q, k, v, log_decay, state, lengths, scale, step): a libscan_attend
+PyObject* attend(PyObject* const* a) {
+    libscan_attend p{};
+    const bool step = truth(a[7]);
+    const at::Tensor& q = first(a[0], "q", step ? 3 : 4, p.type);
+    const at::ScalarType kind = q.scalar_type();
+    const at::Tensor& v = tensor(a[2], "v", step ? 3 : 4,
+                                 step ? " (batch x heads x dv)" : " (batch x steps x heads x dv)");
+    p.batch = q.size(0);
+    p.steps = step ? 1 : q.size(1);
+    p.groups = q.size(-2);
+    p.dk = q.size(-1);
+    p.heads = v.size(-2);
+    p.dv = v.size(-1);
+    if (p.groups < 1 || p.heads % p.groups)
+        raise(PyExc_ValueError, "v: expected heads in equal groups over the ", p.groups,
+              " of q and k, got ", p.heads);
+    const int64_t v4[] = {p.batch, p.steps, p.heads, p.dv}, v3[] = {p.batch, p.heads, p.dv};
+    const int64_t each[] = {p.batch, p.steps, p.heads};
+    const at::Tensor& k = operand(a[1], "k", kind, q.sizes(), q, false);
+    p.q = operand(a[0], "q", kind, q.sizes(), q, false).data_ptr();
+    p.q_batch = q.stride(0);
+    p.q_step = step ? 0 : q.stride(1);
+    p.q_head = q.stride(-2);
+    p.k = k.data_ptr();
+    p.k_batch = k.stride(0);
+    p.k_step = step ? 0 : k.stride(1);
+    p.k_head = k.stride(-2);
+    p.v = operand(a[2], "v", kind, step ? at::IntArrayRef(v3) : at::IntArrayRef(v4), q, false)
+              .data_ptr();
+    p.v_batch = v.stride(0);
+    p.v_step = step ? 0 : v.stride(1);
+    p.v_head = v.stride(-2);
+    const at::Tensor& g = tensor(a[3], "log_decay", -1, "");
+    p.fixed = g.dim() == 1;
+    if (p.fixed) {
+        p.log_decay = address<float>(a[3], "log_decay", at::kFloat, {p.heads}, q, true);
+    } else {
+        const int64_t rows[] = {p.batch, p.heads};
+        p.log_decay = address<float>(a[3], "log_decay", at::kFloat,
+                                     step ? at::IntArrayRef(rows) : at::IntArrayRef(each), q,
+                                     false);
+        p.decay_batch = g.stride(0);
+        p.decay_step = step ? 0 : g.stride(1);
+    }
+    p.state = address<float>(a[4], "state", at::kFloat, {p.batch, p.heads, p.dk, p.dv}, q, true);
+    p.lengths = address<int32_t>(a[5], "lengths", at::kInt, {p.batch}, q, true);
+    p.scale = a[6] == Py_None ? 1.0 / std::sqrt((double)p.dk) : real(a[6]);
+    no_graph(a, 6, step ? "a step has no gradients"
+                        : "linear_attention_backward forms the gradients");
+    return packed(p);
+}
+
+// (x, weight, bias, residual, groups, eps): a libscan_norm
+PyObject* norm(PyObject* const* a) {
+    libscan_norm p{};
+    const at::Tensor& any = tensor(a[0], "x", -1, "");
+    const at::Tensor& x = first(a[0], "x", any.dim() == 2 ? 2 : 3, p.type);
+    const at::ScalarType kind = x.scalar_type();
+    const bool rows = x.dim() == 2;
+    p.batch = rows ? 1 : x.size(0);
+    p.steps = x.size(-2);
+    p.dim = x.size(-1);
+    p.groups = PyLong_AsLongLong(a[4]);
+    if (PyErr_Occurred()) throw Raised();
+    if (p.groups < 1 || p.dim % p.groups)
+        raise(PyExc_ValueError, "groups: expected a divisor of ", p.dim, " channels, got ",
+              p.groups);
+    p.eps = real(a[5]);
+    p.x = operand(a[0], "x", kind, x.sizes(), x, false).data_ptr();
+    p.x_batch = rows ? 0 : x.stride(0);
+    p.x_step = x.stride(-2);
+    if (a[3] != Py_None) {
+        const at::Tensor& r = operand(a[3], "residual", kind, x.sizes(), x, false);
+        p.residual = r.data_ptr();
+        p.residual_batch = rows ? 0 : r.stride(0);
+        p.residual_step = r.stride(-2);
+    }
+    at::ScalarType weights = kind;
+    for (int i = 1; i < 3; ++i) {
+        if (a[i] == Py_None) continue;
+        const char* name = i == 1 ? "weight" : "bias";
+        const at::Tensor& w = tensor(a[i], name, 1, "");
+        if (i == 1 || a[1] == Py_None) weights = w.scalar_type();
+        if (weights != kind && weights != at::kFloat)
+            raise(PyExc_TypeError, name, ": expected ", text(kind), " or torch.float32, got ",
+                  text(weights));
+        (i == 1 ? p.weight : p.bias) = operand(a[i], name, weights, {p.dim}, x, true).data_ptr();
+    }
+    p.weight_type = weights == kind ? p.type : LIBSCAN_F32;
+    no_graph(a, 4, "layer_norm_backward forms the gradients");
+    return packed(p);
+}
+
 // (logits, history, history_len, prompt_len, repetition, presence, frequency,
 // bias_ids, bias_values, allowed, temperature): a libscan_logits
 PyObject* logits(PyObject* const* a) {
@@ -292,6 +393,8 @@ PyObject* sizes(PyObject* const* a) {
     int status;
     if (n == 1)
         status = ((int (*)(const void*, size_t*))fn)(p, v);
+    else if (n == 2)
+        status = ((int (*)(const void*, size_t*, size_t*))fn)(p, v, v + 1);
     else
         status = ((int (*)(const void*, size_t*, size_t*, size_t*))fn)(p, v, v + 1, v + 2);
     PyObject* out = PyTuple_New(1 + n);
@@ -327,6 +430,7 @@ PyObject* entry(PyObject*, PyObject* const* args, Py_ssize_t n) {
 
 #define ENTRY(f, n) {#f, (PyCFunction)(void (*)(void))entry<f, n>, METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {ENTRY(conv, 7),  ENTRY(ssm, 12),  ENTRY(logits, 11),
+                         ENTRY(attend, 8), ENTRY(norm, 6),
                          ENTRY(dense, 5), ENTRY(empty, 2), ENTRY(sizes, 3),
                          ENTRY(memory, 2), ENTRY(floats, 2), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_torch_args", nullptr, -1, methods,

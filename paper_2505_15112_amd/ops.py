@@ -453,8 +453,8 @@ def topk_rows_f32(x, k, largest=True, values_out=None, idx_out=None, ws=None, sc
 # *_backward is what training takes (examples/state_space_lm.py has one for each).
 
 class _Args:
-    """The compiled checks of torch_args.cpp, loaded at the first use: conv, ssm and
-    logits check an operator's tensors and return its struct's bytes."""
+    """The compiled checks of torch_args.cpp, loaded at the first use: conv, ssm, attend,
+    norm and logits check an operator's tensors and return its struct's bytes."""
 
     def __getattr__(self, name):
         path = os.path.join(_lib.PKG, "_torch_args.so")
@@ -463,7 +463,7 @@ class _Args:
         spec = importlib.util.spec_from_file_location("_torch_args", path)
         module = importlib.util.module_from_spec(spec)
         spec.loader.exec_module(module)
-        names = ("conv", "ssm", "logits", "dense", "empty", "sizes", "memory", "floats")
+        names = ("conv", "ssm", "attend", "norm", "logits", "dense", "empty", "sizes", "memory", "floats")
         self.__dict__.update({k: getattr(module, k) for k in names})
         return self.__dict__[name]
 
@@ -642,6 +642,106 @@ def selective_scan_step(x, dt, states, A, B, C, D=None, z=None, dt_bias=None, sl
     y = _into(out, x)
     _launch("selective_scan_step", x, p, *pool, _ptr(y))
     return y
+
+
+def linear_attention(q, k, v, log_decay, state=None, lengths=None, scale=None, with_state=False,
+                     out=None, state_out=None, scratch_buf=None):
+    """Linear attention with a decay for each head: S[t] = exp(log_decay) S[t-1] +
+    k v^T, y = scale q S (scale: dk ** -0.5 by default).  q, k: batch x steps x groups
+    x dk; v: batch x steps x heads x dv, heads a multiple of groups; log_decay: fp32,
+    batch x steps x heads, or heads: one for all tokens; state: batch x heads x dk x dv
+    fp32.  Returns (y, state_out): the last state when with_state (or state_out is
+    given), else None."""
+    p = _args.attend(q, k, v, log_decay, state, lengths, scale, False)
+    y = _into(out, v)
+    if with_state or state_out is not None:
+        state_out = _into(state_out, v, (v.shape[0], v.shape[2], q.shape[3], v.shape[3]), True,
+                          "state_out")
+    need, _ = _sizes("linear_attention_bytes", p, 2)
+    buf = _scratch_for(scratch_buf, need, v) if need else None
+    _launch("linear_attention", q, p, _ptr(y), _ptr(state_out), _ptr(buf),
+            buf.numel() if buf is not None else 0)
+    return y, state_out
+
+
+def linear_attention_backward(dy, q, k, v, log_decay, state=None, lengths=None, scale=None,
+                              dstate_out=None, with_dstate=None, scratch_buf=None):
+    """Gradients of linear_attention from those of its outputs (dy, and dstate_out of
+    its last state).  Returns (dq, dk, dv, dlog_decay fp32, dstate fp32 or None: by
+    default formed when there is a state)."""
+    p = _args.attend(q, k, v, log_decay, state, lengths, scale, False)
+    shape = (v.shape[0], v.shape[2], q.shape[3], v.shape[3])
+    pdy = _strided(dy, "dy", v)
+    pso = _args.dense(dstate_out, "dstate_out", v, shape, True)
+    if with_dstate is None:
+        with_dstate = state is not None
+    new = _args.empty
+    dq, dk, dv, dg = new(q, False), new(k, False), new(v, False), new(log_decay, True)
+    dstate = _into(None, v, shape, True) if with_dstate else None
+    _, need = _sizes("linear_attention_bytes", p, 2)
+    buf = _scratch_for(scratch_buf, need, v)
+    _launch("linear_attention_backward", q, p, pdy, *dy.stride()[:3], pso, _ptr(dq), _ptr(dk),
+            _ptr(dv), _ptr(dg), _ptr(dstate), _ptr(buf), buf.numel())
+    return dq, dk, dv, dg, dstate
+
+
+def linear_attention_step(q, k, v, log_decay, states, slots=None, scale=None, out=None):
+    """One token of every row: q, k: batch x groups x dk; v: batch x heads x dv;
+    log_decay: batch x heads, or heads; states a pool of heads x dk x dv fp32 states (row
+    b's is number slots[b], or b), which move on in place.  Returns y, batch x heads x dv."""
+    p = _args.attend(q, k, v, log_decay, None, None, scale, True)
+    pool = _pool(states, v, (v.shape[1], q.shape[2], v.shape[2]), True, slots)
+    y = _into(out, v)
+    _launch("linear_attention_step", q, p, *pool, _ptr(y))
+    return y
+
+
+def layer_norm(x, weight=None, bias=None, residual=None, groups=1, eps=1e-5, with_stats=False,
+               out=None, sum_out=None, stats_out=None):
+    """Layer norm over each of `groups` groups of neighbouring channels: x is batch x
+    steps x dim or rows x dim, weight and bias dim.  With a residual of x's shape,
+    what is normalised is x + residual, rounded to x's type.  Returns (y, that sum or
+    None, stats or None): the groups' means and 1 / sqrt(variance + eps), fp32, for
+    layer_norm_backward, when with_stats (or stats_out is given)."""
+    p = _args.norm(x, weight, bias, residual, groups, eps)
+    y = _into(out, x)
+    if residual is not None:
+        sum_out = _into(sum_out, x, name="sum_out")
+    elif sum_out is not None:
+        raise ValueError("sum_out: there is no residual")
+    if with_stats or stats_out is not None:
+        stats_out = _into(stats_out, x, (*x.shape[:-1], groups, 2), True, "stats_out")
+    _launch("layer_norm", x, p, _ptr(y), _ptr(sum_out), _ptr(stats_out))
+    return y, sum_out, stats_out
+
+
+def layer_norm_backward(dy, x, stats, weight=None, bias=None, dsum=None, groups=1,
+                        scratch_buf=None):
+    """Gradients of layer_norm from those of its outputs (dy, and dsum of the sum with the
+    residual), with x what it normalised (that sum, if there was a residual) and its
+    stats.  Returns (dx, which is the residual's too, dweight fp32 or None, dbias fp32
+    or None)."""
+    p = _args.norm(x, weight, bias, None, groups, 0.0)
+    pdy = _strided(dy, "dy", x)
+    more = (None, 0, 0)
+    if dsum is not None:
+        more = (_strided(dsum, "dsum", x), *_row_strides(dsum))
+    ps = _args.dense(stats, "stats", x, (*x.shape[:-1], groups, 2), True)
+    if stats is None:
+        raise TypeError("stats: expected a torch.Tensor")
+    dx = _args.empty(x, False)
+    dweight = _args.empty(weight, True) if weight is not None else None
+    dbias = _args.empty(bias, True) if bias is not None else None
+    need = _sizes("layer_norm_scratch_bytes", p, 1)[0]
+    buf = _scratch_for(scratch_buf, need, x)
+    _launch("layer_norm_backward", x, p, pdy, *_row_strides(dy), *more, ps, _ptr(dx),
+            _ptr(dweight), _ptr(dbias), _ptr(buf), buf.numel())
+    return dx, dweight, dbias
+
+
+def _row_strides(t):
+    """The strides over batch and steps of batch x steps x dim, or rows x dim."""
+    return t.stride()[:2] if t.dim() == 3 else (0, t.stride(0))
 
 
 def logits_process(logits, history=None, history_len=None, prompt_len=None, repetition=None,
