@@ -6,56 +6,7 @@
 namespace ls {
 namespace {
 
-constexpr int kCols = 64;  // columns of a workgroup
-
-// One wave for 64 columns of a head's state, which it holds in LDS; token by token.
-template <class T>
-__global__ void __launch_bounds__(kCols) k_walk(Walk w) {
-    extern __shared__ float s_state[];  // dk x 64
-    const int blocks = (w.dv + kCols - 1) / kCols;
-    const int block = blockIdx.x % blocks, bh = blockIdx.x / blocks;
-    const int h = bh % w.heads, b = bh / w.heads;
-    const int lane = threadIdx.x, c = block * kCols + lane;
-    const bool on = c < w.dv;
-    const int len = walk_len(w, b);
-    const int64_t state = (int64_t)bh * w.dk * w.dv;
-    for (int r = 0; r < w.dk; ++r)
-        s_state[r * kCols + lane] =
-            on && w.first.p ? w.first.p[state + r * w.first.row + c * w.first.col] : 0.0f;
-    const auto side = [&](const WalkSide& s, int t) {
-        return (const T*)s.p + b * s.batch + t * s.step + (h / s.share) * s.head;
-    };
-    for (int i = 0; i < w.steps; ++i) {
-        const int t = walk_token(w, i, len);
-        const int64_t at = ((int64_t)b * w.steps + t) * w.heads + h;
-        float o = 0.0f, e = 0.0f;
-        if (i < len) {
-            const T *q = side(w.q, t), *k = side(w.k, t);
-            const float a = exp2_fast(walk_decay(w, b, h, i, len) * kLog2e);
-            const float v = on ? to_f32(side(w.v, t)[c]) : 0.0f;
-            for (int r = 0; r < w.dk; ++r) {
-                const float x = __builtin_fmaf(to_f32(k[r]) * w.inner, v, a * s_state[r * kCols + lane]);
-                s_state[r * kCols + lane] = x;
-                o = __builtin_fmaf(to_f32(q[r]), x, o);
-            }
-            o *= w.outer;
-            if (w.dots && on) e = o * to_f32(side(w.e, t)[c]);
-        }
-        if (w.dots) {
-#pragma unroll
-            for (int m = 32; m > 0; m >>= 1) e += __shfl_xor(e, m);
-            if (lane == 0) w.dots[(int64_t)block * w.batch * w.steps * w.heads + at] = e;
-        }
-        if (!on) continue;
-        if (w.wide)
-            ((float*)w.out)[at * w.dv + c] = o;
-        else
-            ((T*)w.out)[at * w.dv + c] = from_f32<T>(o);
-    }
-    if (w.last.p && on)
-        for (int r = 0; r < w.dk; ++r)
-            w.last.p[state + r * w.last.row + c * w.last.col] = s_state[r * kCols + lane];
-}
+constexpr int kCols = 64;  // columns of a step's workgroup
 
 // Gradients by head, batch x steps x heads x width fp32, to those of the groups.
 template <class T>
@@ -176,18 +127,10 @@ __global__ void __launch_bounds__(kCols)
 
 // ------------------------------------------------ launches
 
-template <class T>
-hipError_t run(const Walk& w, hipStream_t stream) {
-    const int64_t grid = (int64_t)w.batch * w.heads * ((w.dv + kCols - 1) / kCols);
-    if (grid == 0) return hipSuccess;
-    const size_t lds = (size_t)w.dk * kCols * sizeof(float);
-    k_walk<T><<<(uint32_t)grid, kCols, lds, stream>>>(w);
-    return hipGetLastError();
-}
-
-hipError_t run(int64_t type, const Walk& w, hipStream_t stream) {
-    return type == LIBSCAN_F32 ? run<float>(w, stream)
-         : type == LIBSCAN_F16 ? run<_Float16>(w, stream) : run<__bf16>(w, stream);
+hipError_t run(int64_t type, const Walk& w, Grade grade, bool states, hipStream_t stream) {
+    return type == LIBSCAN_F32   ? launch_walk<float>(w, grade, states, stream)
+           : type == LIBSCAN_F16 ? launch_walk<_Float16>(w, grade, states, stream)
+                                 : launch_walk<__bf16>(w, grade, states, stream);
 }
 
 // What all walks of a call have in common.
@@ -198,6 +141,7 @@ Walk base(const libscan_attend& p) {
     w.g_batch = p.fixed ? 0 : p.decay_batch;
     w.g_step = p.fixed ? 0 : p.decay_step;
     w.lengths = p.lengths;
+    w.pieces = 1, w.piece = w.steps;
     w.inner = w.outer = 1.0f;
     return w;
 }
@@ -208,8 +152,6 @@ WalkSide side_k(const libscan_attend& p) {
     return {p.k, p.k_batch, p.k_step, p.k_head, (int)(p.heads / p.groups)};
 }
 WalkSide side_v(const libscan_attend& p) { return {p.v, p.v_batch, p.v_step, p.v_head, 1}; }
-
-int64_t blocks(int64_t columns) { return (columns + kCols - 1) / kCols; }
 
 // Scratch of the gradients, in bytes from its start.
 struct BackPlan {
@@ -224,8 +166,8 @@ BackPlan back_plan(const libscan_attend& p) {
         at += (floats * 4 + 255) / 256 * 256;
         return here;
     };
-    r.dq_dots = take(tokens * blocks(p.dk));
-    r.dk_dots = take(tokens * blocks(p.dk));
+    r.dq_dots = take(tokens * walk_blocks((int)p.dv, (int)p.dk));
+    r.dk_dots = take(tokens * walk_blocks((int)p.dv, (int)p.dk));
     r.gates = take(p.fixed ? tokens : 0);
     r.last = take(p.batch * p.heads * p.dk * p.dv);
     r.dq = take(p.groups < p.heads ? tokens * p.dk : 0);
@@ -248,7 +190,7 @@ hipError_t launch_attend(const libscan_attend& p, void* y, float* state_out, voi
     w.first = {const_cast<float*>(p.state), p.dv, 1};
     w.last = {state_out, p.dv, 1};
     w.out = y;
-    return run(p.type, w, stream);
+    return run(p.type, w, Grade::Narrow, false, stream);
 }
 
 hipError_t launch_attend_back(const libscan_attend& p, const void* dy, int64_t dy_batch,
@@ -273,7 +215,7 @@ hipError_t launch_attend_back(const libscan_attend& p, const void* dy, int64_t d
     w.wide = shared;
     w.e = side_q(p);
     w.dots = floats(plan.dq_dots);
-    if ((e = run(p.type, w, stream)) != hipSuccess) return e;
+    if ((e = run(p.type, w, Grade::Wide, false, stream)) != hipSuccess) return e;
 
     w.reverse = true;  // dk
     w.q = side_v(p), w.k = side_dy, w.v = side_q(p);
@@ -283,7 +225,7 @@ hipError_t launch_attend_back(const libscan_attend& p, const void* dy, int64_t d
     w.out = shared ? floats(plan.dk) : dk;
     w.e = side_k(p);
     w.dots = floats(plan.dk_dots);
-    if ((e = run(p.type, w, stream)) != hipSuccess) return e;
+    if ((e = run(p.type, w, Grade::Wide, false, stream)) != hipSuccess) return e;
 
     w = base(p);  // dv
     w.reverse = true;
@@ -293,12 +235,12 @@ hipError_t launch_attend_back(const libscan_attend& p, const void* dy, int64_t d
     w.first = {const_cast<float*>(dstate_out), p.dv, 1};
     w.last = {dstate, p.dv, 1};
     w.out = dv;
-    if ((e = run(p.type, w, stream)) != hipSuccess) return e;
+    if ((e = run(p.type, w, Grade::Narrow, false, stream)) != hipSuccess) return e;
 
     const uint32_t rows = (uint32_t)(p.batch * p.heads);
     if (rows) {
         k_gates<<<rows, kGateThreads, 0, stream>>>(
-            w, floats(plan.dq_dots), (int)blocks(p.dk), floats(plan.dk_dots), (int)blocks(p.dk),
+            w, floats(plan.dq_dots), walk_blocks((int)p.dv, (int)p.dk), floats(plan.dk_dots), walk_blocks((int)p.dv, (int)p.dk),
             dstate_out, floats(plan.last), state, p.fixed ? floats(plan.gates) : dlog_decay);
         if (dstate) k_first_decay<<<rows, 256, 0, stream>>>(w, dstate, state);
     }
@@ -323,7 +265,7 @@ hipError_t launch_attend_back(const libscan_attend& p, const void* dy, int64_t d
 
 hipError_t launch_attend_step(const libscan_attend& p, float* states, int64_t n_states,
                               const int32_t* slots, void* y, hipStream_t stream) {
-    const uint32_t grid = (uint32_t)(p.batch * p.heads * blocks(p.dv));
+    const uint32_t grid = (uint32_t)(p.batch * p.heads * ((p.dv + kCols - 1) / kCols));
     if (p.type == LIBSCAN_F32)
         k_attend_step<float><<<grid, kCols, 0, stream>>>(p, states, n_states, slots, (float*)y);
     else if (p.type == LIBSCAN_F16)

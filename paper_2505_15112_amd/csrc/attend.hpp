@@ -21,8 +21,7 @@ struct WalkSide {
     int share;
 };
 
-// States of every row and head, element (r, c) of number i at p[i * dk * dv + r * row +
-// c * col].
+// States, dk x dv each: element (r, c) of number i at p[i * dk * dv + r * row + c * col].
 struct WalkState {
     float* p;
     int64_t row, col;
@@ -35,8 +34,15 @@ struct Walk {
     const float* g;    // log decays, [batch, step, head]
     int64_t g_batch, g_step;
     float inner, outer;  // factors of k v^T, and of the output
-    WalkState first, last;  // nullable
     const int32_t* lengths;
+    // Every row's steps are cut into `pieces` of `piece` places, a workgroup to each
+    // (and to a block of columns of v).
+    int pieces, piece;
+    // The states that the rows (pieces == 1: one for each row and head) or their pieces
+    // (one for each row, head and piece) begin with, nullable; and the last ones: the
+    // row's, if pieces == 1, or in a run for the states alone what each piece adds.
+    WalkState first, last;
+    float* whole;  // in such a run, for each row, head and piece: the product of its decays
     // Output: batch x steps x heads x dv, dense; fp32 where `wide`.  With `dots`
     // (batch x steps x heads for each block of columns), the sums of the output
     // times e, before it is rounded.
@@ -62,5 +68,23 @@ __device__ __forceinline__ float walk_decay(const Walk& w, int b, int h, int pla
     const int t = w.reverse ? len - place : place;
     return w.g[b * w.g_batch + t * w.g_step + h];
 }
+
+// How exact a walk is: the outputs to 16 bits, or to 32 (attend_walk.hpp).
+enum class Grade { Narrow, Wide };
+
+// Columns of v that a workgroup has.
+inline int walk_columns(int dk, int dv) { return dk <= 128 && dv > 64 ? 128 : 64; }
+inline int walk_blocks(int dk, int dv) {
+    const int columns = walk_columns(dk, dv);
+    return (dv + columns - 1) / columns;
+}
+
+// One instance for each element type (attend_f32.hip and so on).  `states`: what each
+// piece adds to the state and no outputs.
+template <class T>
+hipError_t launch_walk(const Walk& w, Grade grade, bool states, hipStream_t stream);
+extern template hipError_t launch_walk<float>(const Walk&, Grade, bool, hipStream_t);
+extern template hipError_t launch_walk<_Float16>(const Walk&, Grade, bool, hipStream_t);
+extern template hipError_t launch_walk<__bf16>(const Walk&, Grade, bool, hipStream_t);
 
 }  // namespace ls
