@@ -92,6 +92,25 @@ __global__ void __launch_bounds__(256) k_first_decay(Walk w, float* state, int64
     for (int64_t i = threadIdx.x; i < each; i += 256) state[blockIdx.x * each + i] *= a;
 }
 
+// The states before every piece from what each adds, in place: a workgroup to 256
+// elements of a row and head; piece i of element x is states[i * each + x].
+__global__ void __launch_bounds__(256)
+    k_carry(float* states, const float* whole, int pieces, int64_t each, const float* first,
+            float* last) {
+    const int64_t groups = (each + 255) / 256, bh = blockIdx.x / groups;
+    const int64_t x = blockIdx.x % groups * 256 + threadIdx.x;
+    if (x >= each) return;
+    float* at = states + bh * pieces * each + x;
+    float run = first ? first[bh * each + x] : 0.0f;
+#pragma unroll 8
+    for (int i = 0; i < pieces; ++i) {
+        const float more = at[i * each];
+        at[i * each] = run;
+        run = __builtin_fmaf(whole[bh * pieces + i], run, more);
+    }
+    if (last) last[bh * each + x] = run;
+}
+
 // ------------------------------------------------ a single token
 
 // A workgroup to 64 columns of a row's head.
@@ -153,33 +172,86 @@ WalkSide side_k(const libscan_attend& p) {
 }
 WalkSide side_v(const libscan_attend& p) { return {p.v, p.v_batch, p.v_step, p.v_head, 1}; }
 
-// Scratch of the gradients, in bytes from its start.
-struct BackPlan {
-    int64_t dq_dots, dk_dots, gates, last, dq, dk, bytes;
+// Rows are cut into pieces where they alone do not fill the GPU: a first run over k and
+// v gives what each piece adds to the state.
+struct Pieces {
+    int count, places;
 };
-BackPlan back_plan(const libscan_attend& p) {
-    BackPlan r{};
-    const int64_t tokens = p.batch * p.steps * p.heads;
+Pieces pieces(const libscan_attend& p) {
+    const int64_t chunk = 64, chunks = (p.steps + chunk - 1) / chunk;
+    const int64_t groups = p.batch * p.heads * walk_blocks((int)p.dk, (int)p.dv);
+    int64_t count = groups ? 512 / groups : 1;
+    if (count > chunks / 2) count = chunks / 2;
+    if (count < 2) return {1, (int)p.steps};
+    const int64_t each = (chunks + count - 1) / count;
+    return {(int)((chunks + each - 1) / each), (int)(each * chunk)};
+}
+
+// Scratch in bytes from its start.
+struct Room {
     int64_t at = 0;
-    const auto take = [&](int64_t floats) {
+    int64_t floats(int64_t n) {
         const int64_t here = at;
-        at += (floats * 4 + 255) / 256 * 256;
+        at += (n * 4 + 255) / 256 * 256;
         return here;
-    };
-    r.dq_dots = take(tokens * walk_blocks((int)p.dv, (int)p.dk));
-    r.dk_dots = take(tokens * walk_blocks((int)p.dv, (int)p.dk));
-    r.gates = take(p.fixed ? tokens : 0);
-    r.last = take(p.batch * p.heads * p.dk * p.dv);
-    r.dq = take(p.groups < p.heads ? tokens * p.dk : 0);
-    r.dk = take(p.groups < p.heads ? tokens * p.dk : 0);
-    r.bytes = at;
-    return r;
+    }
+};
+// What each piece adds to the states, and then the states before it.
+struct Cut {
+    int64_t states, whole;
+    Cut(const libscan_attend& p, Room& room) {
+        const int64_t n = pieces(p).count, all = n > 1 ? p.batch * p.heads * n : 0;
+        states = room.floats(all * p.dk * p.dv);
+        whole = room.floats(all);
+    }
+};
+struct FrontPlan {
+    Room room;
+    Cut cut;
+    FrontPlan(const libscan_attend& p) : cut(p, room) {}
+};
+struct BackPlan {
+    Room room;
+    Cut cut, back;  // of S, and of its gradient
+    int64_t dq_dots, dk_dots, gates, last, dq, dk;
+    BackPlan(const libscan_attend& p) : cut(p, room), back(p, room) {
+        const int64_t tokens = p.batch * p.steps * p.heads;
+        const int64_t blocks = walk_blocks((int)p.dv, (int)p.dk);
+        const bool shared = p.groups < p.heads;
+        dq_dots = room.floats(tokens * blocks);
+        dk_dots = room.floats(tokens * blocks);
+        gates = room.floats(p.fixed ? tokens : 0);
+        last = room.floats(p.batch * p.heads * p.dk * p.dv);
+        dq = room.floats(shared ? tokens * p.dk : 0);
+        dk = room.floats(shared ? tokens * p.dk : 0);
+    }
+};
+
+// The states before every piece of the walk w, whose first and last states are its
+// rows'; w then takes them.
+hipError_t cut_rows(int64_t type, Walk& w, const libscan_attend& p, const Cut& cut, char* mem,
+                    hipStream_t stream) {
+    const Pieces n = pieces(p);
+    w.pieces = n.count, w.piece = n.places;
+    if (n.count == 1) return hipSuccess;
+    Walk states = w;
+    states.first = {};
+    states.last = {(float*)(mem + cut.states), p.dv, 1};
+    states.whole = (float*)(mem + cut.whole);
+    const hipError_t e = run(type, states, Grade::Wide, true, stream);
+    if (e != hipSuccess) return e;
+    const int64_t each = p.dk * p.dv, rows = p.batch * p.heads;
+    k_carry<<<(uint32_t)(rows * ((each + 255) / 256)), 256, 0, stream>>>(
+        states.last.p, states.whole, n.count, each, w.first.p, w.last.p);
+    w.first = states.last;
+    w.last = {};
+    return hipGetLastError();
 }
 
 }  // namespace
 
-size_t attend_scratch_bytes(const libscan_attend& p) { return 0; }
-size_t attend_back_scratch_bytes(const libscan_attend& p) { return (size_t)back_plan(p).bytes; }
+size_t attend_scratch_bytes(const libscan_attend& p) { return (size_t)FrontPlan(p).room.at; }
+size_t attend_back_scratch_bytes(const libscan_attend& p) { return (size_t)BackPlan(p).room.at; }
 
 hipError_t launch_attend(const libscan_attend& p, void* y, float* state_out, void* scratch,
                          hipStream_t stream) {
@@ -190,27 +262,45 @@ hipError_t launch_attend(const libscan_attend& p, void* y, float* state_out, voi
     w.first = {const_cast<float*>(p.state), p.dv, 1};
     w.last = {state_out, p.dv, 1};
     w.out = y;
-    return run(p.type, w, Grade::Narrow, false, stream);
+    const hipError_t e = cut_rows(p.type, w, p, FrontPlan(p).cut, (char*)scratch, stream);
+    return e != hipSuccess ? e : run(p.type, w, Grade::Narrow, false, stream);
 }
 
 hipError_t launch_attend_back(const libscan_attend& p, const void* dy, int64_t dy_batch,
                               int64_t dy_step, int64_t dy_head, const float* dstate_out, void* dq,
                               void* dk, void* dv, float* dlog_decay, float* dstate, void* scratch,
                               hipStream_t stream) {
-    const BackPlan plan = back_plan(p);
+    const BackPlan plan(p);
     char* mem = (char*)scratch;
     const auto floats = [&](int64_t at) { return (float*)(mem + at); };
     const bool shared = p.groups < p.heads;
     const WalkSide side_dy = {dy, dy_batch, dy_step, dy_head, 1};
-    const int64_t state = p.dk * p.dv;
+    const int dots = walk_blocks((int)p.dv, (int)p.dk);
+    float* last = dstate_out ? floats(plan.last) : nullptr;
     hipError_t e;
 
-    Walk w = base(p);  // dq
+    // S forwards, and its gradient backwards with dv
+    Walk s = base(p), g = base(p);
+    s.dk = g.dk = (int)p.dk, s.dv = g.dv = (int)p.dv;
+    s.k = side_k(p), s.v = side_v(p);
+    s.first = {const_cast<float*>(p.state), p.dv, 1};
+    s.last = {last, p.dv, 1};
+    if ((e = cut_rows(p.type, s, p, plan.cut, mem, stream)) != hipSuccess) return e;
+    g.reverse = true;
+    g.q = side_k(p), g.k = side_q(p), g.v = side_dy;
+    g.inner = (float)p.scale;
+    g.first = {const_cast<float*>(dstate_out), p.dv, 1};
+    g.last = {dstate, p.dv, 1};
+    g.out = dv;
+    if ((e = cut_rows(p.type, g, p, plan.back, mem, stream)) != hipSuccess) return e;
+    if ((e = run(p.type, g, Grade::Narrow, false, stream)) != hipSuccess) return e;
+
+    Walk w = s;  // dq, with S turned over
     w.dk = (int)p.dv, w.dv = (int)p.dk;
     w.q = side_dy, w.k = side_v(p), w.v = side_k(p);
     w.outer = (float)p.scale;
-    w.first = {const_cast<float*>(p.state), 1, p.dv};
-    w.last = {dstate_out ? floats(plan.last) : nullptr, 1, p.dv};
+    w.first = {s.first.p, 1, p.dv};
+    w.last = {s.last.p, 1, p.dv};
     w.out = shared ? floats(plan.dq) : dq;
     w.wide = shared;
     w.e = side_q(p);
@@ -220,29 +310,20 @@ hipError_t launch_attend_back(const libscan_attend& p, const void* dy, int64_t d
     w.reverse = true;  // dk
     w.q = side_v(p), w.k = side_dy, w.v = side_q(p);
     w.inner = (float)p.scale, w.outer = 1.0f;
-    w.first = {const_cast<float*>(dstate_out), 1, p.dv};
+    w.first = {g.first.p, 1, p.dv};
     w.last = {};
     w.out = shared ? floats(plan.dk) : dk;
     w.e = side_k(p);
     w.dots = floats(plan.dk_dots);
     if ((e = run(p.type, w, Grade::Wide, false, stream)) != hipSuccess) return e;
 
-    w = base(p);  // dv
-    w.reverse = true;
-    w.dk = (int)p.dk, w.dv = (int)p.dv;
-    w.q = side_k(p), w.k = side_q(p), w.v = side_dy;
-    w.inner = (float)p.scale;
-    w.first = {const_cast<float*>(dstate_out), p.dv, 1};
-    w.last = {dstate, p.dv, 1};
-    w.out = dv;
-    if ((e = run(p.type, w, Grade::Narrow, false, stream)) != hipSuccess) return e;
-
     const uint32_t rows = (uint32_t)(p.batch * p.heads);
+    const int64_t each = p.dk * p.dv;
     if (rows) {
         k_gates<<<rows, kGateThreads, 0, stream>>>(
-            w, floats(plan.dq_dots), walk_blocks((int)p.dv, (int)p.dk), floats(plan.dk_dots), walk_blocks((int)p.dv, (int)p.dk),
-            dstate_out, floats(plan.last), state, p.fixed ? floats(plan.gates) : dlog_decay);
-        if (dstate) k_first_decay<<<rows, 256, 0, stream>>>(w, dstate, state);
+            w, floats(plan.dq_dots), dots, floats(plan.dk_dots), dots, dstate_out, last, each,
+            p.fixed ? floats(plan.gates) : dlog_decay);
+        if (dstate && p.steps) k_first_decay<<<rows, 256, 0, stream>>>(w, dstate, each);
     }
     if (p.fixed && p.heads)
         k_gate_sum<<<(uint32_t)p.heads, kGateThreads, 0, stream>>>(

@@ -73,7 +73,7 @@ __device__ __forceinline__ float walk_decay(const Walk& w, int b, int h, int pla
 enum class Grade { Narrow, Wide };
 
 // Columns of v that a workgroup has.
-inline int walk_columns(int dk, int dv) { return dk <= 128 && dv > 64 ? 128 : 64; }
+inline int walk_columns(int dk, int dv) { return dv > 64 ? 128 : 64; }
 inline int walk_blocks(int dk, int dv) {
     const int columns = walk_columns(dk, dv);
     return (dv + columns - 1) / columns;

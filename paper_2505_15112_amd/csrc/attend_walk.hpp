@@ -16,6 +16,8 @@
 // states overflow or lose their small values, as they would in fp16.
 #pragma once
 
+#include <type_traits>
+
 #include "attend.hpp"
 
 namespace ls {
@@ -27,8 +29,6 @@ typedef short s4 __attribute__((ext_vector_type(4)));
 typedef unsigned u2 __attribute__((ext_vector_type(2)));
 typedef unsigned u4 __attribute__((ext_vector_type(4)));
 typedef float f4 __attribute__((ext_vector_type(4)));
-
-constexpr int kThreads = 256, kWaves = 4;
 
 template <class T>
 inline constexpr int kTerms = 3;
@@ -123,11 +123,10 @@ struct Tile {
 };
 
 // A tile on its way from global memory: vectors of 16 bytes in registers.
-template <class T, int ROWS, int WIDTH>
+template <class T, int ROWS, int WIDTH, int THREADS>
 struct Fetch {
-    static constexpr int V = 16 / sizeof(T), PER_ROW = WIDTH / V;
-    static constexpr int N = ROWS * PER_ROW / kThreads;
-    static_assert(N >= 1 && ROWS * PER_ROW % kThreads == 0, "whole vectors for every thread");
+    static constexpr int V = 16 / sizeof(T), PER_ROW = WIDTH / V, ALL = ROWS * PER_ROW;
+    static constexpr int N = (ALL + THREADS - 1) / THREADS;
     Pack<T, V> r[N];
 
     // Rows at places `base` and on, those below `live`, of which `width` elements exist.
@@ -135,7 +134,8 @@ struct Fetch {
                                          int base, int live, int len) {
 #pragma unroll
         for (int i = 0; i < N; ++i) {
-            const int at = threadIdx.x + i * kThreads, col = at % PER_ROW * V;
+            const int at = threadIdx.x + i * THREADS, col = at % PER_ROW * V;
+            if (ALL % THREADS != 0 && at >= ALL) break;
             const int place = base + at / PER_ROW;
             const int count = place < live ? width - col : 0;
             r[i].load(p + walk_token(w, place < live ? place : base, len) * step +
@@ -147,7 +147,8 @@ struct Fetch {
         constexpr int TERMS = kTerms<T>;
 #pragma unroll
         for (int i = 0; i < N; ++i) {
-            const int at = threadIdx.x + i * kThreads, col = at % PER_ROW * V, row = at / PER_ROW;
+            const int at = threadIdx.x + i * THREADS, col = at % PER_ROW * V, row = at / PER_ROW;
+            if (ALL % THREADS != 0 && at >= ALL) break;
             if constexpr (TERMS == 1) {
                 *reinterpret_cast<u4*>(&s.v[0][row][col]) = __builtin_bit_cast(u4, r[i].v);
             } else {
@@ -184,12 +185,13 @@ __device__ __forceinline__ double running_sum(float g, int lane) {
 }
 
 // TP terms of scores and states, LIM for the products that make outputs, DK the
-// width of q and k rounded up, NT tiles of 16 columns of v to a wave, CH tokens to a
-// chunk.  OUT: with outputs; else the pieces' states alone.
-template <class T, int TP, int LIM, int DK, int NT, int CH, bool OUT>
+// width of q and k rounded up, WAVES of 16 columns of v each, CH tokens to a chunk.
+// OUT: with outputs; else the pieces' states alone.
+template <class T, int TP, int LIM, int DK, int WAVES, int CH, bool OUT>
 struct Kernel {
-    static constexpr int TERMS = kTerms<T>, COLS = 16 * NT * kWaves, STEPS = CH / 32;
-    static constexpr int TILES = CH / 16, DIAGONALS = TILES * (TILES + 1) / 2, PAIRS = DK / 32;
+    static constexpr int TERMS = kTerms<T>, COLS = 16 * WAVES, THREADS = 64 * WAVES;
+    static constexpr int STEPS = CH / 32, TILES = CH / 16, PAIRS = DK / 32;
+    static constexpr int DIAGONALS = TILES * (TILES + 1) / 2;
     struct Shared {
         Tile<TERMS, CH, DK> k;
         Tile<TERMS, CH, COLS> v;
@@ -198,7 +200,7 @@ struct Kernel {
         double c[CH];
         float in[CH], left[CH];  // e^c outer; e^(c[last] - c) inner
         float whole;
-        float dots[kWaves][CH];
+        float dots[WAVES][CH];
     };
 
     // Scores of the tiles on and below the diagonal, shared out over the waves: lane l
@@ -206,8 +208,8 @@ struct Kernel {
     static __device__ __forceinline__ void scores(Shared& s, float factor, int wave, int lane) {
         const int g = lane / 16, n = lane % 16;
 #pragma unroll
-        for (int x = 0; x < (DIAGONALS + kWaves - 1) / kWaves; ++x) {
-            const int at = x * kWaves + wave;
+        for (int x = 0; x < (DIAGONALS + WAVES - 1) / WAVES; ++x) {
+            const int at = x * WAVES + wave;
             if (at >= DIAGONALS) break;
             // the tile's place in the lower triangle
             const int row = at < 1 ? 0 : at < 3 ? 1 : at < 6 ? 2 : 3, col = at - row * (row + 1) / 2;
@@ -227,52 +229,47 @@ struct Kernel {
             unsigned u[TP][2];
             split<TP, 4>(v, u);
 #pragma unroll
-            for (int t = 0; t < TP; ++t) *reinterpret_cast<u2*>(&s.p.v[t][i][j]) = u2{u[t][0], u[t][1]};
+            for (int t = 0; t < TP; ++t)
+                *reinterpret_cast<u2*>(&s.p.v[t][i][j]) = u2{u[t][0], u[t][1]};
         }
     }
 
     // o += the scores times v where v has an infinity or a NaN: such an element
     // counts for its own token and later ones alone (0 times it is not 0).
-    static __device__ __forceinline__ void careful(const Shared& s, f4 (&o)[TILES][NT],
-                                                   const Frag<TERMS> (&v)[STEPS][NT], int wave,
+    static __device__ __forceinline__ void careful(const Shared& s, f4 (&o)[TILES],
+                                                   const Frag<TERMS> (&v)[STEPS], int wave,
                                                    int lane) {
         const int g = lane / 16, n = lane % 16;
+#pragma unroll
         for (int step = 0; step < STEPS; ++step) {
-            Frag<TERMS> clean[NT];
+            Frag<TERMS> clean;
 #pragma unroll
-            for (int x = 0; x < NT; ++x)
+            for (int e = 0; e < 8; ++e) {
+                const bool fine = __builtin_isfinite(v[step].value(e));
 #pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    const Frag<TERMS>& f = step == 0 ? v[0][x] : v[STEPS - 1][x];
-                    const bool fine = __builtin_isfinite(f.value(e));
-#pragma unroll
-                    for (int t = 0; t < TERMS; ++t) clean[x].t[t][e] = fine ? f.t[t][e] : (__bf16)0.0f;
-                }
-#pragma unroll
-            for (int row = 0; row < TILES; ++row) {
-                if (32 * step > 16 * row) continue;
-                const Frag<TP> p = s.p.along(16 * row + n, 32 * step + 8 * g);
-#pragma unroll
-                for (int x = 0; x < NT; ++x) mma<LIM>(o[row][x], clean[x], p);
+                for (int t = 0; t < TERMS; ++t)
+                    clean.t[t][e] = fine ? v[step].t[t][e] : (__bf16)0.0f;
             }
+#pragma unroll
+            for (int row = 0; row < TILES; ++row)
+                if (32 * step <= 16 * row)
+                    mma<LIM>(o[row], clean, s.p.along(16 * row + n, 32 * step + 8 * g));
         }
 #pragma unroll
         for (int row = 0; row < TILES; ++row)
+            for (int j = 0; j <= 16 * row + n; ++j) {
+                float p = 0.0f;
 #pragma unroll
-            for (int x = 0; x < NT; ++x)
-                for (int j = 0; j <= 16 * row + n; ++j) {
-                    float p = 0.0f;
+                for (int t = TP - 1; t >= 0; --t) p += (float)s.p.v[t][16 * row + n][j];
 #pragma unroll
-                    for (int t = TP - 1; t >= 0; --t) p += (float)s.p.v[t][16 * row + n][j];
+                for (int e = 0; e < 4; ++e) {
+                    float value = 0.0f;
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        const int c = (wave * NT + x) * 16 + 4 * g + e;
-                        float value = 0.0f;
-#pragma unroll
-                        for (int t = TERMS - 1; t >= 0; --t) value += (float)s.v.v[t][j][c];
-                        if (!__builtin_isfinite(value)) o[row][x][e] += p * value;
-                    }
+                    for (int t = TERMS - 1; t >= 0; --t)
+                        value += (float)s.v.v[t][j][wave * 16 + 4 * g + e];
+                    if (!__builtin_isfinite(value)) o[row][e] += p * value;
                 }
+            }
     }
 
     static __device__ __forceinline__ void run(const Walk& w, Shared& s) {
@@ -298,7 +295,7 @@ struct Kernel {
         if constexpr (OUT) {
             // places without a token, and the scores' tiles above the diagonal
             const int cols = w.dv - c0 < COLS ? w.dv - c0 : COLS;
-            for (int i = (live > start ? live : start) + wave; i < end; i += kWaves) {
+            for (int i = (live > start ? live : start) + wave; i < end; i += WAVES) {
                 const int64_t o = (((int64_t)b * w.steps + i) * w.heads + h) * w.dv + c0;
                 for (int c = lane; c < cols; c += 64) {
                     if (w.wide)
@@ -307,41 +304,36 @@ struct Kernel {
                         ((T*)w.out)[o + c] = T(0);
                 }
             }
-            for (int i = tid; i < TP * CH * (CH + 8); i += kThreads)
+            for (int i = tid; i < TP * CH * (CH + 8); i += THREADS)
                 (&s.p.v[0][0][0])[i] = (__bf16)0.0f;
         }
 
-        // The state: column c0 + (wave NT + x) 16 + n, rows 32 p + 8 g + 4 y + e.
-        f4 state[PAIRS][NT][2];
-#pragma unroll
-        for (int p = 0; p < PAIRS; ++p)
-#pragma unroll
-            for (int x = 0; x < NT; ++x)
-#pragma unroll
-                for (int y = 0; y < 2; ++y) state[p][x][y] = f4{};
+        // The state: column c0 + 16 wave + n, rows 32 p + 8 g + 4 y + e.
+        f4 state[PAIRS][2];
         const auto each = [&](auto f) {
+            const int c = c0 + wave * 16 + n;
+            if (c >= w.dv) return;
 #pragma unroll
             for (int p = 0; p < PAIRS; ++p)
 #pragma unroll
-                for (int x = 0; x < NT; ++x)
+                for (int y = 0; y < 2; ++y)
 #pragma unroll
-                    for (int y = 0; y < 2; ++y)
-#pragma unroll
-                        for (int e = 0; e < 4; ++e) {
-                            const int r = 32 * p + 8 * g + 4 * y + e;
-                            const int c = c0 + (wave * NT + x) * 16 + n;
-                            if (r < w.dk && c < w.dv) f(r, c, p, x, y, e);
-                        }
+                    for (int e = 0; e < 4; ++e) {
+                        const int r = 32 * p + 8 * g + 4 * y + e;
+                        if (r < w.dk) f(r, c, p, y, e);
+                    }
         };
+#pragma unroll
+        for (int p = 0; p < PAIRS; ++p) state[p][0] = state[p][1] = f4{};
         if (OUT && w.first.p) {
             const float* from = w.first.p + number * w.dk * w.dv;
-            each([&](int r, int c, int p, int x, int y, int e) {
-                state[p][x][y][e] = from[r * w.first.row + c * w.first.col];
+            each([&](int r, int c, int p, int y, int e) {
+                state[p][y][e] = from[r * w.first.row + c * w.first.col];
             });
         }
 
-        Fetch<T, CH, DK> fq, fk;
-        Fetch<T, CH, COLS> fv;
+        Fetch<T, CH, DK, THREADS> fq, fk;
+        Fetch<T, CH, COLS, THREADS> fv;
         float decay;
         const auto fetch = [&](int base) {
             fk.load(w, pk, w.k.step, w.dk, base, live, len);
@@ -352,7 +344,9 @@ struct Kernel {
         };
         const auto put_dots = [&](int base) {
             if (tid >= CH || base + tid >= live) return;
-            const float sum = s.dots[0][tid] + s.dots[1][tid] + s.dots[2][tid] + s.dots[3][tid];
+            float sum = 0.0f;
+#pragma unroll
+            for (int i = 0; i < WAVES; ++i) sum += s.dots[i][tid];
             const int t = walk_token(w, base + tid, len);
             w.dots[(((int64_t)block * w.batch + b) * w.steps + t) * w.heads + h] = sum;
         };
@@ -378,95 +372,71 @@ struct Kernel {
             __syncthreads();
             if (base + CH < live) fetch(base + CH);
 
-            Frag<TERMS> v[STEPS][NT];
+            Frag<TERMS> v[STEPS];
 #pragma unroll
             for (int step = 0; step < STEPS; ++step)
-#pragma unroll
-                for (int x = 0; x < NT; ++x)
-                    v[step][x] = s.v.down(32 * step, (wave * NT + x) * 16 + 4 * (lane % 4), lane);
+                v[step] = s.v.down(32 * step, wave * 16 + 4 * (lane % 4), lane);
 
             if constexpr (OUT) {
                 scores(s, w.inner * w.outer, wave, lane);
-                f4 o[TILES][NT];
+                f4 o[TILES];
 #pragma unroll
-                for (int row = 0; row < TILES; ++row)
-#pragma unroll
-                    for (int x = 0; x < NT; ++x) o[row][x] = f4{};
+                for (int row = 0; row < TILES; ++row) o[row] = f4{};
 #pragma unroll
                 for (int p = 0; p < PAIRS; ++p) {
-                    Frag<TP> f[NT];
+                    const f4 lo = state[p][0], hi = state[p][1];
+                    const float r[8] = {lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
+                    Frag<TP> f;
+                    f.from(r);
 #pragma unroll
-                    for (int x = 0; x < NT; ++x) {
-                        const float r[8] = {state[p][x][0][0], state[p][x][0][1], state[p][x][0][2],
-                                            state[p][x][0][3], state[p][x][1][0], state[p][x][1][1],
-                                            state[p][x][1][2], state[p][x][1][3]};
-                        f[x].from(r);
-                    }
-#pragma unroll
-                    for (int row = 0; row < TILES; ++row) {
-                        const Frag<TERMS> q = s.q.along(16 * row + n, 32 * p + 8 * g);
-#pragma unroll
-                        for (int x = 0; x < NT; ++x) mma<LIM>(o[row][x], f[x], q);
-                    }
+                    for (int row = 0; row < TILES; ++row)
+                        mma<LIM>(o[row], f, s.q.along(16 * row + n, 32 * p + 8 * g));
                 }
 #pragma unroll
-                for (int row = 0; row < TILES; ++row)
-#pragma unroll
-                    for (int x = 0; x < NT; ++x) o[row][x] *= s.in[16 * row + n];
-                // finite elements of v times 0 add up to 0
-                float zero = 0.0f;
+                for (int row = 0; row < TILES; ++row) o[row] *= s.in[16 * row + n];
+                // 0 times a finite v adds up to 0
+                f4 zero{};
 #pragma unroll
                 for (int step = 0; step < STEPS; ++step)
-#pragma unroll
-                    for (int x = 0; x < NT; ++x)
-#pragma unroll
-                        for (int e = 0; e < 8; ++e)
-                            zero = __builtin_fmaf(v[step][x].value(e), 0.0f, zero);
-                const bool fine = __all(zero == 0.0f);
+                    zero = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v[step].t[0], bf8{}, zero, 0, 0, 0);
+                const bool fine =
+                    __all(zero[0] == 0.0f && zero[1] == 0.0f && zero[2] == 0.0f && zero[3] == 0.0f);
                 __syncthreads();  // the scores are written
                 if (fine) {
 #pragma unroll
                     for (int row = 0; row < TILES; ++row)
 #pragma unroll
-                        for (int step = 0; step < STEPS; ++step) {
-                            if (32 * step > 16 * row) continue;
-                            const Frag<TP> p = s.p.along(16 * row + n, 32 * step + 8 * g);
-#pragma unroll
-                            for (int x = 0; x < NT; ++x) mma<LIM>(o[row][x], v[step][x], p);
-                        }
+                        for (int step = 0; step < STEPS; ++step)
+                            if (32 * step <= 16 * row)
+                                mma<LIM>(o[row], v[step],
+                                         s.p.along(16 * row + n, 32 * step + 8 * g));
                 } else {
                     careful(s, o, v, wave, lane);
                 }
 #pragma unroll
                 for (int row = 0; row < TILES; ++row) {
-                    const int place = base + 16 * row + n;
+                    const int place = base + 16 * row + n, c = c0 + wave * 16 + 4 * g;
                     float dot = 0.0f;
-                    if (place < live) {
-                        const int t = walk_token(w, place, len);
-                        const int64_t to = (((int64_t)b * w.steps + t) * w.heads + h) * w.dv;
+                    if (place < live && c < w.dv) {
+                        const int t = walk_token(w, place, len), count = w.dv - c;
+                        const int64_t to = (((int64_t)b * w.steps + t) * w.heads + h) * w.dv + c;
+                        if (w.dots) {
+                            Pack<T, 4> e;
+                            e.load(side(w.e) + t * w.e.step + c, count);
 #pragma unroll
-                        for (int x = 0; x < NT; ++x) {
-                            const int c = c0 + (wave * NT + x) * 16 + 4 * g;
-                            if (c >= w.dv) continue;
-                            if (w.dots) {
-                                Pack<T, 4> e;
-                                e.load(side(w.e) + t * w.e.step + c, w.dv - c);
+                            for (int y = 0; y < 4; ++y)
+                                if (y < count) dot = __builtin_fmaf(o[row][y], to_f32(e.v[y]), dot);
+                        }
+                        if (w.wide) {
+                            Pack<float, 4> r;
 #pragma unroll
-                                for (int y = 0; y < 4; ++y)
-                                    if (c + y < w.dv)
-                                        dot = __builtin_fmaf(o[row][x][y], to_f32(e.v[y]), dot);
-                            }
-                            if (w.wide) {
-                                Pack<float, 4> r;
+                            for (int y = 0; y < 4; ++y) r.v[y] = o[row][y];
+                            r.store((float*)w.out + to, count);
+                        } else {
+                            Pack<T, 4> r;
 #pragma unroll
-                                for (int y = 0; y < 4; ++y) r.v[y] = o[row][x][y];
-                                r.store((float*)w.out + to + c, w.dv - c);
-                            } else {
-                                Pack<T, 4> r;
-#pragma unroll
-                                for (int y = 0; y < 4; ++y) r.v[y] = from_f32<T>(o[row][x][y]);
-                                r.store((T*)w.out + to + c, w.dv - c);
-                            }
+                            for (int y = 0; y < 4; ++y) r.v[y] = from_f32<T>(o[row][y]);
+                            r.store((T*)w.out + to, count);
                         }
                     }
                     if (w.dots) {
@@ -479,30 +449,24 @@ struct Kernel {
 
             // the state behind the chunk
             const float whole = s.whole;
-            Frag<3> vw[STEPS][NT];
+            Frag<3> vw[STEPS];
 #pragma unroll
-            for (int step = 0; step < STEPS; ++step)
+            for (int step = 0; step < STEPS; ++step) {
+                float r[8];
 #pragma unroll
-                for (int x = 0; x < NT; ++x) {
-                    float r[8];
-#pragma unroll
-                    for (int e = 0; e < 8; ++e)
-                        r[e] = v[step][x].value(e) * s.left[32 * step + 8 * g + e];
-                    vw[step][x].from(r);
-                }
+                for (int e = 0; e < 8; ++e) r[e] = v[step].value(e) * s.left[32 * step + 8 * g + e];
+                vw[step].from(r);
+            }
 #pragma unroll
             for (int p = 0; p < PAIRS; ++p)
 #pragma unroll
                 for (int y = 0; y < 2; ++y) {
+                    state[p][y] *= whole;
 #pragma unroll
-                    for (int x = 0; x < NT; ++x) state[p][x][y] *= whole;
-#pragma unroll
-                    for (int step = 0; step < STEPS; ++step) {
-                        const Frag<TERMS> k =
-                            s.k.down(32 * step, 32 * p + 8 * (lane % 4) + 4 * y, lane);
-#pragma unroll
-                        for (int x = 0; x < NT; ++x) mma<3>(state[p][x][y], k, vw[step][x]);
-                    }
+                    for (int step = 0; step < STEPS; ++step)
+                        mma<3>(state[p][y],
+                               s.k.down(32 * step, 32 * p + 8 * (lane % 4) + 4 * y, lane),
+                               vw[step]);
                 }
         }
         if (OUT && w.dots && live > start) {
@@ -511,32 +475,32 @@ struct Kernel {
         }
         if (w.last.p && (!OUT || w.pieces == 1)) {
             float* to = w.last.p + number * w.dk * w.dv;
-            each([&](int r, int c, int p, int x, int y, int e) {
-                to[r * w.last.row + c * w.last.col] = state[p][x][y][e];
+            each([&](int r, int c, int p, int y, int e) {
+                to[r * w.last.row + c * w.last.col] = state[p][y][e];
             });
         }
         if (!OUT && block == 0 && tid == 0) w.whole[number] = exp2_fast((float)total);
     }
 };
 
-template <class T, int TP, int LIM, int DK, int NT, int CH, bool OUT>
-__global__ void __launch_bounds__(kThreads, 1) k_walk(Walk w) {
-    using K = Kernel<T, TP, LIM, DK, NT, CH, OUT>;
+template <class T, int TP, int LIM, int DK, int WAVES, int CH, bool OUT>
+__global__ void __launch_bounds__(64 * WAVES, 2) k_walk(Walk w) {
+    using K = Kernel<T, TP, LIM, DK, WAVES, CH, OUT>;
     __shared__ typename K::Shared s;
     K::run(w, s);
 }
 
-template <class T, int DK, int NT, int CH>
+template <class T, int DK, int WAVES, int CH>
 hipError_t launch(const Walk& w, Grade grade, bool states, hipStream_t stream) {
-    constexpr int COLS = 16 * NT * kWaves, NARROW = kTerms<T> == 3 ? 3 : 2;
+    constexpr int COLS = 16 * WAVES, THREADS = 64 * WAVES, NARROW = kTerms<T> == 3 ? 3 : 2;
     const int64_t grid = (int64_t)w.batch * w.heads * w.pieces * ((w.dv + COLS - 1) / COLS);
     if (grid == 0) return hipSuccess;
     if (states)
-        k_walk<T, 1, 3, DK, NT, CH, false><<<(uint32_t)grid, kThreads, 0, stream>>>(w);
+        k_walk<T, 1, 3, DK, WAVES, CH, false><<<(uint32_t)grid, THREADS, 0, stream>>>(w);
     else if (grade == Grade::Narrow)
-        k_walk<T, NARROW, NARROW, DK, NT, CH, true><<<(uint32_t)grid, kThreads, 0, stream>>>(w);
+        k_walk<T, NARROW, NARROW, DK, WAVES, CH, true><<<(uint32_t)grid, THREADS, 0, stream>>>(w);
     else
-        k_walk<T, 3, 3, DK, NT, CH, true><<<(uint32_t)grid, kThreads, 0, stream>>>(w);
+        k_walk<T, 3, 3, DK, WAVES, CH, true><<<(uint32_t)grid, THREADS, 0, stream>>>(w);
     return hipGetLastError();
 }
 
@@ -546,12 +510,13 @@ template <class T>
 hipError_t launch_walk(const Walk& w, Grade grade, bool states, hipStream_t stream) {
     constexpr int CH = walk::kTerms<T> == 1 ? 64 : 32;
     const bool wide = walk_columns(w.dk, w.dv) == 128;
-    if (w.dk > 128) return walk::launch<T, 256, 1, CH>(w, grade, states, stream);
-    if (w.dk > 64)
-        return wide ? walk::launch<T, 128, 2, CH>(w, grade, states, stream)
-                    : walk::launch<T, 128, 1, CH>(w, grade, states, stream);
-    return wide ? walk::launch<T, 64, 2, CH>(w, grade, states, stream)
-                : walk::launch<T, 64, 1, CH>(w, grade, states, stream);
+    const auto by_width = [&](auto dk) {
+        return wide ? walk::launch<T, dk.value, 8, CH>(w, grade, states, stream)
+                    : walk::launch<T, dk.value, 4, CH>(w, grade, states, stream);
+    };
+    if (w.dk > 128) return by_width(std::integral_constant<int, 256>());
+    if (w.dk > 64) return by_width(std::integral_constant<int, 128>());
+    return by_width(std::integral_constant<int, 64>());
 }
 
 }  // namespace ls
