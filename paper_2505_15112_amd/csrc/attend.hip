@@ -146,10 +146,10 @@ __global__ void __launch_bounds__(kCols)
 
 // ------------------------------------------------ launches
 
-hipError_t run(int64_t type, const Walk& w, Grade grade, bool states, hipStream_t stream) {
-    return type == LIBSCAN_F32   ? launch_walk<float>(w, grade, states, stream)
-           : type == LIBSCAN_F16 ? launch_walk<_Float16>(w, grade, states, stream)
-                                 : launch_walk<__bf16>(w, grade, states, stream);
+hipError_t run(int64_t type, const Walk& w, bool states, hipStream_t stream) {
+    return type == LIBSCAN_F32   ? launch_walk<float>(w, states, stream)
+           : type == LIBSCAN_F16 ? launch_walk<_Float16>(w, states, stream)
+                                 : launch_walk<__bf16>(w, states, stream);
 }
 
 // What all walks of a call have in common.
@@ -238,7 +238,7 @@ hipError_t cut_rows(int64_t type, Walk& w, const libscan_attend& p, const Cut& c
     states.first = {};
     states.last = {(float*)(mem + cut.states), p.dv, 1};
     states.whole = (float*)(mem + cut.whole);
-    const hipError_t e = run(type, states, Grade::Wide, true, stream);
+    const hipError_t e = run(type, states, true, stream);
     if (e != hipSuccess) return e;
     const int64_t each = p.dk * p.dv, rows = p.batch * p.heads;
     k_carry<<<(uint32_t)(rows * ((each + 255) / 256)), 256, 0, stream>>>(
@@ -263,7 +263,7 @@ hipError_t launch_attend(const libscan_attend& p, void* y, float* state_out, voi
     w.last = {state_out, p.dv, 1};
     w.out = y;
     const hipError_t e = cut_rows(p.type, w, p, FrontPlan(p).cut, (char*)scratch, stream);
-    return e != hipSuccess ? e : run(p.type, w, Grade::Narrow, false, stream);
+    return e != hipSuccess ? e : run(p.type, w, false, stream);
 }
 
 hipError_t launch_attend_back(const libscan_attend& p, const void* dy, int64_t dy_batch,
@@ -293,7 +293,7 @@ hipError_t launch_attend_back(const libscan_attend& p, const void* dy, int64_t d
     g.last = {dstate, p.dv, 1};
     g.out = dv;
     if ((e = cut_rows(p.type, g, p, plan.back, mem, stream)) != hipSuccess) return e;
-    if ((e = run(p.type, g, Grade::Narrow, false, stream)) != hipSuccess) return e;
+    if ((e = run(p.type, g, false, stream)) != hipSuccess) return e;
 
     Walk w = s;  // dq, with S turned over
     w.dk = (int)p.dv, w.dv = (int)p.dk;
@@ -305,7 +305,7 @@ hipError_t launch_attend_back(const libscan_attend& p, const void* dy, int64_t d
     w.wide = shared;
     w.e = side_q(p);
     w.dots = floats(plan.dq_dots);
-    if ((e = run(p.type, w, Grade::Wide, false, stream)) != hipSuccess) return e;
+    if ((e = run(p.type, w, false, stream)) != hipSuccess) return e;
 
     w.reverse = true;  // dk
     w.q = side_v(p), w.k = side_dy, w.v = side_q(p);
@@ -315,7 +315,7 @@ hipError_t launch_attend_back(const libscan_attend& p, const void* dy, int64_t d
     w.out = shared ? floats(plan.dk) : dk;
     w.e = side_k(p);
     w.dots = floats(plan.dk_dots);
-    if ((e = run(p.type, w, Grade::Wide, false, stream)) != hipSuccess) return e;
+    if ((e = run(p.type, w, false, stream)) != hipSuccess) return e;
 
     const uint32_t rows = (uint32_t)(p.batch * p.heads);
     const int64_t each = p.dk * p.dv;

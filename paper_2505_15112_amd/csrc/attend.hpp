@@ -45,7 +45,7 @@ struct Walk {
     float* whole;  // in such a run, for each row, head and piece: the product of its decays
     // Output: batch x steps x heads x dv, dense; fp32 where `wide`.  With `dots`
     // (batch x steps x heads for each block of columns), the sums of the output
-    // times e, before it is rounded.
+    // times e, before it is rounded; it is then formed to fp32's precision.
     void* out;
     bool wide;
     WalkSide e;
@@ -69,9 +69,6 @@ __device__ __forceinline__ float walk_decay(const Walk& w, int b, int h, int pla
     return w.g[b * w.g_batch + t * w.g_step + h];
 }
 
-// How exact a walk is: the outputs to 16 bits, or to 32 (attend_walk.hpp).
-enum class Grade { Narrow, Wide };
-
 // Columns of v that a workgroup has.
 inline int walk_columns(int dk, int dv) { return dv > 64 ? 128 : 64; }
 inline int walk_blocks(int dk, int dv) {
@@ -82,9 +79,9 @@ inline int walk_blocks(int dk, int dv) {
 // One instance for each element type (attend_f32.hip and so on).  `states`: what each
 // piece adds to the state and no outputs.
 template <class T>
-hipError_t launch_walk(const Walk& w, Grade grade, bool states, hipStream_t stream);
-extern template hipError_t launch_walk<float>(const Walk&, Grade, bool, hipStream_t);
-extern template hipError_t launch_walk<_Float16>(const Walk&, Grade, bool, hipStream_t);
-extern template hipError_t launch_walk<__bf16>(const Walk&, Grade, bool, hipStream_t);
+hipError_t launch_walk(const Walk& w, bool states, hipStream_t stream);
+extern template hipError_t launch_walk<float>(const Walk&, bool, hipStream_t);
+extern template hipError_t launch_walk<_Float16>(const Walk&, bool, hipStream_t);
+extern template hipError_t launch_walk<__bf16>(const Walk&, bool, hipStream_t);
 
 }  // namespace ls

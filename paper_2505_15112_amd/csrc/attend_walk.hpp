@@ -91,11 +91,13 @@ __device__ __forceinline__ void mma(f4& c, const Frag<NA>& a, const Frag<NB>& b)
                     c = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a.t[i], b.t[j], c, 0, 0, 0);
 }
 
-// A tile of ROWS x WIDTH elements in LDS, by terms.
-template <int TERMS, int ROWS, int WIDTH>
+// A tile of ROWS x WIDTH elements in LDS, by terms.  PAD elements behind a row spread
+// the lanes of an access over the banks: 16 bytes each of 16 rows (along), or 8 bytes each
+// of 8 rows, 16 apart (down).
+template <int TERMS, int ROWS, int WIDTH, int PAD>
 struct Tile {
-    static constexpr int ROW = WIDTH + 8;  // rows of 16 lanes fall on different banks
-    __bf16 v[TERMS][ROWS][ROW];
+    static constexpr int ROW = WIDTH + PAD;
+    alignas(16) __bf16 v[TERMS][ROWS][ROW];
 
     // Eight elements along a row.
     __device__ __forceinline__ Frag<TERMS> along(int row, int col) const {
@@ -122,85 +124,140 @@ struct Tile {
     }
 };
 
-// A tile on its way from global memory: vectors of 16 bytes in registers.
+// The chunks of one operand on their way from global memory to LDS: vectors of 16 bytes in
+// registers, the addresses of the first ones moving on from chunk to chunk.
 template <class T, int ROWS, int WIDTH, int THREADS>
 struct Fetch {
     static constexpr int V = 16 / sizeof(T), PER_ROW = WIDTH / V, ALL = ROWS * PER_ROW;
-    static constexpr int N = (ALL + THREADS - 1) / THREADS;
-    Pack<T, V> r[N];
+    static constexpr int N = (ALL + THREADS - 1) / THREADS, BETWEEN = THREADS / PER_ROW;
+    typedef typename Pack<T, V>::Vec Vec;
+    Vec r[N];
+    const T* at;      // this thread's first vector of the next chunk
+    int64_t forward;  // elements to the next place
+    int width;
 
-    // Rows at places `base` and on, those below `live`, of which `width` elements exist.
-    __device__ __forceinline__ void load(const Walk& w, const T* p, int64_t step, int width,
-                                         int base, int live, int len) {
-#pragma unroll
-        for (int i = 0; i < N; ++i) {
-            const int at = threadIdx.x + i * THREADS, col = at % PER_ROW * V;
-            if (ALL % THREADS != 0 && at >= ALL) break;
-            const int place = base + at / PER_ROW;
-            const int count = place < live ? width - col : 0;
-            r[i].load(p + walk_token(w, place < live ? place : base, len) * step +
-                          (col < width ? col : 0),
-                      count);
-        }
+    // p: the operand's row at place `base`, and elements to the next place.
+    __device__ __forceinline__ void init(const T* p, int64_t step, int elements) {
+        forward = step;
+        width = elements;
+        at = p + threadIdx.x / PER_ROW * step + threadIdx.x % PER_ROW * V;
     }
-    __device__ __forceinline__ void store(Tile<kTerms<T>, ROWS, WIDTH>& s) const {
+    // The next chunk, of which the first `rows` places have tokens; 0 elsewhere.
+    __device__ __forceinline__ void load(int rows) {
+        const bool mine = ALL % THREADS == 0 || threadIdx.x < ALL;
+        if (rows >= ROWS && width >= WIDTH) {
+#pragma unroll
+            for (int i = 0; i < N; ++i)
+                if (mine) r[i] = *reinterpret_cast<const Vec*>(at + i * BETWEEN * forward);
+        } else {
+            const int col = threadIdx.x % PER_ROW * V, row = threadIdx.x / PER_ROW;
+#pragma unroll
+            for (int i = 0; i < N; ++i) {
+                Vec v{};
+                if (mine && row + i * BETWEEN < rows && col < width) {
+                    const T* from = at + i * BETWEEN * forward;
+                    if (col + V <= width) {
+                        v = *reinterpret_cast<const Vec*>(from);
+                    } else {
+#pragma unroll
+                        for (int e = 0; e < V - 1; ++e)
+                            if (col + e < width) v[e] = from[e];
+                    }
+                }
+                r[i] = v;
+            }
+        }
+        at += ROWS * forward;
+    }
+    template <class S>
+    __device__ __forceinline__ void store(S& s) const {
         constexpr int TERMS = kTerms<T>;
+        if (ALL % THREADS != 0 && threadIdx.x >= ALL) return;
+        const int col = threadIdx.x % PER_ROW * V, row = threadIdx.x / PER_ROW;
 #pragma unroll
         for (int i = 0; i < N; ++i) {
-            const int at = threadIdx.x + i * THREADS, col = at % PER_ROW * V, row = at / PER_ROW;
-            if (ALL % THREADS != 0 && at >= ALL) break;
             if constexpr (TERMS == 1) {
-                *reinterpret_cast<u4*>(&s.v[0][row][col]) = __builtin_bit_cast(u4, r[i].v);
+                *reinterpret_cast<u4*>(&s.v[0][row + i * BETWEEN][col]) =
+                    __builtin_bit_cast(u4, r[i]);
             } else {
                 float f[V];
                 unsigned u[TERMS][V / 2];
 #pragma unroll
-                for (int e = 0; e < V; ++e) f[e] = to_f32(r[i].v[e]);
+                for (int e = 0; e < V; ++e) f[e] = to_f32(r[i][e]);
                 split<TERMS, V>(f, u);
 #pragma unroll
                 for (int t = 0; t < TERMS; ++t) {
+                    __bf16* to = &s.v[t][row + i * BETWEEN][col];
                     if constexpr (V == 8)
-                        *reinterpret_cast<u4*>(&s.v[t][row][col]) =
-                            u4{u[t][0], u[t][1], u[t][2], u[t][3]};
+                        *reinterpret_cast<u4*>(to) = u4{u[t][0], u[t][1], u[t][2], u[t][3]};
                     else
-                        *reinterpret_cast<u2*>(&s.v[t][row][col]) = u2{u[t][0], u[t][1]};
+                        *reinterpret_cast<u2*>(to) = u2{u[t][0], u[t][1]};
                 }
             }
         }
     }
 };
 
+__device__ __forceinline__ double lane_value(double c, int lane) {
+    const auto b = __builtin_bit_cast(u2, c);
+    return __builtin_bit_cast(double, u2{(unsigned)__builtin_amdgcn_readlane(b[0], lane),
+                                         (unsigned)__builtin_amdgcn_readlane(b[1], lane)});
+}
+
+template <int CTRL, int ROWS>
+__device__ __forceinline__ double add_from(double c) {
+    const auto b = __builtin_bit_cast(u2, c);
+    u2 m;
+    m[0] = __builtin_amdgcn_update_dpp(0, b[0], CTRL, ROWS, 0xf, false);
+    m[1] = __builtin_amdgcn_update_dpp(0, b[1], CTRL, ROWS, 0xf, false);
+    return c + __builtin_bit_cast(double, m);
+}
+
 // Running sums of the chunk's decays over the lanes of a wave, in powers of two.  A
 // decay past +-1024 is one of 0 or infinity either way; infinities would turn the
 // differences of sums to NaN.
-__device__ __forceinline__ double running_sum(float g, int lane) {
+__device__ __forceinline__ double running_sum(float g) {
     double c = (double)g * 1.4426950408889634;
     c = c < -1024.0 ? -1024.0 : c > 1024.0 ? 1024.0 : c;  // a NaN stays
-#pragma unroll
-    for (int m = 1; m < 64; m <<= 1) {
-        const double up = __shfl_up(c, m);
-        if (lane >= m) c += up;
-    }
-    return c;
+    // rows of 16 lanes by shifts of 1, 2, 4 and 8, then the rows before
+    c = add_from<0x111, 0xf>(c);
+    c = add_from<0x112, 0xf>(c);
+    c = add_from<0x114, 0xf>(c);
+    c = add_from<0x118, 0xf>(c);
+    c = add_from<0x142, 0xa>(c);
+    return add_from<0x143, 0xc>(c);
+}
+
+// A running sum's part in 256ths.  Such parts fit fp32 (a chunk's sums stay below 2^16),
+// and so do their differences, which makes that of two sums exact to the rest's 2^-33.
+__device__ __forceinline__ float high_part(double c) {
+    return (float)(__builtin_rint(c * 256.0) * (1.0 / 256.0));
 }
 
 // TP terms of scores and states, LIM for the products that make outputs, DK the
 // width of q and k rounded up, WAVES of 16 columns of v each, CH tokens to a chunk.
-// OUT: with outputs; else the pieces' states alone.
-template <class T, int TP, int LIM, int DK, int WAVES, int CH, bool OUT>
+// OUT: with outputs; else the pieces' states alone.  DOTS: with the sums of the
+// outputs times e.
+template <class T, int TP, int LIM, int DK, int WAVES_, int CH, bool OUT, bool DOTS>
 struct Kernel {
-    static constexpr int TERMS = kTerms<T>, COLS = 16 * WAVES, THREADS = 64 * WAVES;
+    static constexpr int WAVES = WAVES_, COLS = 16 * WAVES, THREADS = 64 * WAVES;
+    static constexpr int TERMS = kTerms<T>;
     static constexpr int STEPS = CH / 32, TILES = CH / 16, PAIRS = DK / 32;
     static constexpr int DIAGONALS = TILES * (TILES + 1) / 2;
     struct Shared {
-        Tile<TERMS, CH, DK> k;
-        Tile<TERMS, CH, COLS> v;
-        Tile<TERMS, OUT ? CH : 1, DK> q;
-        Tile<TP, OUT ? CH : 1, CH> p;
-        double c[CH];
+        Tile<TERMS, CH, DK, DK == 64 ? 16 : 24> k;
+        Tile<TERMS, CH, COLS, 8> v;
+        Tile<TERMS, OUT ? CH : 1, DK, 8> q;
+        Tile<TP, OUT ? CH : 1, CH, 8> p;  // the scores
+        float2 c[CH];            // the running sums in two parts, see high_part
         float in[CH], left[CH];  // e^c outer; e^(c[last] - c) inner
         float whole;
-        float dots[WAVES][CH];
+
+        // A wave's part of a token's dot product, in the padding of k's row.
+        __device__ __forceinline__ float& dot(int wave, int token) {
+            static_assert(WAVES <= 8, "eight floats");
+            return reinterpret_cast<float*>(&k.v[0][token][DK])[wave];
+        }
     };
 
     // Scores of the tiles on and below the diagonal, shared out over the waves: lane l
@@ -219,11 +276,12 @@ struct Kernel {
                 mma<LIM>(acc, s.k.along(16 * col + n, 32 * p + 8 * g),
                          s.q.along(16 * row + n, 32 * p + 8 * g));
             const int i = 16 * row + n, j = 16 * col + 4 * g;
-            const double ci = s.c[i];
+            const float2 ci = s.c[i];
             float v[4];
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
-                const float d = exp2_fast((float)(ci - s.c[j + e])) * factor;
+                const float2 cj = s.c[j + e];
+                const float d = exp2_fast((ci.x - cj.x) + (ci.y - cj.y)) * factor;
                 v[e] = j + e <= i ? acc[e] * d : 0.0f;
             }
             unsigned u[TP][2];
@@ -272,6 +330,39 @@ struct Kernel {
             }
     }
 
+    // Element (r, c) of a state, from its address and strides: the lane's eight rows of
+    // each of PAIRS are 32 p + 8 g + 0..7, its column 16 wave + n.
+    typedef f4 State[PAIRS][2];
+    static __device__ __forceinline__ void load_state(State& state, const float* p, const Walk& w,
+                                                      const WalkState& at, int c, int g) {
+        p += c * at.col + 8 * g * at.row;
+        if (w.dk == DK && at.row == 1) {
+            typedef f4 Vec __attribute__((aligned(4)));
+#pragma unroll
+            for (int x = 0; x < PAIRS; ++x)
+#pragma unroll
+                for (int y = 0; y < 2; ++y)
+                    state[x][y] = *reinterpret_cast<const Vec*>(p + 32 * x + 4 * y);
+            return;
+        }
+#pragma unroll
+        for (int x = 0; x < PAIRS; ++x)
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+                if (32 * x + 8 * g + e < w.dk)
+                    state[x][e / 4][e % 4] = p[(32 * x + e) * at.row];
+    }
+    static __device__ __forceinline__ void store_state(const State& state, float* p, const Walk& w,
+                                                       const WalkState& at, int c, int g) {
+        p += c * at.col + 8 * g * at.row;
+#pragma unroll
+        for (int x = 0; x < PAIRS; ++x)
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+                if (32 * x + 8 * g + e < w.dk)
+                    p[(32 * x + e) * at.row] = state[x][e / 4][e % 4];
+    }
+
     static __device__ __forceinline__ void run(const Walk& w, Shared& s) {
         const int tid = threadIdx.x, wave = tid / 64, lane = tid % 64, g = lane / 16, n = lane % 16;
         const int blocks = (w.dv + COLS - 1) / COLS;
@@ -286,11 +377,34 @@ struct Kernel {
         const int end = start + w.piece < w.steps ? start + w.piece : w.steps;
         const int live = len < end ? len : end;  // places of this piece that have tokens
         const int64_t number = (int64_t)bh * w.pieces + piece;
+        const int column = c0 + wave * 16 + n;  // of the state
 
-        const auto side = [&](const WalkSide& x) {
-            return (const T*)x.p + b * x.batch + (h / x.share) * x.head;
+        // The first place's token, and the way from token to token.
+        const int way = w.reverse ? -1 : 1, first = w.reverse ? len - 1 - start : start;
+        const auto side = [&](const WalkSide& x, int t) {
+            return (const T*)x.p + b * x.batch + (h / x.share) * x.head + t * x.step;
         };
-        const T *pq = side(w.q), *pk = side(w.k), *pv = side(w.v) + c0;
+        Fetch<T, CH, DK, THREADS> fq, fk;
+        Fetch<T, CH, COLS, THREADS> fv;
+        float decay = 0.0f;
+        const auto fetch = [&](int base) {
+            fk.load(live - base);
+            fv.load(live - base);
+            if constexpr (OUT) fq.load(live - base);
+            if (wave == 0)
+                decay = lane < CH && base + lane < live ? walk_decay(w, b, h, base + lane, len) : 0.0f;
+        };
+        State state;
+#pragma unroll
+        for (int x = 0; x < PAIRS; ++x) state[x][0] = state[x][1] = f4{};
+        if (start < live) {
+            fk.init(side(w.k, first), way * w.k.step, w.dk);
+            fv.init(side(w.v, first) + c0, way * w.v.step, w.dv - c0);
+            if constexpr (OUT) fq.init(side(w.q, first), way * w.q.step, w.dk);
+            fetch(start);
+        }
+        if (OUT && w.first.p && column < w.dv)
+            load_state(state, w.first.p + number * w.dk * w.dv, w, w.first, column, g);
 
         if constexpr (OUT) {
             // places without a token, and the scores' tiles above the diagonal
@@ -304,67 +418,40 @@ struct Kernel {
                         ((T*)w.out)[o + c] = T(0);
                 }
             }
-            for (int i = tid; i < TP * CH * (CH + 8); i += THREADS)
+            for (int i = tid; i < TP * CH * s.p.ROW; i += THREADS)
                 (&s.p.v[0][0][0])[i] = (__bf16)0.0f;
         }
 
-        // The state: column c0 + 16 wave + n, rows 32 p + 8 g + 4 y + e.
-        f4 state[PAIRS][2];
-        const auto each = [&](auto f) {
-            const int c = c0 + wave * 16 + n;
-            if (c >= w.dv) return;
-#pragma unroll
-            for (int p = 0; p < PAIRS; ++p)
-#pragma unroll
-                for (int y = 0; y < 2; ++y)
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        const int r = 32 * p + 8 * g + 4 * y + e;
-                        if (r < w.dk) f(r, c, p, y, e);
-                    }
-        };
-#pragma unroll
-        for (int p = 0; p < PAIRS; ++p) state[p][0] = state[p][1] = f4{};
-        if (OUT && w.first.p) {
-            const float* from = w.first.p + number * w.dk * w.dv;
-            each([&](int r, int c, int p, int y, int e) {
-                state[p][y][e] = from[r * w.first.row + c * w.first.col];
-            });
-        }
-
-        Fetch<T, CH, DK, THREADS> fq, fk;
-        Fetch<T, CH, COLS, THREADS> fv;
-        float decay;
-        const auto fetch = [&](int base) {
-            fk.load(w, pk, w.k.step, w.dk, base, live, len);
-            fv.load(w, pv, w.v.step, w.dv - c0, base, live, len);
-            if constexpr (OUT) fq.load(w, pq, w.q.step, w.dk, base, live, len);
-            if (wave == 0)
-                decay = lane < CH && base + lane < live ? walk_decay(w, b, h, base + lane, len) : 0.0f;
-        };
         const auto put_dots = [&](int base) {
             if (tid >= CH || base + tid >= live) return;
             float sum = 0.0f;
 #pragma unroll
-            for (int i = 0; i < WAVES; ++i) sum += s.dots[i][tid];
+            for (int i = 0; i < WAVES; ++i) sum += s.dot(i, tid);
             const int t = walk_token(w, base + tid, len);
             w.dots[(((int64_t)block * w.batch + b) * w.steps + t) * w.heads + h] = sum;
         };
 
+        // The lane's outputs: 4 columns of token n of every tile of 16.
+        const int c = c0 + wave * 16 + 4 * g, count = w.dv - c;
+        const int64_t row_step = (int64_t)way * w.heads * w.dv;
+        int64_t to = (((int64_t)b * w.steps + first) * w.heads + h) * w.dv + c + n * row_step;
+        const T* pe = nullptr;
+        if constexpr (DOTS) pe = side(w.e, first) + c + n * way * w.e.step;
+
         double total = 0.0;
-        if (start < live) fetch(start);
         for (int base = start; base < live; base += CH) {
             __syncthreads();  // the last chunk's tiles are read
-            if (OUT && w.dots && base > start) put_dots(base - CH);
+            if (DOTS && base > start) put_dots(base - CH);
             fk.store(s.k);
             fv.store(s.v);
             if constexpr (OUT) fq.store(s.q);
             if (wave == 0) {
-                const double c = running_sum(decay, lane), last = __shfl(c, CH - 1);
+                const double sum = running_sum(decay), last = lane_value(sum, CH - 1);
                 if (lane < CH) {
-                    s.c[lane] = c;
-                    s.in[lane] = exp2_fast((float)c) * w.outer;
-                    s.left[lane] = exp2_fast((float)(last - c)) * w.inner;
+                    const float high = high_part(sum);
+                    s.c[lane] = float2{high, (float)(sum - high)};
+                    s.in[lane] = exp2_fast((float)sum) * w.outer;
+                    s.left[lane] = exp2_fast((float)(last - sum)) * w.inner;
                 }
                 total += last;
                 if (lane == 0) s.whole = exp2_fast((float)last);
@@ -415,14 +502,12 @@ struct Kernel {
                 }
 #pragma unroll
                 for (int row = 0; row < TILES; ++row) {
-                    const int place = base + 16 * row + n, c = c0 + wave * 16 + 4 * g;
                     float dot = 0.0f;
-                    if (place < live && c < w.dv) {
-                        const int t = walk_token(w, place, len), count = w.dv - c;
-                        const int64_t to = (((int64_t)b * w.steps + t) * w.heads + h) * w.dv + c;
-                        if (w.dots) {
+                    const int64_t here = to + 16 * row * row_step;
+                    if (base + 16 * row + n < live && count > 0) {
+                        if constexpr (DOTS) {
                             Pack<T, 4> e;
-                            e.load(side(w.e) + t * w.e.step + c, count);
+                            e.load(pe + 16 * row * way * w.e.step, count);
 #pragma unroll
                             for (int y = 0; y < 4; ++y)
                                 if (y < count) dot = __builtin_fmaf(o[row][y], to_f32(e.v[y]), dot);
@@ -431,88 +516,88 @@ struct Kernel {
                             Pack<float, 4> r;
 #pragma unroll
                             for (int y = 0; y < 4; ++y) r.v[y] = o[row][y];
-                            r.store((float*)w.out + to, count);
+                            r.store((float*)w.out + here, count);
                         } else {
                             Pack<T, 4> r;
 #pragma unroll
                             for (int y = 0; y < 4; ++y) r.v[y] = from_f32<T>(o[row][y]);
-                            r.store((T*)w.out + to, count);
+                            r.store((T*)w.out + here, count);
                         }
                     }
-                    if (w.dots) {
+                    if constexpr (DOTS) {
                         dot += __shfl_xor(dot, 16);
                         dot += __shfl_xor(dot, 32);
-                        if (g == 0) s.dots[wave][16 * row + n] = dot;
+                        if (g == 0) s.dot(wave, 16 * row + n) = dot;
                     }
                 }
+                to += CH * row_step;
+                if constexpr (DOTS) pe += CH * way * w.e.step;
             }
 
             // the state behind the chunk
             const float whole = s.whole;
-            Frag<3> vw[STEPS];
+#pragma unroll
+            for (int p = 0; p < PAIRS; ++p) state[p][0] *= whole, state[p][1] *= whole;
 #pragma unroll
             for (int step = 0; step < STEPS; ++step) {
+                Frag<3> vw;
                 float r[8];
 #pragma unroll
                 for (int e = 0; e < 8; ++e) r[e] = v[step].value(e) * s.left[32 * step + 8 * g + e];
-                vw[step].from(r);
-            }
+                vw.from(r);
 #pragma unroll
-            for (int p = 0; p < PAIRS; ++p)
+                for (int p = 0; p < PAIRS; ++p)
 #pragma unroll
-                for (int y = 0; y < 2; ++y) {
-                    state[p][y] *= whole;
-#pragma unroll
-                    for (int step = 0; step < STEPS; ++step)
+                    for (int y = 0; y < 2; ++y)
                         mma<3>(state[p][y],
-                               s.k.down(32 * step, 32 * p + 8 * (lane % 4) + 4 * y, lane),
-                               vw[step]);
-                }
+                               s.k.down(32 * step, 32 * p + 8 * (lane % 4) + 4 * y, lane), vw);
+            }
         }
-        if (OUT && w.dots && live > start) {
+        if (DOTS && live > start) {
             __syncthreads();
             put_dots(start + (live - start - 1) / CH * CH);
         }
-        if (w.last.p && (!OUT || w.pieces == 1)) {
-            float* to = w.last.p + number * w.dk * w.dv;
-            each([&](int r, int c, int p, int y, int e) {
-                to[r * w.last.row + c * w.last.col] = state[p][y][e];
-            });
-        }
+        if (w.last.p && (!OUT || w.pieces == 1) && column < w.dv)
+            store_state(state, w.last.p + number * w.dk * w.dv, w, w.last, column, g);
         if (!OUT && block == 0 && tid == 0) w.whole[number] = exp2_fast((float)total);
     }
 };
 
-template <class T, int TP, int LIM, int DK, int WAVES, int CH, bool OUT>
-__global__ void __launch_bounds__(64 * WAVES, 2) k_walk(Walk w) {
-    using K = Kernel<T, TP, LIM, DK, WAVES, CH, OUT>;
+// Two workgroups share a CU's LDS and registers where they fit: their phases between
+// barriers hide each other's latencies.
+template <class K>
+constexpr int kPerSimd = 2;
+
+template <class K>
+__global__ void __launch_bounds__(K::THREADS, kPerSimd<K>) k_walk(Walk w) {
     __shared__ typename K::Shared s;
     K::run(w, s);
 }
 
 template <class T, int DK, int WAVES, int CH>
-hipError_t launch(const Walk& w, Grade grade, bool states, hipStream_t stream) {
+hipError_t launch(const Walk& w, bool states, hipStream_t stream) {
     constexpr int COLS = 16 * WAVES, THREADS = 64 * WAVES, NARROW = kTerms<T> == 3 ? 3 : 2;
     const int64_t grid = (int64_t)w.batch * w.heads * w.pieces * ((w.dv + COLS - 1) / COLS);
     if (grid == 0) return hipSuccess;
     if (states)
-        k_walk<T, 1, 3, DK, WAVES, CH, false><<<(uint32_t)grid, THREADS, 0, stream>>>(w);
-    else if (grade == Grade::Narrow)
-        k_walk<T, NARROW, NARROW, DK, WAVES, CH, true><<<(uint32_t)grid, THREADS, 0, stream>>>(w);
+        k_walk<Kernel<T, 1, 3, DK, WAVES, CH, false, false>><<<(uint32_t)grid, THREADS, 0, stream>>>(w);
+    else if (!w.dots)
+        k_walk<Kernel<T, NARROW, NARROW, DK, WAVES, CH, true, false>>
+            <<<(uint32_t)grid, THREADS, 0, stream>>>(w);
     else
-        k_walk<T, 3, 3, DK, WAVES, CH, true><<<(uint32_t)grid, THREADS, 0, stream>>>(w);
+        k_walk<Kernel<T, 3, 3, DK, WAVES, CH, true, true>><<<(uint32_t)grid, THREADS, 0, stream>>>(w);
     return hipGetLastError();
 }
 
 }  // namespace walk
 
 template <class T>
-hipError_t launch_walk(const Walk& w, Grade grade, bool states, hipStream_t stream) {
+hipError_t launch_walk(const Walk& w, bool states, hipStream_t stream) {
     constexpr int CH = walk::kTerms<T> == 1 ? 64 : 32;
     const bool wide = walk_columns(w.dk, w.dv) == 128;
     const auto by_width = [&](auto dk) {
-        return wide ? walk::launch<T, dk.value, 8, CH>(w, grade, states, stream)
-                    : walk::launch<T, dk.value, 4, CH>(w, grade, states, stream);
+        return wide ? walk::launch<T, dk.value, 8, CH>(w, states, stream)
+                    : walk::launch<T, dk.value, 4, CH>(w, states, stream);
     };
     if (w.dk > 128) return by_width(std::integral_constant<int, 256>());
     if (w.dk > 64) return by_width(std::integral_constant<int, 128>());
