@@ -6,90 +6,116 @@
 namespace ls {
 namespace {
 
-constexpr int kCols = 64;  // columns of a step's workgroup
+typedef float f4 __attribute__((ext_vector_type(4)));
 
-// Gradients by head, batch x steps x heads x width fp32, to those of the groups.
+// Gradients by head, batch x steps x heads x width fp32, to those of the groups: dq's
+// and dk's at once.
 template <class T>
-__global__ void __launch_bounds__(256) k_join_heads(const float* in, T* out, int64_t count, int per,
-                                                    int width) {
+__global__ void __launch_bounds__(256) k_join_heads(const float* dq_in, const float* dk_in, T* dq,
+                                                    T* dk, int64_t count, int per, int width) {
     const int64_t i = blockIdx.x * (int64_t)256 + threadIdx.x;
     if (i >= count) return;
-    const int64_t group = i / width, at = group * per * width + i % width;
+    const float* in = blockIdx.y ? dk_in : dq_in;
+    const int64_t at = i / width * per * width + i % width;
     float sum = 0.0f;
+#pragma unroll 4
     for (int j = 0; j < per; ++j) sum += in[at + (int64_t)j * width];
-    out[i] = from_f32<T>(sum);
+    (blockIdx.y ? dk : dq)[i] = from_f32<T>(sum);
+}
+
+// Sums over the workgroup's threads, in 64 bits: v becomes the sum over the threads
+// before this one (no difference of sums: a NaN of its own or behind it is not in it);
+// returns that of all.
+constexpr int kGateThreads = 256, kGateWaves = kGateThreads / 64;
+__device__ double block_scan(double& v, double* s) {
+    const int lane = threadIdx.x % 64, wave = threadIdx.x / 64;
+#pragma unroll
+    for (int m = 1; m < 64; m <<= 1) {
+        const double up = __shfl_up(v, m);
+        if (lane >= m) v += up;
+    }
+    if (lane == 63) s[wave] = v;
+    v = __shfl_up(v, 1);
+    if (lane == 0) v = 0.0;
+    __syncthreads();
+    double all = 0.0;
+#pragma unroll
+    for (int i = 0; i < kGateWaves; ++i) {
+        if (i == wave) v += all;
+        all += s[i];
+    }
+    __syncthreads();
+    return all;
 }
 
 // The decays' gradients: dg[t] = sum over s >= t of (q.dq - k.dk)[s], and the part
-// of the last state, <dS, S>.  A workgroup to a row and head.
-constexpr int kGateThreads = 256;
-__device__ double block_sum(double v, double* s) {
-    const int tid = threadIdx.x;
-    s[tid] = v;
-    __syncthreads();
-    for (int m = kGateThreads / 2; m > 0; m >>= 1) {
-        if (tid < m) s[tid] += s[tid + m];
-        __syncthreads();
-    }
-    const double r = s[0];
-    __syncthreads();
-    return r;
-}
-
-__global__ void __launch_bounds__(kGateThreads)
-    k_gates(Walk w, const float* dq_dots, int dq_blocks, const float* dk_dots, int dk_blocks,
-            const float* dstate_out, const float* last, int64_t state, float* out) {
-    __shared__ double s[kGateThreads];
+// of the last state, <dS, S>; and dS_0 = e^g[0] G[0], in place (a row without tokens
+// keeps dS).  A workgroup to a row and head; eight tokens to a thread.
+struct Gates {
+    const float* dq_dots;
+    const float* dk_dots;
+    int blocks;               // of dots
+    const float* dstate_out;  // and the last state, where it is given
+    const float* last;
+    int64_t state;  // elements of a state
+    float* dstate;  // nullable
+    float* out;
+};
+__global__ void __launch_bounds__(kGateThreads) k_gates(Walk w, Gates a) {
+    constexpr int PER = 8;
+    __shared__ double s[kGateWaves];
     const int h = blockIdx.x % w.heads, b = blockIdx.x / w.heads, tid = threadIdx.x;
     const int len = walk_len(w, b);
-    const int64_t all = (int64_t)w.batch * w.steps * w.heads;
+    const int64_t all = (int64_t)w.batch * w.steps * w.heads, own = blockIdx.x * a.state;
+    const float* g = w.g + b * w.g_batch + h;
     double carry = 0.0;
-    if (dstate_out) {
-        for (int64_t i = tid; i < state; i += kGateThreads)
-            carry += (double)dstate_out[blockIdx.x * state + i] * last[blockIdx.x * state + i];
-        carry = block_sum(carry, s);
+    if (a.dstate_out) {
+        for (int64_t i = tid; i < a.state; i += kGateThreads)
+            carry += (double)a.dstate_out[own + i] * a.last[own + i];
+        double before = carry;
+        carry = block_scan(before, s);
     }
-    for (int end = w.steps; end > 0; end -= kGateThreads) {
-        const int t = end - 1 - tid;  // thread 0 has the last token
-        double v = 0.0;
-        const int64_t at = ((int64_t)b * w.steps + t) * w.heads + h;
-        if (t >= 0 && t < len) {
-            for (int i = 0; i < dq_blocks; ++i) v += dq_dots[i * all + at];
-            for (int i = 0; i < dk_blocks; ++i) v -= dk_dots[i * all + at];
+    for (int end = w.steps; end > 0; end -= kGateThreads * PER) {
+        const int t0 = end - 1 - tid * PER;  // thread 0 has the last tokens
+        const int64_t at = ((int64_t)b * w.steps + t0) * w.heads + h;
+        double v[PER], sum = 0.0;
+#pragma unroll
+        for (int i = 0; i < PER; ++i) {
+            v[i] = 0.0;
+            if (t0 - i >= 0 && t0 - i < len)
+                for (int k = 0; k < a.blocks; ++k)
+                    v[i] += (double)a.dq_dots[k * all + at - (int64_t)i * w.heads] -
+                            a.dk_dots[k * all + at - (int64_t)i * w.heads];
         }
-        s[tid] = v;
-        __syncthreads();
-        for (int m = 1; m < kGateThreads; m <<= 1) {
-            const double more = tid >= m ? s[tid - m] : 0.0;
-            __syncthreads();
-            s[tid] += more;
-            __syncthreads();
+#pragma unroll
+        for (int i = 0; i < PER; ++i) v[i] = sum += v[i];
+        const double more = block_scan(sum, s);
+#pragma unroll
+        for (int i = 0; i < PER; ++i) {
+            const int t = t0 - i;
+            if (t < 0) break;
+            // a decay of -infinity leaves nothing to change
+            a.out[at - (int64_t)i * w.heads] =
+                t < len && g[t * w.g_step] != -__builtin_inff()
+                    ? (float)(carry + sum + v[i]) : 0.0f;
         }
-        // a decay of -infinity leaves nothing to change
-        if (t >= 0)
-            out[at] = t < len && w.g[b * w.g_batch + t * w.g_step + h] != -__builtin_inff()
-                          ? (float)(carry + s[tid]) : 0.0f;
-        carry += s[kGateThreads - 1];
-        __syncthreads();
+        carry += more;
+    }
+    if (a.dstate && len > 0) {
+        const float decay = exp2_fast(g[0] * kLog2e);
+        for (int64_t i = tid; i < a.state; i += kGateThreads) a.dstate[own + i] *= decay;
     }
 }
 
 // One decay for all tokens of a head: the sum of their gradients.
 __global__ void __launch_bounds__(kGateThreads) k_gate_sum(const float* in, float* out,
                                                            int64_t tokens, int heads) {
-    __shared__ double s[kGateThreads];
+    __shared__ double s[kGateWaves];
     double v = 0.0;
+#pragma unroll 8
     for (int64_t i = threadIdx.x; i < tokens; i += kGateThreads) v += in[i * heads + blockIdx.x];
-    v = block_sum(v, s);
+    v = block_scan(v, s);
     if (threadIdx.x == 0) out[blockIdx.x] = (float)v;
-}
-
-// dS_0 = e^g[0] G[0], in place; a row without tokens keeps dS.
-__global__ void __launch_bounds__(256) k_first_decay(Walk w, float* state, int64_t each) {
-    const int h = blockIdx.x % w.heads, b = blockIdx.x / w.heads;
-    if (walk_len(w, b) == 0) return;
-    const float a = exp2_fast(w.g[b * w.g_batch + h] * kLog2e);
-    for (int64_t i = threadIdx.x; i < each; i += 256) state[blockIdx.x * each + i] *= a;
 }
 
 // The states before every piece from what each adds, in place: a workgroup to 256
@@ -113,35 +139,71 @@ __global__ void __launch_bounds__(256)
 
 // ------------------------------------------------ a single token
 
-// A workgroup to 64 columns of a row's head.
+// A workgroup to `cols` columns (a multiple of 4) of a row's head: a thread has four
+// columns of every `down`-th row, and the threads of a column add up what they have of
+// the output.  Bound by the state's bytes, read and written once.
+constexpr int kStepThreads = 256;
 template <class T>
-__global__ void __launch_bounds__(kCols)
-    k_attend_step(libscan_attend p, float* states, int64_t n_states, const int32_t* slots, T* y) {
-    const int blocks = ((int)p.dv + kCols - 1) / kCols;
+__global__ void __launch_bounds__(kStepThreads)
+    k_attend_step(libscan_attend p, float* states, int64_t n_states, const int32_t* slots, T* y,
+                  int cols) {
+    constexpr int AHEAD = 8;
+    __shared__ float s_q[256], s_k[256];
+    __shared__ f4 s_out[kStepThreads];
+    const int dk = (int)p.dk, dv = (int)p.dv, heads = (int)p.heads;
+    const int blocks = (dv + cols - 1) / cols;
     const int block = blockIdx.x % blocks, bh = blockIdx.x / blocks;
-    const int h = bh % (int)p.heads, b = bh / (int)p.heads;
-    const int c = block * kCols + threadIdx.x;
-    if (c >= p.dv) return;
-    T* out = y + (int64_t)bh * p.dv + c;
+    const int h = bh % heads, b = bh / heads, tid = threadIdx.x;
+    const int across = cols / 4, down = kStepThreads / across;
+    const int c = block * cols + tid % across * 4, row = tid / across, count = dv - c;
     const int64_t slot = slots ? slots[b] : b;
-    if (slot < 0 || slot >= n_states) {
-        *out = T(0);
-        return;
+    const bool held = slot >= 0 && slot < n_states;
+    const bool on = held && row < down && count > 0;
+    const int share = heads / (int)p.groups;
+    float g = p.fixed ? p.log_decay[h] : p.log_decay[b * p.decay_batch + h];
+    f4 v{}, o{};
+    if (on) {
+        Pack<T, 4> x;
+        x.load((const T*)p.v + b * p.v_batch + h * p.v_head + c, count);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v[e] = to_f32(x.v[e]);
     }
-    const int share = (int)(p.heads / p.groups);
-    const T* q = (const T*)p.q + b * p.q_batch + (h / share) * p.q_head;
-    const T* k = (const T*)p.k + b * p.k_batch + (h / share) * p.k_head;
-    const float v = to_f32(((const T*)p.v + b * p.v_batch + h * p.v_head)[c]);
-    const float g = p.fixed ? p.log_decay[h] : p.log_decay[b * p.decay_batch + h];
-    const float a = exp2_fast(g * kLog2e);
-    float* s = states + (slot * p.heads + h) * p.dk * p.dv + c;
-    float o = 0.0f;
-    for (int r = 0; r < p.dk; ++r) {
-        const float x = __builtin_fmaf(to_f32(k[r]), v, a * s[r * p.dv]);
-        s[r * p.dv] = x;
-        o = __builtin_fmaf(to_f32(q[r]), x, o);
+    for (int r = tid; r < dk; r += kStepThreads) {
+        s_q[r] = to_f32(((const T*)p.q + b * p.q_batch + (h / share) * p.q_head)[r]);
+        s_k[r] = to_f32(((const T*)p.k + b * p.k_batch + (h / share) * p.k_head)[r]);
     }
-    *out = from_f32<T>(o * (float)p.scale);
+    __syncthreads();
+    if (on) {
+        const float a = exp2_fast(g * kLog2e);
+        float* s = states + ((slot * heads + h) * dk + row) * dv + c;
+        const int64_t step = (int64_t)down * dv;
+        for (int r = row; r < dk; r += AHEAD * down, s += AHEAD * step) {
+            Pack<float, 4> x[AHEAD];
+#pragma unroll
+            for (int i = 0; i < AHEAD; ++i)
+                if (r + i * down < dk) x[i].load(s + i * step, count);
+#pragma unroll
+            for (int i = 0; i < AHEAD; ++i) {
+                if (r + i * down >= dk) break;
+                const float k = s_k[r + i * down], q = s_q[r + i * down];
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    x[i].v[e] = __builtin_fmaf(k, v[e], a * x[i].v[e]);
+                    o[e] = __builtin_fmaf(q, x[i].v[e], o[e]);
+                }
+                x[i].store(s + i * step, count);
+            }
+        }
+    }
+    s_out[tid] = o;
+    __syncthreads();
+    if (row == 0 && count > 0) {
+        for (int i = 1; i < down; ++i) o += s_out[tid + i * across];
+        Pack<T, 4> out;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) out.v[e] = from_f32<T>(held ? o[e] * (float)p.scale : 0.0f);
+        out.store(y + (int64_t)bh * dv + c, count);
+    }
 }
 
 // ------------------------------------------------ launches
@@ -173,17 +235,34 @@ WalkSide side_k(const libscan_attend& p) {
 WalkSide side_v(const libscan_attend& p) { return {p.v, p.v_batch, p.v_step, p.v_head, 1}; }
 
 // Rows are cut into pieces where they alone do not fill the GPU: a first run over k and
-// v gives what each piece adds to the state.
+// v gives what each piece adds to the state.  More pieces make for more workgroups and a
+// longer carry, which reads and writes every piece's state.  The times that are weighed
+// up are those of 128 x 128 states in bf16, in units of 5 us: 512 workgroups (two to a CU) walk
+// n chunks of 64 tokens in 2 n + 1.5 and run for their states in 0.8 n + 1.4, 256 in 1.2 n
+// + 1.5 and 0.45 n + 1.3; the carry moves 4.6 TB/s; two launches take 1.
 struct Pieces {
     int count, places;
 };
 Pieces pieces(const libscan_attend& p) {
     const int64_t chunk = 64, chunks = (p.steps + chunk - 1) / chunk;
     const int64_t groups = p.batch * p.heads * walk_blocks((int)p.dk, (int)p.dv);
-    int64_t count = groups ? 512 / groups : 1;
-    if (count > chunks / 2) count = chunks / 2;
-    if (count < 2) return {1, (int)p.steps};
-    const int64_t each = (chunks + count - 1) / count;
+    const auto time = [](int64_t count, double full, double half) {
+        const int64_t left = count % 512;
+        return count / 512 * full + (left > 256 ? full : left ? half : 0.0);
+    };
+    const auto walk = [&](int64_t n, int64_t size) {
+        return time(groups * n, 2.0 * size + 1.5, 1.2 * size + 1.5);
+    };
+    int64_t each = chunks;
+    double best = walk(1, chunks);
+    for (int64_t n = 2; n <= chunks / 2 && groups * n <= 2048; ++n) {
+        const int64_t size = (chunks + n - 1) / n, count = (chunks + size - 1) / size;
+        const double cost = walk(count, size) +
+                            time(groups * count, 0.8 * size + 1.4, 0.45 * size + 1.3) +
+                            p.batch * p.heads * count * p.dk * p.dv * 8 / 4.6e6 / 5 + 1;
+        if (cost < best) best = cost, each = size;
+    }
+    if (each >= chunks) return {1, (int)p.steps};
     return {(int)((chunks + each - 1) / each), (int)(each * chunk)};
 }
 
@@ -318,24 +397,22 @@ hipError_t launch_attend_back(const libscan_attend& p, const void* dy, int64_t d
     if ((e = run(p.type, w, false, stream)) != hipSuccess) return e;
 
     const uint32_t rows = (uint32_t)(p.batch * p.heads);
-    const int64_t each = p.dk * p.dv;
     if (rows) {
-        k_gates<<<rows, kGateThreads, 0, stream>>>(
-            w, floats(plan.dq_dots), dots, floats(plan.dk_dots), dots, dstate_out, last, each,
-            p.fixed ? floats(plan.gates) : dlog_decay);
-        if (dstate && p.steps) k_first_decay<<<rows, 256, 0, stream>>>(w, dstate, each);
+        const Gates a{floats(plan.dq_dots), floats(plan.dk_dots), dots, dstate_out, last,
+                      p.dk * p.dv, p.steps ? dstate : nullptr,
+                      p.fixed ? floats(plan.gates) : dlog_decay};
+        k_gates<<<rows, kGateThreads, 0, stream>>>(w, a);
     }
     if (p.fixed && p.heads)
         k_gate_sum<<<(uint32_t)p.heads, kGateThreads, 0, stream>>>(
             floats(plan.gates), dlog_decay, p.batch * p.steps, (int)p.heads);
     const int64_t count = p.batch * p.steps * p.groups * p.dk;
     if (shared && count) {
-        const uint32_t grid = (uint32_t)((count + 255) / 256);
+        const dim3 grid((uint32_t)((count + 255) / 256), 2);
         const auto join = [&](auto zero) {
             using T = decltype(zero);
-            const int per = (int)(p.heads / p.groups);
-            k_join_heads<<<grid, 256, 0, stream>>>(floats(plan.dq), (T*)dq, count, per, (int)p.dk);
-            k_join_heads<<<grid, 256, 0, stream>>>(floats(plan.dk), (T*)dk, count, per, (int)p.dk);
+            k_join_heads<<<grid, 256, 0, stream>>>(floats(plan.dq), floats(plan.dk), (T*)dq, (T*)dk,
+                                                   count, (int)(p.heads / p.groups), (int)p.dk);
         };
         if (p.type == LIBSCAN_F32) join(float());
         else if (p.type == LIBSCAN_F16) join(_Float16());
@@ -346,14 +423,20 @@ hipError_t launch_attend_back(const libscan_attend& p, const void* dy, int64_t d
 
 hipError_t launch_attend_step(const libscan_attend& p, float* states, int64_t n_states,
                               const int32_t* slots, void* y, hipStream_t stream) {
-    const uint32_t grid = (uint32_t)(p.batch * p.heads * ((p.dv + kCols - 1) / kCols));
-    if (p.type == LIBSCAN_F32)
-        k_attend_step<float><<<grid, kCols, 0, stream>>>(p, states, n_states, slots, (float*)y);
-    else if (p.type == LIBSCAN_F16)
-        k_attend_step<_Float16><<<grid, kCols, 0, stream>>>(p, states, n_states, slots,
-                                                            (_Float16*)y);
-    else
-        k_attend_step<__bf16><<<grid, kCols, 0, stream>>>(p, states, n_states, slots, (__bf16*)y);
+    // whole rows of the state to a workgroup, where that makes enough of them: longer runs
+    // of bytes, fewer sums
+    const int64_t rows = p.batch * p.heads;
+    int64_t cols = (p.dv + 3) / 4 * 4;
+    while (cols > 16 && rows * ((p.dv + cols - 1) / cols) < 512) cols = (cols / 2 + 3) / 4 * 4;
+    const uint32_t grid = (uint32_t)(rows * ((p.dv + cols - 1) / cols));
+    const auto go = [&](auto zero) {
+        using T = decltype(zero);
+        k_attend_step<T><<<grid, kStepThreads, 0, stream>>>(p, states, n_states, slots, (T*)y,
+                                                            (int)cols);
+    };
+    if (p.type == LIBSCAN_F32) go(float());
+    else if (p.type == LIBSCAN_F16) go(_Float16());
+    else go(__bf16());
     return hipGetLastError();
 }
 

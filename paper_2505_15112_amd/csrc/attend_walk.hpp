@@ -1,6 +1,6 @@
 // attend_walk.hpp -- the walk of linear attention (attend.hpp) on the matrix cores.
 //
-// A workgroup takes a row's head in chunks of CH tokens.  With c the running sum of
+// A workgroup takes a row's head in chunks of kChunk tokens.  With c the running sum of
 // the decays' logarithms inside the chunk and S the state before it,
 //   o[i] = e^c[i] q[i] S + sum over j <= i of (q[i] . k[j]) e^(c[i] - c[j]) v[j],
 //   S' = e^c[last] S + sum over j of k[j] (e^(c[last] - c[j]) v[j])^T:
@@ -70,9 +70,9 @@ struct Frag {
             t[i] = __builtin_bit_cast(bf8, u4{u[i][0], u[i][1], u[i][2], u[i][3]});
     }
     __device__ __forceinline__ float value(int e) const {
-        float v = 0.0f;
+        float v = (float)t[TERMS - 1][e];
 #pragma unroll
-        for (int i = TERMS - 1; i >= 0; --i) v += (float)t[i][e];
+        for (int i = TERMS - 2; i >= 0; --i) v += (float)t[i][e];
         return v;
     }
 };
@@ -234,16 +234,19 @@ __device__ __forceinline__ float high_part(double c) {
     return (float)(__builtin_rint(c * 256.0) * (1.0 / 256.0));
 }
 
+// Tokens of a chunk: as many as one matrix instruction sums over.  64 make the states'
+// part of the work half as large, but leave room for one workgroup on a CU, not two (4 x
+// 2048 x 16 x 128 x 128, bf16: 50 us a walk against 45).
+constexpr int kChunk = 32;
+
 // TP terms of scores and states, LIM for the products that make outputs, DK the
-// width of q and k rounded up, WAVES of 16 columns of v each, CH tokens to a chunk.
-// OUT: with outputs; else the pieces' states alone.  DOTS: with the sums of the
+// width of q and k rounded up, WAVES of 16 columns of v each.  OUT: with outputs; else the pieces' states alone.  DOTS: with the sums of the
 // outputs times e.
-template <class T, int TP, int LIM, int DK, int WAVES_, int CH, bool OUT, bool DOTS>
+template <class T, int TP, int LIM, int DK, int WAVES_, bool OUT, bool DOTS>
 struct Kernel {
     static constexpr int WAVES = WAVES_, COLS = 16 * WAVES, THREADS = 64 * WAVES;
     static constexpr int TERMS = kTerms<T>;
-    static constexpr int STEPS = CH / 32, TILES = CH / 16, PAIRS = DK / 32;
-    static constexpr int DIAGONALS = TILES * (TILES + 1) / 2;
+    static constexpr int CH = kChunk, PAIRS = DK / 32;
     struct Shared {
         Tile<TERMS, CH, DK, DK == 64 ? 16 : 24> k;
         Tile<TERMS, CH, COLS, 8> v;
@@ -260,61 +263,48 @@ struct Kernel {
         }
     };
 
-    // Scores of the tiles on and below the diagonal, shared out over the waves: lane l
-    // gets those of token l % 16 with four others, next to each other in a row.
+    // Scores of 16 x 16 tokens, of the three such tiles on and below the diagonal the one
+    // of this wave: lane l gets those of token l % 16 with four others, next to each other
+    // in a row.
     static __device__ __forceinline__ void scores(Shared& s, float factor, int wave, int lane) {
-        const int g = lane / 16, n = lane % 16;
+        if (wave >= 3) return;
+        const int g = lane / 16, n = lane % 16, row = wave > 0, col = wave > 1;
+        f4 acc{};
 #pragma unroll
-        for (int x = 0; x < (DIAGONALS + WAVES - 1) / WAVES; ++x) {
-            const int at = x * WAVES + wave;
-            if (at >= DIAGONALS) break;
-            // the tile's place in the lower triangle
-            const int row = at < 1 ? 0 : at < 3 ? 1 : at < 6 ? 2 : 3, col = at - row * (row + 1) / 2;
-            f4 acc{};
+        for (int p = 0; p < PAIRS; ++p)
+            mma<LIM>(acc, s.k.along(16 * col + n, 32 * p + 8 * g),
+                     s.q.along(16 * row + n, 32 * p + 8 * g));
+        const int i = 16 * row + n, j = 16 * col + 4 * g;
+        const float2 ci = s.c[i];
+        float v[4];
 #pragma unroll
-            for (int p = 0; p < PAIRS; ++p)
-                mma<LIM>(acc, s.k.along(16 * col + n, 32 * p + 8 * g),
-                         s.q.along(16 * row + n, 32 * p + 8 * g));
-            const int i = 16 * row + n, j = 16 * col + 4 * g;
-            const float2 ci = s.c[i];
-            float v[4];
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                const float2 cj = s.c[j + e];
-                const float d = exp2_fast((ci.x - cj.x) + (ci.y - cj.y)) * factor;
-                v[e] = j + e <= i ? acc[e] * d : 0.0f;
-            }
-            unsigned u[TP][2];
-            split<TP, 4>(v, u);
-#pragma unroll
-            for (int t = 0; t < TP; ++t)
-                *reinterpret_cast<u2*>(&s.p.v[t][i][j]) = u2{u[t][0], u[t][1]};
+        for (int e = 0; e < 4; ++e) {
+            const float2 cj = s.c[j + e];
+            const float d = exp2_fast((ci.x - cj.x) + (ci.y - cj.y)) * factor;
+            v[e] = j + e <= i ? acc[e] * d : 0.0f;
         }
+        unsigned u[TP][2];
+        split<TP, 4>(v, u);
+#pragma unroll
+        for (int t = 0; t < TP; ++t)
+            *reinterpret_cast<u2*>(&s.p.v[t][i][j]) = u2{u[t][0], u[t][1]};
     }
 
     // o += the scores times v where v has an infinity or a NaN: such an element
     // counts for its own token and later ones alone (0 times it is not 0).
-    static __device__ __forceinline__ void careful(const Shared& s, f4 (&o)[TILES],
-                                                   const Frag<TERMS> (&v)[STEPS], int wave,
-                                                   int lane) {
+    static __device__ __forceinline__ void careful(const Shared& s, f4 (&o)[2],
+                                                   const Frag<TERMS>& v, int wave, int lane) {
         const int g = lane / 16, n = lane % 16;
+        Frag<TERMS> clean;
 #pragma unroll
-        for (int step = 0; step < STEPS; ++step) {
-            Frag<TERMS> clean;
+        for (int e = 0; e < 8; ++e) {
+            const bool fine = __builtin_isfinite(v.value(e));
 #pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                const bool fine = __builtin_isfinite(v[step].value(e));
-#pragma unroll
-                for (int t = 0; t < TERMS; ++t)
-                    clean.t[t][e] = fine ? v[step].t[t][e] : (__bf16)0.0f;
-            }
-#pragma unroll
-            for (int row = 0; row < TILES; ++row)
-                if (32 * step <= 16 * row)
-                    mma<LIM>(o[row], clean, s.p.along(16 * row + n, 32 * step + 8 * g));
+            for (int t = 0; t < TERMS; ++t) clean.t[t][e] = fine ? v.t[t][e] : (__bf16)0.0f;
         }
 #pragma unroll
-        for (int row = 0; row < TILES; ++row)
+        for (int row = 0; row < 2; ++row) {
+            mma<LIM>(o[row], clean, s.p.along(16 * row + n, 8 * g));
             for (int j = 0; j <= 16 * row + n; ++j) {
                 float p = 0.0f;
 #pragma unroll
@@ -328,6 +318,7 @@ struct Kernel {
                     if (!__builtin_isfinite(value)) o[row][e] += p * value;
                 }
             }
+        }
     }
 
     // Element (r, c) of a state, from its address and strides: the lane's eight rows of
@@ -459,16 +450,11 @@ struct Kernel {
             __syncthreads();
             if (base + CH < live) fetch(base + CH);
 
-            Frag<TERMS> v[STEPS];
-#pragma unroll
-            for (int step = 0; step < STEPS; ++step)
-                v[step] = s.v.down(32 * step, wave * 16 + 4 * (lane % 4), lane);
+            const Frag<TERMS> v = s.v.down(0, wave * 16 + 4 * (lane % 4), lane);
 
             if constexpr (OUT) {
                 scores(s, w.inner * w.outer, wave, lane);
-                f4 o[TILES];
-#pragma unroll
-                for (int row = 0; row < TILES; ++row) o[row] = f4{};
+                f4 o[2]{};
 #pragma unroll
                 for (int p = 0; p < PAIRS; ++p) {
                     const f4 lo = state[p][0], hi = state[p][1];
@@ -476,32 +462,26 @@ struct Kernel {
                     Frag<TP> f;
                     f.from(r);
 #pragma unroll
-                    for (int row = 0; row < TILES; ++row)
+                    for (int row = 0; row < 2; ++row)
                         mma<LIM>(o[row], f, s.q.along(16 * row + n, 32 * p + 8 * g));
                 }
 #pragma unroll
-                for (int row = 0; row < TILES; ++row) o[row] *= s.in[16 * row + n];
+                for (int row = 0; row < 2; ++row) o[row] *= s.in[16 * row + n];
                 // 0 times a finite v adds up to 0
-                f4 zero{};
-#pragma unroll
-                for (int step = 0; step < STEPS; ++step)
-                    zero = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v[step].t[0], bf8{}, zero, 0, 0, 0);
+                const f4 zero =
+                    __builtin_amdgcn_mfma_f32_16x16x32_bf16(v.t[0], bf8{}, f4{}, 0, 0, 0);
                 const bool fine =
                     __all(zero[0] == 0.0f && zero[1] == 0.0f && zero[2] == 0.0f && zero[3] == 0.0f);
                 __syncthreads();  // the scores are written
                 if (fine) {
 #pragma unroll
-                    for (int row = 0; row < TILES; ++row)
-#pragma unroll
-                        for (int step = 0; step < STEPS; ++step)
-                            if (32 * step <= 16 * row)
-                                mma<LIM>(o[row], v[step],
-                                         s.p.along(16 * row + n, 32 * step + 8 * g));
+                    for (int row = 0; row < 2; ++row)
+                        mma<LIM>(o[row], v, s.p.along(16 * row + n, 8 * g));
                 } else {
                     careful(s, o, v, wave, lane);
                 }
 #pragma unroll
-                for (int row = 0; row < TILES; ++row) {
+                for (int row = 0; row < 2; ++row) {
                     float dot = 0.0f;
                     const int64_t here = to + 16 * row * row_step;
                     if (base + 16 * row + n < live && count > 0) {
@@ -538,20 +518,16 @@ struct Kernel {
             const float whole = s.whole;
 #pragma unroll
             for (int p = 0; p < PAIRS; ++p) state[p][0] *= whole, state[p][1] *= whole;
+            Frag<3> vw;
+            float r[8];
 #pragma unroll
-            for (int step = 0; step < STEPS; ++step) {
-                Frag<3> vw;
-                float r[8];
+            for (int e = 0; e < 8; ++e) r[e] = v.value(e) * s.left[8 * g + e];
+            vw.from(r);
 #pragma unroll
-                for (int e = 0; e < 8; ++e) r[e] = v[step].value(e) * s.left[32 * step + 8 * g + e];
-                vw.from(r);
+            for (int p = 0; p < PAIRS; ++p)
 #pragma unroll
-                for (int p = 0; p < PAIRS; ++p)
-#pragma unroll
-                    for (int y = 0; y < 2; ++y)
-                        mma<3>(state[p][y],
-                               s.k.down(32 * step, 32 * p + 8 * (lane % 4) + 4 * y, lane), vw);
-            }
+                for (int y = 0; y < 2; ++y)
+                    mma<3>(state[p][y], s.k.down(0, 32 * p + 8 * (lane % 4) + 4 * y, lane), vw);
         }
         if (DOTS && live > start) {
             __syncthreads();
@@ -563,10 +539,10 @@ struct Kernel {
     }
 };
 
-// Two workgroups share a CU's LDS and registers where they fit: their phases between
-// barriers hide each other's latencies.
+// Where two workgroups of eight waves fit a CU they hide each other's latencies between
+// barriers; that takes no more than 128 registers.
 template <class K>
-constexpr int kPerSimd = 2;
+constexpr int kPerSimd = K::PAIRS * K::TERMS <= 4 ? K::WAVES / 2 : 2;
 
 template <class K>
 __global__ void __launch_bounds__(K::THREADS, kPerSimd<K>) k_walk(Walk w) {
@@ -574,18 +550,18 @@ __global__ void __launch_bounds__(K::THREADS, kPerSimd<K>) k_walk(Walk w) {
     K::run(w, s);
 }
 
-template <class T, int DK, int WAVES, int CH>
+template <class T, int DK, int WAVES>
 hipError_t launch(const Walk& w, bool states, hipStream_t stream) {
     constexpr int COLS = 16 * WAVES, THREADS = 64 * WAVES, NARROW = kTerms<T> == 3 ? 3 : 2;
     const int64_t grid = (int64_t)w.batch * w.heads * w.pieces * ((w.dv + COLS - 1) / COLS);
     if (grid == 0) return hipSuccess;
     if (states)
-        k_walk<Kernel<T, 1, 3, DK, WAVES, CH, false, false>><<<(uint32_t)grid, THREADS, 0, stream>>>(w);
+        k_walk<Kernel<T, 1, 3, DK, WAVES, false, false>><<<(uint32_t)grid, THREADS, 0, stream>>>(w);
     else if (!w.dots)
-        k_walk<Kernel<T, NARROW, NARROW, DK, WAVES, CH, true, false>>
+        k_walk<Kernel<T, NARROW, NARROW, DK, WAVES, true, false>>
             <<<(uint32_t)grid, THREADS, 0, stream>>>(w);
     else
-        k_walk<Kernel<T, 3, 3, DK, WAVES, CH, true, true>><<<(uint32_t)grid, THREADS, 0, stream>>>(w);
+        k_walk<Kernel<T, 3, 3, DK, WAVES, true, true>><<<(uint32_t)grid, THREADS, 0, stream>>>(w);
     return hipGetLastError();
 }
 
@@ -593,11 +569,10 @@ hipError_t launch(const Walk& w, bool states, hipStream_t stream) {
 
 template <class T>
 hipError_t launch_walk(const Walk& w, bool states, hipStream_t stream) {
-    constexpr int CH = walk::kTerms<T> == 1 ? 64 : 32;
     const bool wide = walk_columns(w.dk, w.dv) == 128;
     const auto by_width = [&](auto dk) {
-        return wide ? walk::launch<T, dk.value, 8, CH>(w, states, stream)
-                    : walk::launch<T, dk.value, 4, CH>(w, states, stream);
+        return wide ? walk::launch<T, dk.value, 8>(w, states, stream)
+                    : walk::launch<T, dk.value, 4>(w, states, stream);
     };
     if (w.dk > 128) return by_width(std::integral_constant<int, 256>());
     if (w.dk > 64) return by_width(std::integral_constant<int, 128>());
