@@ -5,73 +5,132 @@
 // w = dy weight and xhat = (x - mean) rstd,
 //   dx = rstd (w - mean(w) - xhat mean(w xhat)) + dsum,
 //   dweight = sum over rows of dy xhat, dbias = sum over rows of dy.
+#include <type_traits>
+
 #include "launch.hpp"
 #include "lm.hpp"
 
 namespace ls {
 namespace {
 
-constexpr int kThreads = 256;
+// A lane's vector of 16 bytes of T.
+template <class T>
+constexpr int kVec = 16 / sizeof(T);
 
-__device__ __forceinline__ float block_sum(float v, float* s) {
+// Keeps what was computed from a vector from being held until later uses: it is computed
+// again from the 4 registers of the vector.
+template <class P>
+__device__ __forceinline__ void forget(P& x) {
+    if constexpr (sizeof(P) == 16) {
+        typedef unsigned U __attribute__((ext_vector_type(4)));
+        U u = __builtin_bit_cast(U, x.v);
+        asm volatile("" : "+v"(u));
+        x.v = __builtin_bit_cast(decltype(x.v), u);
+    }
+}
+
+// Sums over the LANES threads of a team (a power of two; a workgroup's teams all call).
+template <int LANES>
+__device__ __forceinline__ float team_sum(float v, float* s) {
 #pragma unroll
-    for (int m = 32; m > 0; m >>= 1) v += __shfl_xor(v, m);
-    __syncthreads();
-    if (threadIdx.x % 64 == 0) s[threadIdx.x / 64] = v;
-    __syncthreads();
-    v = 0.0f;
+    for (int m = (LANES < 64 ? LANES : 64) / 2; m > 0; m >>= 1) v += __shfl_xor(v, m);
+    if constexpr (LANES > 64) {
+        constexpr int WAVES = LANES / 64;
+        float* mine = s + threadIdx.x / LANES * WAVES;
+        __syncthreads();  // the last sum is read
+        if (threadIdx.x % 64 == 0) mine[threadIdx.x % LANES / 64] = v;
+        __syncthreads();
+        v = mine[0];
 #pragma unroll
-    for (int i = 0; i < kThreads / 64; ++i) v += s[i];
+        for (int i = 1; i < WAVES; ++i) v += mine[i];
+    }
     return v;
 }
 
-// The workgroup's row and group.
-struct Place {
-    int64_t row, x, residual;
-    int c0, per;
-};
-__device__ __forceinline__ Place place(const libscan_norm& p) {
-    Place r;
-    r.row = blockIdx.x / p.groups;
-    r.per = (int)(p.dim / p.groups);
-    r.c0 = (int)(blockIdx.x % p.groups) * r.per;
-    const int64_t b = r.row / p.steps, t = r.row % p.steps;
-    r.x = b * p.x_batch + t * p.x_step + r.c0;
-    r.residual = b * p.residual_batch + t * p.residual_step + r.c0;
-    return r;
+// Row `row`'s elements of a batch x steps x dim operand.
+__device__ __forceinline__ int64_t row_at(const libscan_norm& p, int64_t row, int64_t batch,
+                                          int64_t step) {
+    if (p.batch == 1) return row * step;
+    return row / p.steps * batch + row % p.steps * step;
 }
 
-template <class T, class W>
-__global__ void __launch_bounds__(kThreads) k_norm(libscan_norm p, T* y, T* sum, float* stats) {
-    __shared__ float s[kThreads / 64];
-    const Place at = place(p);
-    const T* x = (const T*)p.x + at.x;
-    const T* res = p.residual ? (const T*)p.residual + at.residual : nullptr;
-    const auto value = [&](int c) {
-        const float v = to_f32(x[c]);
-        return res ? to_f32(from_f32<T>(v + to_f32(res[c]))) : v;
-    };
-    float mean = 0.0f, var = 0.0f;
-    for (int c = threadIdx.x; c < at.per; c += kThreads) mean += value(c);
-    mean = block_sum(mean, s) / at.per;
-    for (int c = threadIdx.x; c < at.per; c += kThreads) {
-        const float d = value(c) - mean;
-        var = __builtin_fmaf(d, d, var);
+// A vector of weights or biases, as they are stored; `fill` where there are none.
+template <class W, int V>
+__device__ __forceinline__ Pack<W, V> load_weights(const void* w, int at, int count, float fill) {
+    Pack<W, V> x;
+    if (w) {
+        x.load((const W*)w + at, count);
+    } else {
+#pragma unroll
+        for (int e = 0; e < V; ++e) x.v[e] = from_f32<W>(fill);
     }
-    var = block_sum(var, s) / at.per;
-    const float rstd = 1.0f / __builtin_sqrtf(var + (float)p.eps);
-    const int64_t out = at.row * p.dim + at.c0;
-    for (int c = threadIdx.x; c < at.per; c += kThreads) {
-        const float v = value(c);
-        float n = (v - mean) * rstd;
-        if (p.weight) n *= to_f32(((const W*)p.weight)[at.c0 + c]);
-        if (p.bias) n += to_f32(((const W*)p.bias)[at.c0 + c]);
-        if (sum) sum[out + c] = from_f32<T>(v);
-        y[out + c] = from_f32<T>(n);
-    }
-    if (stats && threadIdx.x == 0) {
-        stats[2 * (int64_t)blockIdx.x] = mean;
-        stats[2 * (int64_t)blockIdx.x + 1] = rstd;
+    return x;
+}
+
+// ------------------------------------------------ rows in registers
+
+// A team of LANES threads to a group of a row, with NV vectors a thread: one read of the
+// row, the mean, then the sum of the squared differences.
+constexpr int kFrontThreads = 256;
+template <class T, class W, int LANES, int NV>
+__global__ void __launch_bounds__(LANES > kFrontThreads ? LANES : kFrontThreads)
+    k_norm(libscan_norm p, T* y, T* sum, float* stats) {
+    constexpr int V = kVec<T>, THREADS = LANES > kFrontThreads ? LANES : kFrontThreads;
+    constexpr int TEAMS = THREADS / LANES;
+    __shared__ float s[THREADS / 64];
+    const int lane = threadIdx.x % LANES, per = (int)(p.dim / p.groups);
+    const int64_t all = p.batch * p.steps * p.groups;
+    for (int64_t first = blockIdx.x * (int64_t)TEAMS; first < all;
+         first += (int64_t)gridDim.x * TEAMS) {
+        const int64_t seg = first + threadIdx.x / LANES;
+        const bool on = seg < all;
+        const int64_t row = seg / p.groups;
+        const int c0 = (int)(seg % p.groups) * per;
+        const T* x = (const T*)p.x + row_at(p, row, p.x_batch, p.x_step) + c0;
+        const T* res = p.residual ? (const T*)p.residual +
+                                        row_at(p, row, p.residual_batch, p.residual_step) + c0
+                                  : nullptr;
+        Pack<T, V> a[NV], b[NV];
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+            const int c = (i * LANES + lane) * V, left = on ? per - c : 0;
+            a[i].load(x + c, left);
+            if (res) b[i].load(res + c, left);
+        }
+        float v[NV][V], mean = 0.0f, var = 0.0f;
+#pragma unroll
+        for (int i = 0; i < NV; ++i)
+#pragma unroll
+            for (int e = 0; e < V; ++e) {
+                if (res) a[i].v[e] = from_f32<T>(to_f32(a[i].v[e]) + to_f32(b[i].v[e]));
+                mean += v[i][e] = to_f32(a[i].v[e]);
+            }
+        mean = team_sum<LANES>(mean, s) / per;
+#pragma unroll
+        for (int i = 0; i < NV; ++i)
+#pragma unroll
+            for (int e = 0; e < V; ++e) {
+                const float d = v[i][e] - mean;
+                if ((i * LANES + lane) * V + e < per) var = __builtin_fmaf(d, d, var);
+            }
+        var = team_sum<LANES>(var, s) / per;
+        const float rstd = 1.0f / __builtin_sqrtf(var + (float)p.eps);
+        if (!on) continue;
+        const int64_t out = row * p.dim + c0;
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+            const int c = (i * LANES + lane) * V, left = per - c;
+            if (left <= 0) continue;
+            const auto w = load_weights<W, V>(p.weight, c0 + c, left, 1.0f);
+            const auto bias = load_weights<W, V>(p.bias, c0 + c, left, 0.0f);
+            if (sum) a[i].store(sum + out + c, left);
+#pragma unroll
+            for (int e = 0; e < V; ++e)
+                a[i].v[e] = from_f32<T>(__builtin_fmaf((v[i][e] - mean) * rstd, to_f32(w.v[e]),
+                                                       to_f32(bias.v[e])));
+            a[i].store(y + out + c, left);
+        }
+        if (stats && lane == 0) *(float2*)(stats + 2 * seg) = float2{mean, rstd};
     }
 }
 
@@ -83,57 +142,302 @@ struct Grad {
     const float* stats;
 };
 
-template <class T, class W>
-__global__ void __launch_bounds__(kThreads) k_norm_dx(libscan_norm p, Grad g, T* dx) {
-    __shared__ float s[kThreads / 64];
-    const Place at = place(p);
-    const int64_t b = at.row / p.steps, t = at.row % p.steps;
-    const T* x = (const T*)p.x + at.x;
-    const T* dy = (const T*)g.dy + b * g.dy_batch + t * g.dy_step + at.c0;
-    const T* dsum = g.dsum ? (const T*)g.dsum + b * g.dsum_batch + t * g.dsum_step + at.c0 : nullptr;
-    const float mean = g.stats[2 * (int64_t)blockIdx.x], rstd = g.stats[2 * (int64_t)blockIdx.x + 1];
-    const auto weighted = [&](int c) {
-        const float d = to_f32(dy[c]);
-        return p.weight ? d * to_f32(((const W*)p.weight)[at.c0 + c]) : d;
-    };
-    float m0 = 0.0f, m1 = 0.0f;
-    for (int c = threadIdx.x; c < at.per; c += kThreads) {
-        const float w = weighted(c);
-        m0 += w;
-        m1 = __builtin_fmaf(w, (to_f32(x[c]) - mean) * rstd, m1);
+// The gradients likewise: the teams of a workgroup take rows of one group of channels,
+// the next row's elements on their way while one is worked on, and add up dweight
+// and dbias of their columns in registers, then over the teams in order.
+// part[block of the group][2][dim].
+constexpr int kBackThreads = 1024;
+template <class T, class W, int LANES, int NV>
+__global__ void __launch_bounds__(kBackThreads)
+    k_norm_back(libscan_norm p, Grad g, T* dx, float* part) {
+    constexpr int V = kVec<T>, TEAMS = kBackThreads / LANES;
+    // teams within a wave are joined by shifts, those left take turns in LDS
+    constexpr int TURNS = LANES < 64 ? kBackThreads / 64 : TEAMS, COLS = LANES * NV * V;
+    __shared__ float s[kBackThreads / 64], s_sum[TURNS > 1 ? 2 : 1][TURNS > 1 ? COLS : 1];
+    const int lane = threadIdx.x % LANES, team = threadIdx.x / LANES;
+    const int per = (int)(p.dim / p.groups), groups = (int)p.groups;
+    const int group = blockIdx.x % groups, block = blockIdx.x / groups;
+    const int64_t rows = p.batch * p.steps, every = (int64_t)(gridDim.x / groups) * TEAMS;
+    const int c0 = group * per;
+    Pack<W, V> w[NV];
+    float dw[NV][V], db[NV][V];
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+        const int c = (i * LANES + lane) * V;
+        w[i] = load_weights<W, V>(p.weight, c0 + c, per - c, 1.0f);
+#pragma unroll
+        for (int e = 0; e < V; ++e) dw[i][e] = db[i][e] = 0.0f;
     }
-    m0 = block_sum(m0, s) / at.per;
-    m1 = block_sum(m1, s) / at.per;
-    T* out = dx + at.row * p.dim + at.c0;
-    for (int c = threadIdx.x; c < at.per; c += kThreads) {
-        float d = rstd * (weighted(c) - m0 - (to_f32(x[c]) - mean) * rstd * m1);
-        if (dsum) d += to_f32(dsum[c]);
-        out[c] = from_f32<T>(d);
+    struct Row {
+        Pack<T, V> x[NV], dy[NV];
+        float2 stats;
+    };
+    const auto load = [&](Row& r, int64_t row) {
+        const bool on = row < rows;
+        const T* x = (const T*)p.x + row_at(p, row, p.x_batch, p.x_step) + c0;
+        const T* dy = (const T*)g.dy + row_at(p, row, g.dy_batch, g.dy_step) + c0;
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+            const int c = (i * LANES + lane) * V, left = on ? per - c : 0;
+            r.x[i].load(x + c, left);
+            r.dy[i].load(dy + c, left);
+        }
+        r.stats = on ? *(const float2*)(g.stats + 2 * (row * groups + group)) : float2{0.0f, 0.0f};
+    };
+    Row now;
+    int64_t row = (int64_t)block * TEAMS + team;
+    load(now, row);
+    // the teams of a workgroup stay together
+    for (int64_t at = (int64_t)block * TEAMS; at < rows; at += every, row += every) {
+        const bool on = row < rows;
+        Pack<T, V> dsum[NV];
+        if (g.dsum) {
+            const T* ds = (const T*)g.dsum + row_at(p, row, g.dsum_batch, g.dsum_step) + c0;
+#pragma unroll
+            for (int i = 0; i < NV; ++i) {
+                const int c = (i * LANES + lane) * V;
+                dsum[i].load(ds + c, on ? per - c : 0);
+            }
+        }
+        Row next;
+        if (at + every < rows) load(next, row + every);
+        const float mean = now.stats.x, rstd = now.stats.y;
+        float m0 = 0.0f, m1 = 0.0f;
+#pragma unroll
+        for (int i = 0; i < NV; ++i)
+#pragma unroll
+            for (int e = 0; e < V; ++e) {
+                // behind the group's end dy is 0
+                const float d = to_f32(now.dy[i].v[e]);
+                const float hat = (to_f32(now.x[i].v[e]) - mean) * rstd;
+                const float u = d * to_f32(w[i].v[e]);
+                m0 += u;
+                m1 = __builtin_fmaf(u, hat, m1);
+                dw[i][e] = __builtin_fmaf(d, hat, dw[i][e]);
+                db[i][e] += d;
+            }
+        m0 = team_sum<LANES>(m0, s) / per;
+        m1 = team_sum<LANES>(m1, s) / per;
+        if (on) {
+            T* out = dx + row * p.dim + c0;
+#pragma unroll
+            for (int i = 0; i < NV; ++i) {
+                const int c = (i * LANES + lane) * V, left = per - c;
+                if (left <= 0) continue;
+                forget(now.x[i]), forget(now.dy[i]), forget(w[i]);
+                Pack<T, V> o;
+#pragma unroll
+                for (int e = 0; e < V; ++e) {
+                    const float hat = (to_f32(now.x[i].v[e]) - mean) * rstd;
+                    const float u = to_f32(now.dy[i].v[e]) * to_f32(w[i].v[e]);
+                    float v = rstd * (u - m0 - hat * m1);
+                    if (g.dsum) v += to_f32(dsum[i].v[e]);
+                    o.v[e] = from_f32<T>(v);
+                }
+                o.store(out + c, left);
+            }
+        }
+        now = next;
+    }
+    if constexpr (LANES < 64) {
+#pragma unroll
+        for (int i = 0; i < NV; ++i)
+#pragma unroll
+            for (int e = 0; e < V; ++e)
+#pragma unroll
+                for (int m = LANES; m < 64; m <<= 1) {
+                    dw[i][e] += __shfl_xor(dw[i][e], m);
+                    db[i][e] += __shfl_xor(db[i][e], m);
+                }
+    }
+    constexpr int TURN = LANES < 64 ? 64 : LANES;
+    const bool mine = LANES >= 64 || threadIdx.x % 64 < LANES;
+    if constexpr (TURNS > 1) {
+        for (int turn = 0; turn < TURNS; ++turn) {
+            __syncthreads();
+            if (threadIdx.x / TURN == turn && mine) {
+#pragma unroll
+                for (int i = 0; i < NV; ++i)
+#pragma unroll
+                    for (int e = 0; e < V; ++e) {
+                        const int c = (i * V + e) * LANES + lane;  // lanes next to each other
+                        if (turn > 0) {
+                            dw[i][e] += s_sum[0][c];
+                            db[i][e] += s_sum[1][c];
+                        }
+                        s_sum[0][c] = dw[i][e];
+                        s_sum[1][c] = db[i][e];
+                    }
+            }
+        }
+        __syncthreads();
+    }
+    // the last turn's threads have the sums
+    if (threadIdx.x / TURN != TURNS - 1 || !mine) return;
+    float* to = part + 2 * (int64_t)block * p.dim + c0;
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+        const int c = (i * LANES + lane) * V;
+#pragma unroll
+        for (int e = 0; e < V; ++e)
+            if (c + e < per) {
+                to[c + e] = dw[i][e];
+                to[p.dim + c + e] = db[i][e];
+            }
     }
 }
 
-// Partial sums of dweight and dbias over `rows` rows, a column to a thread:
-// part[block][2][dim].
-template <class T>
+// ------------------------------------------------ rows that do not fit registers
+
+constexpr int kThreads = 1024;
+
+// A workgroup to a group of a row, which is read three times.
+template <class T, class W>
 __global__ void __launch_bounds__(kThreads)
-    k_norm_dw(libscan_norm p, Grad g, int64_t rows, float* part) {
-    const int c = blockIdx.y * kThreads + threadIdx.x;
-    if (c >= p.dim) return;
-    const int64_t all = p.batch * p.steps, lo = blockIdx.x * rows;
-    const int64_t hi = lo + rows < all ? lo + rows : all;
-    const int group = (int)(c / (p.dim / p.groups));
-    float dw = 0.0f, db = 0.0f;
-    for (int64_t r = lo; r < hi; ++r) {
-        const int64_t b = r / p.steps, t = r % p.steps;
-        const float d = to_f32(((const T*)g.dy)[b * g.dy_batch + t * g.dy_step + c]);
-        const float x = to_f32(((const T*)p.x)[b * p.x_batch + t * p.x_step + c]);
-        const float* st = g.stats + 2 * (r * p.groups + group);
-        dw = __builtin_fmaf(d, (x - st[0]) * st[1], dw);
-        db += d;
+    k_norm_long(libscan_norm p, T* y, T* sum, float* stats) {
+    constexpr int V = kVec<T>;
+    __shared__ float s[kThreads / 64];
+    const int per = (int)(p.dim / p.groups);
+    const int64_t all = p.batch * p.steps * p.groups;
+    for (int64_t seg = blockIdx.x; seg < all; seg += gridDim.x) {
+        const int64_t row = seg / p.groups;
+        const int c0 = (int)(seg % p.groups) * per;
+        const T* x = (const T*)p.x + row_at(p, row, p.x_batch, p.x_step) + c0;
+        const T* res = p.residual ? (const T*)p.residual +
+                                        row_at(p, row, p.residual_batch, p.residual_step) + c0
+                                  : nullptr;
+        // f(c, the vector at c, elements there) over the group; behind its end they are 0
+        const auto each = [&](auto f) {
+            for (int c = threadIdx.x * V; c < per; c += kThreads * V) {
+                Pack<T, V> a, b;
+                a.load(x + c, per - c);
+                if (res) {
+                    b.load(res + c, per - c);
+#pragma unroll
+                    for (int e = 0; e < V; ++e)
+                        a.v[e] = from_f32<T>(to_f32(a.v[e]) + to_f32(b.v[e]));
+                }
+                f(c, a, per - c);
+            }
+        };
+        float mean = 0.0f, var = 0.0f;
+        each([&](int, const Pack<T, V>& a, int) {
+#pragma unroll
+            for (int e = 0; e < V; ++e) mean += to_f32(a.v[e]);
+        });
+        mean = team_sum<kThreads>(mean, s) / per;
+        each([&](int, const Pack<T, V>& a, int left) {
+#pragma unroll
+            for (int e = 0; e < V; ++e) {
+                const float d = to_f32(a.v[e]) - mean;
+                if (e < left) var = __builtin_fmaf(d, d, var);
+            }
+        });
+        var = team_sum<kThreads>(var, s) / per;
+        const float rstd = 1.0f / __builtin_sqrtf(var + (float)p.eps);
+        const int64_t out = row * p.dim + c0;
+        each([&](int c, Pack<T, V>& a, int left) {
+            const auto w = load_weights<W, V>(p.weight, c0 + c, left, 1.0f);
+            const auto bias = load_weights<W, V>(p.bias, c0 + c, left, 0.0f);
+            if (sum) a.store(sum + out + c, left);
+#pragma unroll
+            for (int e = 0; e < V; ++e)
+                a.v[e] = from_f32<T>(__builtin_fmaf((to_f32(a.v[e]) - mean) * rstd, to_f32(w.v[e]),
+                                                    to_f32(bias.v[e])));
+            a.store(y + out + c, left);
+        });
+        if (stats && threadIdx.x == 0) *(float2*)(stats + 2 * seg) = float2{mean, rstd};
     }
-    part[(2 * (int64_t)blockIdx.x) * p.dim + c] = dw;
-    part[(2 * (int64_t)blockIdx.x + 1) * p.dim + c] = db;
 }
+
+template <class T, class W>
+__global__ void __launch_bounds__(kThreads) k_norm_long_dx(libscan_norm p, Grad g, T* dx) {
+    constexpr int V = kVec<T>;
+    __shared__ float s[kThreads / 64];
+    const int per = (int)(p.dim / p.groups);
+    const int64_t all = p.batch * p.steps * p.groups;
+    for (int64_t seg = blockIdx.x; seg < all; seg += gridDim.x) {
+        const int64_t row = seg / p.groups;
+        const int c0 = (int)(seg % p.groups) * per;
+        const T* x = (const T*)p.x + row_at(p, row, p.x_batch, p.x_step) + c0;
+        const T* dy = (const T*)g.dy + row_at(p, row, g.dy_batch, g.dy_step) + c0;
+        const T* ds = (const T*)g.dsum + row_at(p, row, g.dsum_batch, g.dsum_step) + c0;
+        const float2 st = *(const float2*)(g.stats + 2 * seg);
+        // f(c, elements there, dy weight, xhat) over the group
+        const auto each = [&](auto f) {
+            for (int c = threadIdx.x * V; c < per; c += kThreads * V) {
+                const int left = per - c;
+                Pack<T, V> a, b;
+                a.load(dy + c, left);
+                b.load(x + c, left);
+                const auto w = load_weights<W, V>(p.weight, c0 + c, left, 1.0f);
+                float u[V], hat[V];
+#pragma unroll
+                for (int e = 0; e < V; ++e) {
+                    u[e] = to_f32(a.v[e]) * to_f32(w.v[e]);
+                    hat[e] = (to_f32(b.v[e]) - st.x) * st.y;
+                }
+                f(c, left, u, hat);
+            }
+        };
+        float m0 = 0.0f, m1 = 0.0f;
+        each([&](int, int left, const float (&u)[V], const float (&hat)[V]) {
+#pragma unroll
+            for (int e = 0; e < V; ++e) {
+                m0 += u[e];  // 0 behind the end
+                if (e < left) m1 = __builtin_fmaf(u[e], hat[e], m1);
+            }
+        });
+        m0 = team_sum<kThreads>(m0, s) / per;
+        m1 = team_sum<kThreads>(m1, s) / per;
+        T* out = dx + row * p.dim + c0;
+        each([&](int c, int left, const float (&u)[V], const float (&hat)[V]) {
+            Pack<T, V> d, o;
+            if (g.dsum) d.load(ds + c, left);
+#pragma unroll
+            for (int e = 0; e < V; ++e) {
+                float v = st.y * (u[e] - m0 - hat[e] * m1);
+                if (g.dsum) v += to_f32(d.v[e]);
+                o.v[e] = from_f32<T>(v);
+            }
+            o.store(out + c, left);
+        });
+    }
+}
+
+// Partial sums of dweight and dbias over kPartRows rows, four columns to a thread.
+constexpr int kPartRows = 64, kPartThreads = 256, kPartCols = 4 * kPartThreads;
+template <class T>
+__global__ void __launch_bounds__(kPartThreads) k_norm_long_dw(libscan_norm p, Grad g, float* part) {
+    const int blocks = (int)((p.dim + kPartCols - 1) / kPartCols);
+    const int c = blockIdx.x % blocks * kPartCols + threadIdx.x * 4, block = blockIdx.x / blocks;
+    if (c >= p.dim) return;
+    const int64_t all = p.batch * p.steps, lo = (int64_t)block * kPartRows;
+    const int64_t hi = lo + kPartRows < all ? lo + kPartRows : all;
+    const int per = (int)(p.dim / p.groups), left = (int)p.dim - c;
+    float dw[4]{}, db[4]{};
+#pragma unroll 4
+    for (int64_t r = lo; r < hi; ++r) {
+        Pack<T, 4> d, x;
+        d.load((const T*)g.dy + row_at(p, r, g.dy_batch, g.dy_step) + c, left);
+        x.load((const T*)p.x + row_at(p, r, p.x_batch, p.x_step) + c, left);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            if (e >= left) break;
+            const float2 st = *(const float2*)(g.stats + 2 * (r * p.groups + (c + e) / per));
+            dw[e] = __builtin_fmaf(to_f32(d.v[e]), (to_f32(x.v[e]) - st.x) * st.y, dw[e]);
+            db[e] += to_f32(d.v[e]);
+        }
+    }
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+        if (e < left) {
+            part[2 * (int64_t)block * p.dim + c + e] = dw[e];
+            part[(2 * (int64_t)block + 1) * p.dim + c + e] = db[e];
+        }
+}
+
+// ------------------------------------------------ the sums' last step
 
 template <int SLICES>
 __global__ void __launch_bounds__(kSumThreads)
@@ -146,11 +450,7 @@ __global__ void __launch_bounds__(kSumThreads)
     if (out) out[i < dim ? i : i - dim] = v;
 }
 
-constexpr int64_t kPartRows = 64;
-int64_t parts(const libscan_norm& p) {
-    const int64_t rows = p.batch * p.steps;
-    return (rows + kPartRows - 1) / kPartRows;
-}
+// ------------------------------------------------ launches
 
 template <class F>
 hipError_t by_type(const libscan_norm& p, F f) {
@@ -161,15 +461,68 @@ hipError_t by_type(const libscan_norm& p, F f) {
     return hipGetLastError();
 }
 
+// The smallest team and number of vectors, up to `most`, that hold a group's channels; no
+// lanes if none does.  The gradients' sums take registers for two vectors.
+struct Team {
+    int lanes, vectors;
+};
+Team team(const libscan_norm& p, int most) {
+    const int64_t per = p.dim / p.groups, vec = p.type == LIBSCAN_F32 ? 4 : 8;
+    const Team all[] = {{16, 1}, {32, 1}, {64, 1}, {128, 1}, {256, 1}, {512, 1}, {1024, 1},
+                        {1024, 2}, {1024, 4}};
+    for (const Team& t : all)
+        if (t.vectors <= most && t.lanes * t.vectors * vec >= per) return t;
+    return {0, 0};
+}
+template <int MOST, class F>
+void by_team(const Team& t, F f) {
+    const std::integral_constant<int, 1> one;
+    const std::integral_constant<int, 1024> all;
+    if (t.lanes == 16) f(std::integral_constant<int, 16>(), one);
+    else if (t.lanes == 32) f(std::integral_constant<int, 32>(), one);
+    else if (t.lanes == 64) f(std::integral_constant<int, 64>(), one);
+    else if (t.lanes == 128) f(std::integral_constant<int, 128>(), one);
+    else if (t.lanes == 256) f(std::integral_constant<int, 256>(), one);
+    else if (t.lanes == 512) f(std::integral_constant<int, 512>(), one);
+    else if (t.vectors == 1) f(all, one);
+    else if (t.vectors == 2 || MOST == 2) f(all, std::integral_constant<int, 2>());
+    else f(all, std::integral_constant<int, MOST == 2 ? 2 : 4>());
+}
+
+constexpr int64_t kMostBlocks = 1 << 20;  // the rest in further turns
+uint32_t capped(int64_t blocks) { return (uint32_t)(blocks < kMostBlocks ? blocks : kMostBlocks); }
+
+// Blocks of rows that dweight and dbias are added up over first.
+int64_t parts(const libscan_norm& p) {
+    const int64_t rows = p.batch * p.steps;
+    const Team t = team(p, 2);
+    if (!t.lanes) return (rows + kPartRows - 1) / kPartRows;
+    const int64_t teams = kBackThreads / t.lanes, blocks = (rows + teams - 1) / teams;
+    // a workgroup to a CU, two where rows are short
+    const int64_t most = p.groups >= 512 ? 1 : 512 / p.groups;
+    return blocks < most ? blocks : most;
+}
+
 }  // namespace
 
 hipError_t launch_norm(const libscan_norm& p, void* y, void* sum, float* stats,
                        hipStream_t stream) {
-    const int64_t grid = p.batch * p.steps * p.groups;
-    if (grid == 0 || p.dim == 0) return hipSuccess;
-    return by_type(p, [&](auto t, auto w) {
-        using T = decltype(t);
-        k_norm<T, decltype(w)><<<(uint32_t)grid, kThreads, 0, stream>>>(p, (T*)y, (T*)sum, stats);
+    const int64_t all = p.batch * p.steps * p.groups;
+    if (all == 0 || p.dim == 0) return hipSuccess;
+    const Team t = team(p, 4);
+    return by_type(p, [&](auto type, auto weights) {
+        using T = decltype(type);
+        using W = decltype(weights);
+        if (!t.lanes) {
+            k_norm_long<T, W><<<capped(all), kThreads, 0, stream>>>(p, (T*)y, (T*)sum, stats);
+            return;
+        }
+        by_team<4>(t, [&](auto lanes, auto vectors) {
+            constexpr int L = lanes.value, THREADS = L > kFrontThreads ? L : kFrontThreads;
+            constexpr int TEAMS = THREADS / L;
+            k_norm<T, W, L, vectors.value><<<capped((all + TEAMS - 1) / TEAMS), THREADS, 0, stream>>>(
+                p, (T*)y, (T*)sum, stats);
+        });
     });
 }
 
@@ -180,18 +533,30 @@ hipError_t launch_norm_back(const libscan_norm& p, const void* dy, int64_t dy_ba
                             int64_t dsum_step, const float* stats, void* dx, float* dweight,
                             float* dbias, void* scratch, hipStream_t stream) {
     const Grad g{dy, dy_batch, dy_step, dsum, dsum_batch, dsum_step, stats};
-    const int64_t grid = p.batch * p.steps * p.groups;
+    const int64_t all = p.batch * p.steps * p.groups, count = parts(p);
     if (p.dim == 0) return hipSuccess;
     float* part = (float*)scratch;
-    return by_type(p, [&](auto t, auto w) {
-        using T = decltype(t);
-        if (grid) {
-            k_norm_dx<T, decltype(w)><<<(uint32_t)grid, kThreads, 0, stream>>>(p, g, (T*)dx);
-            k_norm_dw<T><<<dim3((uint32_t)parts(p), (uint32_t)((p.dim + kThreads - 1) / kThreads)),
-                           kThreads, 0, stream>>>(p, g, kPartRows, part);
+    const Team t = team(p, 2);
+    return by_type(p, [&](auto type, auto weights) {
+        using T = decltype(type);
+        using W = decltype(weights);
+        if (all && t.lanes)
+            by_team<2>(t, [&](auto lanes, auto vectors) {
+                k_norm_back<T, W, lanes.value, vectors.value>
+                    <<<(uint32_t)(count * p.groups), kBackThreads, 0, stream>>>(p, g, (T*)dx, part);
+            });
+        if (all && !t.lanes) {
+            k_norm_long_dx<T, W><<<capped(all), kThreads, 0, stream>>>(p, g, (T*)dx);
+            k_norm_long_dw<T><<<(uint32_t)(count * ((p.dim + kPartCols - 1) / kPartCols)),
+                                kPartThreads, 0, stream>>>(p, g, part);
         }
-        k_norm_sum<8><<<(uint32_t)((2 * p.dim + kSumOuts<8> - 1) / kSumOuts<8>), kSumThreads, 0,
-                        stream>>>(part, parts(p), p.dim, dweight, dbias);
+        if (!dweight && !dbias) return;
+        if (long_sum(count))
+            k_norm_sum<8><<<(uint32_t)((2 * p.dim + kSumOuts<8> - 1) / kSumOuts<8>), kSumThreads, 0,
+                            stream>>>(part, count, p.dim, dweight, dbias);
+        else
+            k_norm_sum<1><<<(uint32_t)((2 * p.dim + kSumOuts<1> - 1) / kSumOuts<1>), kSumThreads, 0,
+                            stream>>>(part, count, p.dim, dweight, dbias);
     });
 }
 
