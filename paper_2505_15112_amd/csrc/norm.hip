@@ -30,21 +30,34 @@ __device__ __forceinline__ void forget(P& x) {
 }
 
 // Sums over the LANES threads of a team (a power of two; a workgroup's teams all call).
-template <int LANES>
-__device__ __forceinline__ float team_sum(float v, float* s) {
+// Calls take turns with two buffers `s` of N floats for each wave: what a buffer holds is
+// read before the other's barrier, so one barrier a call will do.
+template <int LANES, int N>
+__device__ __forceinline__ void team_sums(float (&v)[N], float* s) {
 #pragma unroll
-    for (int m = (LANES < 64 ? LANES : 64) / 2; m > 0; m >>= 1) v += __shfl_xor(v, m);
+    for (int m = (LANES < 64 ? LANES : 64) / 2; m > 0; m >>= 1)
+#pragma unroll
+        for (int k = 0; k < N; ++k) v[k] += __shfl_xor(v[k], m);
     if constexpr (LANES > 64) {
         constexpr int WAVES = LANES / 64;
-        float* mine = s + threadIdx.x / LANES * WAVES;
-        __syncthreads();  // the last sum is read
-        if (threadIdx.x % 64 == 0) mine[threadIdx.x % LANES / 64] = v;
-        __syncthreads();
-        v = mine[0];
+        float* mine = s + threadIdx.x / LANES * WAVES * N;
+        if (threadIdx.x % 64 == 0)
 #pragma unroll
-        for (int i = 1; i < WAVES; ++i) v += mine[i];
+            for (int k = 0; k < N; ++k) mine[threadIdx.x % LANES / 64 * N + k] = v[k];
+        __syncthreads();
+#pragma unroll
+        for (int k = 0; k < N; ++k) {
+            v[k] = mine[k];
+#pragma unroll
+            for (int i = 1; i < WAVES; ++i) v[k] += mine[i * N + k];
+        }
     }
-    return v;
+}
+template <int LANES>
+__device__ __forceinline__ float team_sum(float v, float* s) {
+    float one[1] = {v};
+    team_sums<LANES>(one, s);
+    return one[0];
 }
 
 // Row `row`'s elements of a batch x steps x dim operand.
@@ -73,11 +86,11 @@ __device__ __forceinline__ Pack<W, V> load_weights(const void* w, int at, int co
 // row, the mean, then the sum of the squared differences.
 constexpr int kFrontThreads = 256;
 template <class T, class W, int LANES, int NV>
-__global__ void __launch_bounds__(LANES > kFrontThreads ? LANES : kFrontThreads)
+__global__ void __launch_bounds__(LANES > kFrontThreads ? LANES : kFrontThreads, NV == 4 ? 4 : 8)
     k_norm(libscan_norm p, T* y, T* sum, float* stats) {
     constexpr int V = kVec<T>, THREADS = LANES > kFrontThreads ? LANES : kFrontThreads;
     constexpr int TEAMS = THREADS / LANES;
-    __shared__ float s[THREADS / 64];
+    __shared__ float s[2][THREADS / 64];
     const int lane = threadIdx.x % LANES, per = (int)(p.dim / p.groups);
     const int64_t all = p.batch * p.steps * p.groups;
     for (int64_t first = blockIdx.x * (int64_t)TEAMS; first < all;
@@ -97,23 +110,25 @@ __global__ void __launch_bounds__(LANES > kFrontThreads ? LANES : kFrontThreads)
             a[i].load(x + c, left);
             if (res) b[i].load(res + c, left);
         }
-        float v[NV][V], mean = 0.0f, var = 0.0f;
+        float mean = 0.0f, var = 0.0f;
 #pragma unroll
         for (int i = 0; i < NV; ++i)
 #pragma unroll
             for (int e = 0; e < V; ++e) {
                 if (res) a[i].v[e] = from_f32<T>(to_f32(a[i].v[e]) + to_f32(b[i].v[e]));
-                mean += v[i][e] = to_f32(a[i].v[e]);
+                mean += to_f32(a[i].v[e]);
             }
-        mean = team_sum<LANES>(mean, s) / per;
+        mean = team_sum<LANES>(mean, s[0]) / per;
 #pragma unroll
-        for (int i = 0; i < NV; ++i)
+        for (int i = 0; i < NV; ++i) {
+            forget(a[i]);
 #pragma unroll
             for (int e = 0; e < V; ++e) {
-                const float d = v[i][e] - mean;
+                const float d = to_f32(a[i].v[e]) - mean;
                 if ((i * LANES + lane) * V + e < per) var = __builtin_fmaf(d, d, var);
             }
-        var = team_sum<LANES>(var, s) / per;
+        }
+        var = team_sum<LANES>(var, s[1]) / per;
         const float rstd = 1.0f / __builtin_sqrtf(var + (float)p.eps);
         if (!on) continue;
         const int64_t out = row * p.dim + c0;
@@ -121,12 +136,13 @@ __global__ void __launch_bounds__(LANES > kFrontThreads ? LANES : kFrontThreads)
         for (int i = 0; i < NV; ++i) {
             const int c = (i * LANES + lane) * V, left = per - c;
             if (left <= 0) continue;
+            forget(a[i]);
             const auto w = load_weights<W, V>(p.weight, c0 + c, left, 1.0f);
             const auto bias = load_weights<W, V>(p.bias, c0 + c, left, 0.0f);
             if (sum) a[i].store(sum + out + c, left);
 #pragma unroll
             for (int e = 0; e < V; ++e)
-                a[i].v[e] = from_f32<T>(__builtin_fmaf((v[i][e] - mean) * rstd, to_f32(w.v[e]),
+                a[i].v[e] = from_f32<T>(__builtin_fmaf((to_f32(a[i].v[e]) - mean) * rstd, to_f32(w.v[e]),
                                                        to_f32(bias.v[e])));
             a[i].store(y + out + c, left);
         }
@@ -153,7 +169,7 @@ __global__ void __launch_bounds__(kBackThreads)
     constexpr int V = kVec<T>, TEAMS = kBackThreads / LANES;
     // teams within a wave are joined by shifts, those left take turns in LDS
     constexpr int TURNS = LANES < 64 ? kBackThreads / 64 : TEAMS, COLS = LANES * NV * V;
-    __shared__ float s[kBackThreads / 64], s_sum[TURNS > 1 ? 2 : 1][TURNS > 1 ? COLS : 1];
+    __shared__ float s[2][kBackThreads / 64 * 2], s_sum[TURNS > 1 ? 2 : 1][TURNS > 1 ? COLS : 1];
     const int lane = threadIdx.x % LANES, team = threadIdx.x / LANES;
     const int per = (int)(p.dim / p.groups), groups = (int)p.groups;
     const int group = blockIdx.x % groups, block = blockIdx.x / groups;
@@ -188,7 +204,8 @@ __global__ void __launch_bounds__(kBackThreads)
     int64_t row = (int64_t)block * TEAMS + team;
     load(now, row);
     // the teams of a workgroup stay together
-    for (int64_t at = (int64_t)block * TEAMS; at < rows; at += every, row += every) {
+    int turn = 0;
+    for (int64_t at = (int64_t)block * TEAMS; at < rows; at += every, row += every, turn ^= 1) {
         const bool on = row < rows;
         Pack<T, V> dsum[NV];
         if (g.dsum) {
@@ -202,7 +219,7 @@ __global__ void __launch_bounds__(kBackThreads)
         Row next;
         if (at + every < rows) load(next, row + every);
         const float mean = now.stats.x, rstd = now.stats.y;
-        float m0 = 0.0f, m1 = 0.0f;
+        float m[2] = {0.0f, 0.0f};
 #pragma unroll
         for (int i = 0; i < NV; ++i)
 #pragma unroll
@@ -211,13 +228,13 @@ __global__ void __launch_bounds__(kBackThreads)
                 const float d = to_f32(now.dy[i].v[e]);
                 const float hat = (to_f32(now.x[i].v[e]) - mean) * rstd;
                 const float u = d * to_f32(w[i].v[e]);
-                m0 += u;
-                m1 = __builtin_fmaf(u, hat, m1);
+                m[0] += u;
+                m[1] = __builtin_fmaf(u, hat, m[1]);
                 dw[i][e] = __builtin_fmaf(d, hat, dw[i][e]);
                 db[i][e] += d;
             }
-        m0 = team_sum<LANES>(m0, s) / per;
-        m1 = team_sum<LANES>(m1, s) / per;
+        team_sums<LANES>(m, s[turn]);
+        const float m0 = m[0] / per, m1 = m[1] / per;
         if (on) {
             T* out = dx + row * p.dim + c0;
 #pragma unroll
@@ -253,15 +270,15 @@ __global__ void __launch_bounds__(kBackThreads)
     constexpr int TURN = LANES < 64 ? 64 : LANES;
     const bool mine = LANES >= 64 || threadIdx.x % 64 < LANES;
     if constexpr (TURNS > 1) {
-        for (int turn = 0; turn < TURNS; ++turn) {
+        for (int next = 0; next < TURNS; ++next) {
             __syncthreads();
-            if (threadIdx.x / TURN == turn && mine) {
+            if (threadIdx.x / TURN == next && mine) {
 #pragma unroll
                 for (int i = 0; i < NV; ++i)
 #pragma unroll
                     for (int e = 0; e < V; ++e) {
                         const int c = (i * V + e) * LANES + lane;  // lanes next to each other
-                        if (turn > 0) {
+                        if (next > 0) {
                             dw[i][e] += s_sum[0][c];
                             db[i][e] += s_sum[1][c];
                         }
@@ -296,7 +313,7 @@ template <class T, class W>
 __global__ void __launch_bounds__(kThreads)
     k_norm_long(libscan_norm p, T* y, T* sum, float* stats) {
     constexpr int V = kVec<T>;
-    __shared__ float s[kThreads / 64];
+    __shared__ float s[2][kThreads / 64];
     const int per = (int)(p.dim / p.groups);
     const int64_t all = p.batch * p.steps * p.groups;
     for (int64_t seg = blockIdx.x; seg < all; seg += gridDim.x) {
@@ -325,7 +342,7 @@ __global__ void __launch_bounds__(kThreads)
 #pragma unroll
             for (int e = 0; e < V; ++e) mean += to_f32(a.v[e]);
         });
-        mean = team_sum<kThreads>(mean, s) / per;
+        mean = team_sum<kThreads>(mean, s[0]) / per;
         each([&](int, const Pack<T, V>& a, int left) {
 #pragma unroll
             for (int e = 0; e < V; ++e) {
@@ -333,7 +350,7 @@ __global__ void __launch_bounds__(kThreads)
                 if (e < left) var = __builtin_fmaf(d, d, var);
             }
         });
-        var = team_sum<kThreads>(var, s) / per;
+        var = team_sum<kThreads>(var, s[1]) / per;
         const float rstd = 1.0f / __builtin_sqrtf(var + (float)p.eps);
         const int64_t out = row * p.dim + c0;
         each([&](int c, Pack<T, V>& a, int left) {
@@ -353,7 +370,7 @@ __global__ void __launch_bounds__(kThreads)
 template <class T, class W>
 __global__ void __launch_bounds__(kThreads) k_norm_long_dx(libscan_norm p, Grad g, T* dx) {
     constexpr int V = kVec<T>;
-    __shared__ float s[kThreads / 64];
+    __shared__ float s[2][kThreads / 64];
     const int per = (int)(p.dim / p.groups);
     const int64_t all = p.batch * p.steps * p.groups;
     for (int64_t seg = blockIdx.x; seg < all; seg += gridDim.x) {
@@ -388,8 +405,8 @@ __global__ void __launch_bounds__(kThreads) k_norm_long_dx(libscan_norm p, Grad 
                 if (e < left) m1 = __builtin_fmaf(u[e], hat[e], m1);
             }
         });
-        m0 = team_sum<kThreads>(m0, s) / per;
-        m1 = team_sum<kThreads>(m1, s) / per;
+        m0 = team_sum<kThreads>(m0, s[0]) / per;
+        m1 = team_sum<kThreads>(m1, s[1]) / per;
         T* out = dx + row * p.dim + c0;
         each([&](int c, int left, const float (&u)[V], const float (&hat)[V]) {
             Pack<T, V> d, o;
@@ -469,7 +486,7 @@ struct Team {
 Team team(const libscan_norm& p, int most) {
     const int64_t per = p.dim / p.groups, vec = p.type == LIBSCAN_F32 ? 4 : 8;
     const Team all[] = {{16, 1}, {32, 1}, {64, 1}, {128, 1}, {256, 1}, {512, 1}, {1024, 1},
-                        {1024, 2}, {1024, 4}};
+                        {1024, 2}, {1024, 3}, {1024, 4}};
     for (const Team& t : all)
         if (t.vectors <= most && t.lanes * t.vectors * vec >= per) return t;
     return {0, 0};
@@ -486,6 +503,7 @@ void by_team(const Team& t, F f) {
     else if (t.lanes == 512) f(std::integral_constant<int, 512>(), one);
     else if (t.vectors == 1) f(all, one);
     else if (t.vectors == 2 || MOST == 2) f(all, std::integral_constant<int, 2>());
+    else if (t.vectors == 3) f(all, std::integral_constant<int, MOST == 2 ? 2 : 3>());
     else f(all, std::integral_constant<int, MOST == 2 ? 2 : 4>());
 }
 
