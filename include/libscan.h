@@ -528,7 +528,9 @@ int selective_scan_step(const libscan_ssm* p, float* states, int64_t n_states,
  * stride over the last dimension.  log_decay: fp32, batch x steps x heads with
  * unit stride over heads, or (fixed != 0) heads, one for all tokens; 0 keeps the
  * state, -infinity clears it.  state (nullable: zeros): batch x heads x dk x dv,
- * dense fp32.  1 <= dk, dv <= 256, heads a multiple of groups. */
+ * dense fp32.  1 <= dk, dv <= 256, heads a multiple of groups.  An infinity or a NaN
+ * in an operand makes the outputs that it reaches infinite or NaN (which of the two is
+ * not said), and no others: of v, one column of its head; of any, no earlier token. */
 typedef struct {
     int64_t type, batch, steps, heads, groups, dk, dv, fixed;
     const void* q;
@@ -557,7 +559,8 @@ int linear_attention(const libscan_attend* p, void* y, float* state_out, void* s
  * and dstate_out (nullable, batch x heads x dk x dv fp32: the gradient of the last
  * state), from the same *p: dq, dk (of the groups), dv, of `type`; dlog_decay (of
  * log_decay's shape: 0 where the decay is -infinity) and dstate (nullable: batch x
- * heads x dk x dv), fp32.  Sums run in a fixed order. */
+ * heads x dk x dv), fp32.  Sums run in a fixed order.  A token's dlog_decay is formed
+ * of q dq - k dk of the tokens from it on: an infinity or a NaN there reaches it. */
 int linear_attention_backward(const libscan_attend* p, const void* dy, int64_t dy_batch,
                               int64_t dy_step, int64_t dy_head, const float* dstate_out, void* dq,
                               void* dk, void* dv, float* dlog_decay, float* dstate, void* scratch,

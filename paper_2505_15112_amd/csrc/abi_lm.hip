@@ -140,10 +140,8 @@ int check_attend(const libscan_attend* p) {
     const int r = check_sizes(p->batch, p->steps, p->heads * (p->dk > p->dv ? p->dk : p->dv));
     if (r != LIBSCAN_OK) return r;
     if (p->heads % p->groups) return LIBSCAN_EINVAL;
-    // workgroups of at least 16 columns of a row's head, of 256 shared gradients
-    if ((__int128)p->batch * p->heads * 16 >= kMaxBlocks ||
-        (__int128)p->batch * p->steps * p->groups * p->dk / 256 >= kMaxBlocks)
-        return LIBSCAN_ERANGE;
+    // at most two workgroups to a row's head (more only where there are few)
+    if ((__int128)p->batch * p->heads * 2 >= kMaxBlocks) return LIBSCAN_ERANGE;
     return LIBSCAN_OK;
 }
 
@@ -168,10 +166,7 @@ int check_norm(const libscan_norm* p) {
     if (p->groups < 1 || !(p->eps >= 0.0)) return LIBSCAN_EINVAL;
     const int r = check_sizes(p->batch, p->steps, p->dim);
     if (r != LIBSCAN_OK) return r;
-    if (p->dim % p->groups) return LIBSCAN_EINVAL;
-    // a workgroup to a row's group at most
-    if ((__int128)p->batch * p->steps * p->groups >= kMaxBlocks) return LIBSCAN_ERANGE;
-    return LIBSCAN_OK;
+    return p->dim % p->groups ? LIBSCAN_EINVAL : LIBSCAN_OK;
 }
 
 constexpr int kLogitsInputs = 11;

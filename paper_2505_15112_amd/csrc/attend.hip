@@ -13,14 +13,16 @@ typedef float f4 __attribute__((ext_vector_type(4)));
 template <class T>
 __global__ void __launch_bounds__(256) k_join_heads(const float* dq_in, const float* dk_in, T* dq,
                                                     T* dk, int64_t count, int per, int width) {
-    const int64_t i = blockIdx.x * (int64_t)256 + threadIdx.x;
-    if (i >= count) return;
     const float* in = blockIdx.y ? dk_in : dq_in;
-    const int64_t at = i / width * per * width + i % width;
-    float sum = 0.0f;
+    T* out = blockIdx.y ? dk : dq;
+    for (int64_t i = blockIdx.x * (int64_t)256 + threadIdx.x; i < count;
+         i += (int64_t)gridDim.x * 256) {
+        const int64_t at = i / width * per * width + i % width;
+        float sum = 0.0f;
 #pragma unroll 4
-    for (int j = 0; j < per; ++j) sum += in[at + (int64_t)j * width];
-    (blockIdx.y ? dk : dq)[i] = from_f32<T>(sum);
+        for (int j = 0; j < per; ++j) sum += in[at + (int64_t)j * width];
+        out[i] = from_f32<T>(sum);
+    }
 }
 
 // Sums over the workgroup's threads, in 64 bits: v becomes the sum over the threads
@@ -408,7 +410,8 @@ hipError_t launch_attend_back(const libscan_attend& p, const void* dy, int64_t d
             floats(plan.gates), dlog_decay, p.batch * p.steps, (int)p.heads);
     const int64_t count = p.batch * p.steps * p.groups * p.dk;
     if (shared && count) {
-        const dim3 grid((uint32_t)((count + 255) / 256), 2);
+        const int64_t blocks = (count + 255) / 256, most = 1 << 20;
+        const dim3 grid((uint32_t)(blocks < most ? blocks : most), 2);
         const auto join = [&](auto zero) {
             using T = decltype(zero);
             k_join_heads<<<grid, 256, 0, stream>>>(floats(plan.dq), floats(plan.dk), (T*)dq, (T*)dk,

@@ -157,6 +157,40 @@ def test_ragged_rows_do_not_read_past_their_tokens(kind, dims):
     assert torch.equal(got[4][0].cpu(), so[0])
 
 
+@pytest.mark.parametrize("kind", [F32, F16, BF16])
+@pytest.mark.parametrize("dims", [(32, 16), (100, 130)])
+def test_ragged_rows_in_pieces(kind, dims):
+    """Rows long enough to be cut: lengths that end in every piece and at their edges."""
+    lengths = [640, 0, 64, 129, 320, 577]
+    a, dy = inputs(6, 640, 2, 1, *dims, kind=kind, state=True, lengths=lengths, rate=0.05)
+    so = torch.randn(*a["state"].shape, generator=torch.Generator().manual_seed(3))
+    check_forward(a)
+    check_backward(a, dy, so)
+
+
+def test_rows_beyond_32_bit_offsets():
+    """2.4e9 elements: what lies behind 2^31 of them against a call of its own."""
+    steps, heads, d = 150000, 64, 128
+    if torch.cuda.mem_get_info()[0] < 90 << 30:
+        pytest.skip("needs 70 GB")
+    g = torch.Generator(device=DEV).manual_seed(1)
+    q, k, v, dy = (torch.empty(2, steps, heads, d, dtype=BF16, device=DEV).normal_(generator=g)
+                   for _ in range(4))
+    decay = torch.full((heads,), -0.02, device=DEV)
+    announce("linear_attention", tuple(q.shape))
+    y, last = ops.linear_attention(q, k, v, decay, with_state=True)
+    one, end = ops.linear_attention(q[1:], k[1:], v[1:], decay, with_state=True)
+    # rows may be cut into other pieces: sums in another order, one unit of bfloat16
+    assert (y[1, -500:].float() - one[0, -500:].float()).abs().max() <= 2.0**-7 * one.abs().max()
+    assert (last[1] - end[0]).abs().max() <= 1e-5 * end.abs().max()
+    del y, one
+    announce("linear_attention_backward", tuple(q.shape))
+    grads = ops.linear_attention_backward(dy, q, k, v, decay)
+    part = ops.linear_attention_backward(dy[1:], q[1:], k[1:], v[1:], decay)
+    for x, w in zip(grads[:3], part[:3]):
+        assert (x[1, -500:].float() - w[0, -500:].float()).abs().max() <= 2.0**-7 * w.abs().max()
+
+
 def test_strided_operands():
     """q, k, v as parts of one projection, decays and dy as slices, all unaligned."""
     a, dy = inputs(2, 90, 4, 2, 40, 24, kind=BF16)

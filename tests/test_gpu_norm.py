@@ -99,6 +99,33 @@ def test_many_rows():
         check(a, dy, dsum, groups)
 
 
+def test_more_groups_than_one_launch_takes():
+    """2^21 + 3 rows of 8 groups of 4 channels: the groups come in turns."""
+    rows = (1 << 21) + 3
+    x = torch.randn(rows, 32, device=DEV, generator=torch.Generator(device=DEV).manual_seed(1))
+    y, _, stats = ops.layer_norm(x, groups=8, with_stats=True)
+    dx, _, _ = ops.layer_norm_backward(y, x, stats, groups=8)
+    for part in (slice(0, 50), slice(rows - 50, rows), slice(rows // 2, rows // 2 + 50)):
+        ref = R.norm(x[part].cpu(), groups=8, dy=y[part].cpu())
+        R.assert_within(y[part], ref["y"], ref["my"], 2 * roundings(32, 8), "y")
+        R.assert_within(dx[part], ref["dx"], ref["mdx"], 4 * roundings(32, 8), "dx")
+
+
+def test_rows_beyond_32_bit_offsets():
+    """2.2e9 elements."""
+    rows, dim = 135000, 16384
+    if torch.cuda.mem_get_info()[0] < 30 << 30:
+        pytest.skip("needs 18 GB")
+    x = torch.empty(rows, dim, dtype=BF16, device=DEV).normal_(
+        generator=torch.Generator(device=DEV).manual_seed(1))
+    announce("layer_norm", tuple(x.shape))
+    y, _, stats = ops.layer_norm(x, with_stats=True)
+    dx, _, _ = ops.layer_norm_backward(y, x, stats)
+    want, _, st = ops.layer_norm(x[-40:], with_stats=True)
+    assert torch.equal(y[-40:], want) and torch.equal(stats[-40:], st)
+    assert torch.equal(dx[-40:], ops.layer_norm_backward(want, x[-40:], st)[0])
+
+
 def test_rows_far_from_zero():
     """A mean of 1000 times the deviation: the variance is that of the differences."""
     a, dy, dsum = inputs(4, 1024, F32, shift=1000.0)
