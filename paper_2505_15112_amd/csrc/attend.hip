@@ -122,21 +122,29 @@ __global__ void __launch_bounds__(kGateThreads) k_gate_sum(const float* in, floa
 
 // The states before every piece from what each adds, in place: a workgroup to 256
 // elements of a row and head; piece i of element x is states[i * each + x].
-__global__ void __launch_bounds__(256)
-    k_carry(float* states, const float* whole, int pieces, int64_t each, const float* first,
-            float* last) {
+struct Carry {
+    float* states;
+    const float* whole;
+    const float* first;  // nullable
+    float* last;         // nullable
+};
+struct Carries {
+    Carry c[2];
+};
+__global__ void __launch_bounds__(256) k_carry(Carries all, int pieces, int64_t each) {
+    const Carry& c = all.c[blockIdx.y];
     const int64_t groups = (each + 255) / 256, bh = blockIdx.x / groups;
     const int64_t x = blockIdx.x % groups * 256 + threadIdx.x;
     if (x >= each) return;
-    float* at = states + bh * pieces * each + x;
-    float run = first ? first[bh * each + x] : 0.0f;
+    float* at = c.states + bh * pieces * each + x;
+    float run = c.first ? c.first[bh * each + x] : 0.0f;
 #pragma unroll 8
     for (int i = 0; i < pieces; ++i) {
         const float more = at[i * each];
         at[i * each] = run;
-        run = __builtin_fmaf(whole[bh * pieces + i], run, more);
+        run = __builtin_fmaf(c.whole[bh * pieces + i], run, more);
     }
-    if (last) last[bh * each + x] = run;
+    if (c.last) c.last[bh * each + x] = run;
 }
 
 // ------------------------------------------------ a single token
@@ -210,7 +218,7 @@ __global__ void __launch_bounds__(kStepThreads)
 
 // ------------------------------------------------ launches
 
-hipError_t run(int64_t type, const Walk& w, bool states, hipStream_t stream) {
+hipError_t run(int64_t type, const Walks& w, bool states, hipStream_t stream) {
     return type == LIBSCAN_F32   ? launch_walk<float>(w, states, stream)
            : type == LIBSCAN_F16 ? launch_walk<_Float16>(w, states, stream)
                                  : launch_walk<__bf16>(w, states, stream);
@@ -245,9 +253,10 @@ WalkSide side_v(const libscan_attend& p) { return {p.v, p.v_batch, p.v_step, p.v
 struct Pieces {
     int count, places;
 };
-Pieces pieces(const libscan_attend& p) {
+// `together`: walks of one launch.
+Pieces pieces(const libscan_attend& p, int together) {
     const int64_t chunk = 64, chunks = (p.steps + chunk - 1) / chunk;
-    const int64_t groups = p.batch * p.heads * walk_blocks((int)p.dk, (int)p.dv);
+    const int64_t groups = together * p.batch * p.heads * walk_blocks((int)p.dk, (int)p.dv);
     const auto time = [](int64_t count, double full, double half) {
         const int64_t left = count % 512;
         return count / 512 * full + (left > 256 ? full : left ? half : 0.0);
@@ -261,7 +270,7 @@ Pieces pieces(const libscan_attend& p) {
         const int64_t size = (chunks + n - 1) / n, count = (chunks + size - 1) / size;
         const double cost = walk(count, size) +
                             time(groups * count, 0.8 * size + 1.4, 0.45 * size + 1.3) +
-                            p.batch * p.heads * count * p.dk * p.dv * 8 / 4.6e6 / 5 + 1;
+                            together * p.batch * p.heads * count * p.dk * p.dv * 8 / 4.6e6 / 5 + 1;
         if (cost < best) best = cost, each = size;
     }
     if (each >= chunks) return {1, (int)p.steps};
@@ -279,9 +288,10 @@ struct Room {
 };
 // What each piece adds to the states, and then the states before it.
 struct Cut {
+    Pieces n;
     int64_t states, whole;
-    Cut(const libscan_attend& p, Room& room) {
-        const int64_t n = pieces(p).count, all = n > 1 ? p.batch * p.heads * n : 0;
+    Cut(const libscan_attend& p, int together, Room& room) : n(pieces(p, together)) {
+        const int64_t all = n.count > 1 ? p.batch * p.heads * n.count : 0;
         states = room.floats(all * p.dk * p.dv);
         whole = room.floats(all);
     }
@@ -289,13 +299,13 @@ struct Cut {
 struct FrontPlan {
     Room room;
     Cut cut;
-    FrontPlan(const libscan_attend& p) : cut(p, room) {}
+    FrontPlan(const libscan_attend& p) : cut(p, 1, room) {}
 };
 struct BackPlan {
     Room room;
     Cut cut, back;  // of S, and of its gradient
     int64_t dq_dots, dk_dots, gates, last, dq, dk;
-    BackPlan(const libscan_attend& p) : cut(p, room), back(p, room) {
+    BackPlan(const libscan_attend& p) : cut(p, 2, room), back(p, 2, room) {
         const int64_t tokens = p.batch * p.steps * p.heads;
         const int64_t blocks = walk_blocks((int)p.dv, (int)p.dk);
         const bool shared = p.groups < p.heads;
@@ -308,24 +318,29 @@ struct BackPlan {
     }
 };
 
-// The states before every piece of the walk w, whose first and last states are its
-// rows'; w then takes them.
-hipError_t cut_rows(int64_t type, Walk& w, const libscan_attend& p, const Cut& cut, char* mem,
+// The states before every piece of the walks, whose first and last states are their
+// rows'; the walks then take them.
+hipError_t cut_rows(const libscan_attend& p, Walks& walks, const Cut* const (&cuts)[2], char* mem,
                     hipStream_t stream) {
-    const Pieces n = pieces(p);
-    w.pieces = n.count, w.piece = n.places;
+    const Pieces n = cuts[0]->n;
+    for (int i = 0; i < walks.count; ++i) walks.w[i].pieces = n.count, walks.w[i].piece = n.places;
     if (n.count == 1) return hipSuccess;
-    Walk states = w;
-    states.first = {};
-    states.last = {(float*)(mem + cut.states), p.dv, 1};
-    states.whole = (float*)(mem + cut.whole);
-    const hipError_t e = run(type, states, true, stream);
+    Walks states = walks;
+    Carries carries{};
+    for (int i = 0; i < walks.count; ++i) {
+        Walk &s = states.w[i], &w = walks.w[i];
+        s.first = {};
+        s.last = {(float*)(mem + cuts[i]->states), p.dv, 1};
+        s.whole = (float*)(mem + cuts[i]->whole);
+        carries.c[i] = {s.last.p, s.whole, w.first.p, w.last.p};
+        w.first = s.last;
+        w.last = {};
+    }
+    const hipError_t e = run(p.type, states, true, stream);
     if (e != hipSuccess) return e;
-    const int64_t each = p.dk * p.dv, rows = p.batch * p.heads;
-    k_carry<<<(uint32_t)(rows * ((each + 255) / 256)), 256, 0, stream>>>(
-        states.last.p, states.whole, n.count, each, w.first.p, w.last.p);
-    w.first = states.last;
-    w.last = {};
+    const int64_t each = p.dk * p.dv, blocks = p.batch * p.heads * ((each + 255) / 256);
+    if (blocks == 0) return hipSuccess;
+    k_carry<<<dim3((uint32_t)blocks, walks.count), 256, 0, stream>>>(carries, n.count, each);
     return hipGetLastError();
 }
 
@@ -343,8 +358,10 @@ hipError_t launch_attend(const libscan_attend& p, void* y, float* state_out, voi
     w.first = {const_cast<float*>(p.state), p.dv, 1};
     w.last = {state_out, p.dv, 1};
     w.out = y;
-    const hipError_t e = cut_rows(p.type, w, p, FrontPlan(p).cut, (char*)scratch, stream);
-    return e != hipSuccess ? e : run(p.type, w, false, stream);
+    const FrontPlan plan(p);
+    Walks walks{{w}, 1};
+    const hipError_t e = cut_rows(p, walks, {&plan.cut, nullptr}, (char*)scratch, stream);
+    return e != hipSuccess ? e : run(p.type, walks, false, stream);
 }
 
 hipError_t launch_attend_back(const libscan_attend& p, const void* dy, int64_t dy_batch,
@@ -360,50 +377,50 @@ hipError_t launch_attend_back(const libscan_attend& p, const void* dy, int64_t d
     float* last = dstate_out ? floats(plan.last) : nullptr;
     hipError_t e;
 
-    // S forwards, and its gradient backwards with dv
-    Walk s = base(p), g = base(p);
+    // S forwards, and its gradient G backwards
+    Walks both{{base(p), base(p)}, 2};
+    Walk &s = both.w[0], &g = both.w[1];
     s.dk = g.dk = (int)p.dk, s.dv = g.dv = (int)p.dv;
     s.k = side_k(p), s.v = side_v(p);
     s.first = {const_cast<float*>(p.state), p.dv, 1};
     s.last = {last, p.dv, 1};
-    if ((e = cut_rows(p.type, s, p, plan.cut, mem, stream)) != hipSuccess) return e;
     g.reverse = true;
-    g.q = side_k(p), g.k = side_q(p), g.v = side_dy;
+    g.k = side_q(p), g.v = side_dy;
     g.inner = (float)p.scale;
     g.first = {const_cast<float*>(dstate_out), p.dv, 1};
     g.last = {dstate, p.dv, 1};
-    g.out = dv;
-    if ((e = cut_rows(p.type, g, p, plan.back, mem, stream)) != hipSuccess) return e;
-    if ((e = run(p.type, g, false, stream)) != hipSuccess) return e;
+    if ((e = cut_rows(p, both, {&plan.cut, &plan.back}, mem, stream)) != hipSuccess) return e;
 
-    Walk w = s;  // dq, with S turned over
-    w.dk = (int)p.dv, w.dv = (int)p.dk;
-    w.q = side_dy, w.k = side_v(p), w.v = side_k(p);
-    w.outer = (float)p.scale;
-    w.first = {s.first.p, 1, p.dv};
-    w.last = {s.last.p, 1, p.dv};
-    w.out = shared ? floats(plan.dq) : dq;
-    w.wide = shared;
-    w.e = side_q(p);
-    w.dots = floats(plan.dq_dots);
-    if ((e = run(p.type, w, false, stream)) != hipSuccess) return e;
+    Walks one{{g}, 1};  // dv, with G
+    one.w[0].q = side_k(p);
+    one.w[0].out = dv;
+    if ((e = run(p.type, one, false, stream)) != hipSuccess) return e;
 
-    w.reverse = true;  // dk
-    w.q = side_v(p), w.k = side_dy, w.v = side_q(p);
-    w.inner = (float)p.scale, w.outer = 1.0f;
-    w.first = {g.first.p, 1, p.dv};
-    w.last = {};
-    w.out = shared ? floats(plan.dk) : dk;
-    w.e = side_k(p);
-    w.dots = floats(plan.dk_dots);
-    if ((e = run(p.type, w, false, stream)) != hipSuccess) return e;
+    Walks two{{s, g}, 2};  // dq with S and dk with G, turned over
+    Walk &wq = two.w[0], &wk = two.w[1];
+    wq.dk = wk.dk = (int)p.dv, wq.dv = wk.dv = (int)p.dk;
+    wq.q = side_dy, wq.k = side_v(p), wq.v = side_k(p);
+    wq.outer = (float)p.scale;
+    wq.first = {s.first.p, 1, p.dv};
+    wq.last = {s.last.p, 1, p.dv};
+    wq.out = shared ? floats(plan.dq) : dq;
+    wq.e = side_q(p);
+    wq.dots = floats(plan.dq_dots);
+    wk.q = side_v(p), wk.k = side_dy, wk.v = side_q(p);
+    wk.first = {g.first.p, 1, p.dv};
+    wk.last = {};
+    wk.out = shared ? floats(plan.dk) : dk;
+    wk.e = side_k(p);
+    wk.dots = floats(plan.dk_dots);
+    wq.wide = wk.wide = shared;
+    if ((e = run(p.type, two, false, stream)) != hipSuccess) return e;
 
     const uint32_t rows = (uint32_t)(p.batch * p.heads);
     if (rows) {
         const Gates a{floats(plan.dq_dots), floats(plan.dk_dots), dots, dstate_out, last,
                       p.dk * p.dv, p.steps ? dstate : nullptr,
                       p.fixed ? floats(plan.gates) : dlog_decay};
-        k_gates<<<rows, kGateThreads, 0, stream>>>(w, a);
+        k_gates<<<rows, kGateThreads, 0, stream>>>(g, a);
     }
     if (p.fixed && p.heads)
         k_gate_sum<<<(uint32_t)p.heads, kGateThreads, 0, stream>>>(

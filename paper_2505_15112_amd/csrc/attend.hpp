@@ -76,12 +76,18 @@ inline int walk_blocks(int dk, int dv) {
     return (dv + columns - 1) / columns;
 }
 
+// Walks of one launch: of the same sizes, and both with dots or without.
+struct Walks {
+    Walk w[2];
+    int count;
+};
+
 // One instance for each element type (attend_f32.hip and so on).  `states`: what each
 // piece adds to the state and no outputs.
 template <class T>
-hipError_t launch_walk(const Walk& w, bool states, hipStream_t stream);
-extern template hipError_t launch_walk<float>(const Walk&, bool, hipStream_t);
-extern template hipError_t launch_walk<_Float16>(const Walk&, bool, hipStream_t);
-extern template hipError_t launch_walk<__bf16>(const Walk&, bool, hipStream_t);
+hipError_t launch_walk(const Walks& walks, bool states, hipStream_t stream);
+extern template hipError_t launch_walk<float>(const Walks&, bool, hipStream_t);
+extern template hipError_t launch_walk<_Float16>(const Walks&, bool, hipStream_t);
+extern template hipError_t launch_walk<__bf16>(const Walks&, bool, hipStream_t);
 
 }  // namespace ls

@@ -2,5 +2,5 @@
 #include "attend_walk.hpp"
 
 namespace ls {
-template hipError_t launch_walk<__bf16>(const Walk&, bool, hipStream_t);
+template hipError_t launch_walk<__bf16>(const Walks&, bool, hipStream_t);
 }  // namespace ls

@@ -544,35 +544,39 @@ struct Kernel {
 template <class K>
 constexpr int kPerSimd = K::PAIRS * K::TERMS <= 4 ? K::WAVES / 2 : 2;
 
+// One walk, or two of the same sizes, one after the other in the grid.
 template <class K>
-__global__ void __launch_bounds__(K::THREADS, kPerSimd<K>) k_walk(Walk w) {
+__global__ void __launch_bounds__(K::THREADS, kPerSimd<K>) k_walk(Walks walks) {
     __shared__ typename K::Shared s;
-    K::run(w, s);
+    K::run(walks.w[blockIdx.y], s);
 }
 
 template <class T, int DK, int WAVES>
-hipError_t launch(const Walk& w, bool states, hipStream_t stream) {
+hipError_t launch(const Walks& walks, bool states, hipStream_t stream) {
+    const Walk& w = walks.w[0];
     constexpr int COLS = 16 * WAVES, THREADS = 64 * WAVES, NARROW = kTerms<T> == 3 ? 3 : 2;
-    const int64_t grid = (int64_t)w.batch * w.heads * w.pieces * ((w.dv + COLS - 1) / COLS);
-    if (grid == 0) return hipSuccess;
+    const int64_t blocks = (int64_t)w.batch * w.heads * w.pieces * ((w.dv + COLS - 1) / COLS);
+    if (blocks == 0) return hipSuccess;
+    const dim3 grid((uint32_t)blocks, walks.count);
     if (states)
-        k_walk<Kernel<T, 1, 3, DK, WAVES, false, false>><<<(uint32_t)grid, THREADS, 0, stream>>>(w);
+        k_walk<Kernel<T, 1, 3, DK, WAVES, false, false>><<<grid, THREADS, 0, stream>>>(walks);
     else if (!w.dots)
         k_walk<Kernel<T, NARROW, NARROW, DK, WAVES, true, false>>
-            <<<(uint32_t)grid, THREADS, 0, stream>>>(w);
+            <<<grid, THREADS, 0, stream>>>(walks);
     else
-        k_walk<Kernel<T, 3, 3, DK, WAVES, true, true>><<<(uint32_t)grid, THREADS, 0, stream>>>(w);
+        k_walk<Kernel<T, 3, 3, DK, WAVES, true, true>><<<grid, THREADS, 0, stream>>>(walks);
     return hipGetLastError();
 }
 
 }  // namespace walk
 
 template <class T>
-hipError_t launch_walk(const Walk& w, bool states, hipStream_t stream) {
+hipError_t launch_walk(const Walks& walks, bool states, hipStream_t stream) {
+    const Walk& w = walks.w[0];
     const bool wide = walk_columns(w.dk, w.dv) == 128;
     const auto by_width = [&](auto dk) {
-        return wide ? walk::launch<T, dk.value, 8>(w, states, stream)
-                    : walk::launch<T, dk.value, 4>(w, states, stream);
+        return wide ? walk::launch<T, dk.value, 8>(walks, states, stream)
+                    : walk::launch<T, dk.value, 4>(walks, states, stream);
     };
     if (w.dk > 128) return by_width(std::integral_constant<int, 256>());
     if (w.dk > 64) return by_width(std::integral_constant<int, 128>());
