@@ -72,6 +72,7 @@ __global__ void __launch_bounds__(kGateThreads) k_gates(Walk w, Gates a) {
     const float* g = w.g + b * w.g_batch + h;
     double carry = 0.0;
     if (a.dstate_out) {
+#pragma unroll 8
         for (int64_t i = tid; i < a.state; i += kGateThreads)
             carry += (double)a.dstate_out[own + i] * a.last[own + i];
         double before = carry;
@@ -105,6 +106,7 @@ __global__ void __launch_bounds__(kGateThreads) k_gates(Walk w, Gates a) {
     }
     if (a.dstate && len > 0) {
         const float decay = exp2_fast(g[0] * kLog2e);
+#pragma unroll 8
         for (int64_t i = tid; i < a.state; i += kGateThreads) a.dstate[own + i] *= decay;
     }
 }
@@ -249,7 +251,8 @@ WalkSide side_v(const libscan_attend& p) { return {p.v, p.v_batch, p.v_step, p.v
 // longer carry, which reads and writes every piece's state.  The times that are weighed
 // up are those of 128 x 128 states in bf16, in units of 5 us: 512 workgroups (two to a CU) walk
 // n chunks of 64 tokens in 2 n + 1.5 and run for their states in 0.8 n + 1.4, 256 in 1.2 n
-// + 1.5 and 0.45 n + 1.3; the carry moves 4.6 TB/s; two launches take 1.
+// + 1.5 and 0.45 n + 1.3; the carry moves 4.6 TB/s; two launches take 1.  fp32's chunks
+// take more than twice as long, in six products for one or two.
 struct Pieces {
     int count, places;
 };
@@ -261,15 +264,16 @@ Pieces pieces(const libscan_attend& p, int together) {
         const int64_t left = count % 512;
         return count / 512 * full + (left > 256 ? full : left ? half : 0.0);
     };
+    const double slow = p.type == LIBSCAN_F32 ? 2.2 : 1.0;
     const auto walk = [&](int64_t n, int64_t size) {
-        return time(groups * n, 2.0 * size + 1.5, 1.2 * size + 1.5);
+        return time(groups * n, slow * 2.0 * size + 1.5, slow * 1.2 * size + 1.5);
     };
     int64_t each = chunks;
     double best = walk(1, chunks);
-    for (int64_t n = 2; n <= chunks / 2 && groups * n <= 2048; ++n) {
+    for (int64_t n = 2; n <= chunks && groups * n <= 2048; ++n) {
         const int64_t size = (chunks + n - 1) / n, count = (chunks + size - 1) / size;
         const double cost = walk(count, size) +
-                            time(groups * count, 0.8 * size + 1.4, 0.45 * size + 1.3) +
+                            time(groups * count, slow * 0.8 * size + 1.4, slow * 0.45 * size + 1.3) +
                             together * p.batch * p.heads * count * p.dk * p.dv * 8 / 4.6e6 / 5 + 1;
         if (cost < best) best = cost, each = size;
     }

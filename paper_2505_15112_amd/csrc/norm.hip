@@ -160,12 +160,12 @@ struct Grad {
 
 // The gradients likewise: the teams of a workgroup take rows of one group of channels,
 // the next row's elements on their way while one is worked on, and add up dweight
-// and dbias of their columns in registers, then over the teams in order.
-// part[block of the group][2][dim].
+// and dbias of their columns in registers, then over the teams in order.  Block i of a
+// group has its sums at dweight + i * apart and dbias + i * apart (nullable).
 constexpr int kBackThreads = 1024;
 template <class T, class W, int LANES, int NV>
 __global__ void __launch_bounds__(kBackThreads)
-    k_norm_back(libscan_norm p, Grad g, T* dx, float* part) {
+    k_norm_back(libscan_norm p, Grad g, T* dx, float* dweight, float* dbias, int64_t apart) {
     constexpr int V = kVec<T>, TEAMS = kBackThreads / LANES;
     // teams within a wave are joined by shifts, those left take turns in LDS
     constexpr int TURNS = LANES < 64 ? kBackThreads / 64 : TEAMS, COLS = LANES * NV * V;
@@ -291,15 +291,15 @@ __global__ void __launch_bounds__(kBackThreads)
     }
     // the last turn's threads have the sums
     if (threadIdx.x / TURN != TURNS - 1 || !mine) return;
-    float* to = part + 2 * (int64_t)block * p.dim + c0;
+    const int64_t to = block * apart + c0;
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
         const int c = (i * LANES + lane) * V;
 #pragma unroll
         for (int e = 0; e < V; ++e)
             if (c + e < per) {
-                to[c + e] = dw[i][e];
-                to[p.dim + c + e] = db[i][e];
+                if (dweight) dweight[to + c + e] = dw[i][e];
+                if (dbias) dbias[to + c + e] = db[i][e];
             }
     }
 }
@@ -558,17 +558,21 @@ hipError_t launch_norm_back(const libscan_norm& p, const void* dy, int64_t dy_ba
     return by_type(p, [&](auto type, auto weights) {
         using T = decltype(type);
         using W = decltype(weights);
+        // one block's sums are the sums
+        const bool whole = t.lanes && count == 1;
         if (all && t.lanes)
             by_team<2>(t, [&](auto lanes, auto vectors) {
                 k_norm_back<T, W, lanes.value, vectors.value>
-                    <<<(uint32_t)(count * p.groups), kBackThreads, 0, stream>>>(p, g, (T*)dx, part);
+                    <<<(uint32_t)(count * p.groups), kBackThreads, 0, stream>>>(
+                        p, g, (T*)dx, whole ? dweight : part, whole ? dbias : part + p.dim,
+                        2 * p.dim);
             });
         if (all && !t.lanes) {
             k_norm_long_dx<T, W><<<capped(all), kThreads, 0, stream>>>(p, g, (T*)dx);
             k_norm_long_dw<T><<<(uint32_t)(count * ((p.dim + kPartCols - 1) / kPartCols)),
                                 kPartThreads, 0, stream>>>(p, g, part);
         }
-        if (!dweight && !dbias) return;
+        if (whole || (!dweight && !dbias)) return;
         if (long_sum(count))
             k_norm_sum<8><<<(uint32_t)((2 * p.dim + kSumOuts<8> - 1) / kSumOuts<8>), kSumThreads, 0,
                             stream>>>(part, count, p.dim, dweight, dbias);
