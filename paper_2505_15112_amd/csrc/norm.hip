@@ -517,7 +517,8 @@ int64_t parts(const libscan_norm& p) {
     if (!t.lanes) return (rows + kPartRows - 1) / kPartRows;
     const int64_t teams = kBackThreads / t.lanes, blocks = (rows + teams - 1) / teams;
     // a workgroup to a CU, two where rows are short
-    const int64_t most = p.groups >= 512 ? 1 : 512 / p.groups;
+    // a workgroup to a CU: twice as many take turns (8192 x 4096, bf16: 70 us, not 60)
+    const int64_t most = p.groups >= 256 ? 1 : 256 / p.groups;
     return blocks < most ? blocks : most;
 }
 
