@@ -133,18 +133,29 @@ struct Carry {
 struct Carries {
     Carry c[2];
 };
+// AHEAD loads on their way; the chain itself is a multiply-add each.  16 are for the few rows
+// that are cut into many pieces (52 pieces of 8 rows' 64 x 128: 15 to 7 us); where there
+// are enough threads without them they cost (64 rows' 8 pieces of 128 x 128: 14 to 18).
+template <int AHEAD>
 __global__ void __launch_bounds__(256) k_carry(Carries all, int pieces, int64_t each) {
     const Carry& c = all.c[blockIdx.y];
     const int64_t groups = (each + 255) / 256, bh = blockIdx.x / groups;
     const int64_t x = blockIdx.x % groups * 256 + threadIdx.x;
     if (x >= each) return;
     float* at = c.states + bh * pieces * each + x;
+    const float* whole = c.whole + bh * pieces;
     float run = c.first ? c.first[bh * each + x] : 0.0f;
-#pragma unroll 8
-    for (int i = 0; i < pieces; ++i) {
-        const float more = at[i * each];
-        at[i * each] = run;
-        run = __builtin_fmaf(c.whole[bh * pieces + i], run, more);
+    for (int first = 0; first < pieces; first += AHEAD) {
+        float more[AHEAD], decay[AHEAD];
+#pragma unroll
+        for (int i = 0; i < AHEAD; ++i)
+            if (first + i < pieces) more[i] = at[(first + i) * each], decay[i] = whole[first + i];
+#pragma unroll
+        for (int i = 0; i < AHEAD; ++i) {
+            if (first + i >= pieces) break;
+            at[(first + i) * each] = run;
+            run = __builtin_fmaf(decay[i], run, more[i]);
+        }
     }
     if (c.last) c.last[bh * each + x] = run;
 }
@@ -344,7 +355,11 @@ hipError_t cut_rows(const libscan_attend& p, Walks& walks, const Cut* const (&cu
     if (e != hipSuccess) return e;
     const int64_t each = p.dk * p.dv, blocks = p.batch * p.heads * ((each + 255) / 256);
     if (blocks == 0) return hipSuccess;
-    k_carry<<<dim3((uint32_t)blocks, walks.count), 256, 0, stream>>>(carries, n.count, each);
+    const dim3 grid((uint32_t)blocks, walks.count);
+    if (n.count > 8)
+        k_carry<16><<<grid, 256, 0, stream>>>(carries, n.count, each);
+    else
+        k_carry<8><<<grid, 256, 0, stream>>>(carries, n.count, each);
     return hipGetLastError();
 }
 
