@@ -527,7 +527,8 @@ int selective_scan_step(const libscan_ssm* p, float* states, int64_t n_states,
  * q, k: batch x steps x groups x dk; v, y: batch x steps x heads x dv, with unit
  * stride over the last dimension.  log_decay: fp32, batch x steps x heads with
  * unit stride over heads, or (fixed != 0) heads, one for all tokens; 0 keeps the
- * state, -infinity clears it.  state (nullable: zeros): batch x heads x dk x dv,
+ * state, -infinity clears it; values above 0 let it grow, and products of decays over
+ * 32 tokens have to stay within fp32.  state (nullable: zeros): batch x heads x dk x dv,
  * dense fp32.  1 <= dk, dv <= 256, heads a multiple of groups.  An infinity or a NaN
  * in an operand makes the outputs that it reaches infinite or NaN (which of the two is
  * not said), and no others: of v, one column of its head; of any, no earlier token. */
