@@ -309,6 +309,28 @@ def test_the_same_call_twice_gives_the_same_bits():
         assert all(torch.equal(x, w) for x, w in zip(again, first))
 
 
+def test_given_outputs_and_scratch():
+    """The caller's outputs, and scratch of just the size that is asked for, whatever it holds."""
+    a, dy = inputs(2, 300, 4, 2, 64, 96, kind=BF16, state=True, fixed=True)
+    d, dy = dev(a), dy.to(DEV)
+    y, last = ops.linear_attention(**d, with_state=True)
+    grads = ops.linear_attention_backward(dy, **d, dstate_out=last)
+    p = ops._args.attend(d["q"], d["k"], d["v"], d["log_decay"], d["state"], None, None, False)
+    front, back = ops._sizes("linear_attention_bytes", p, 2)
+    assert front > 0 and back > 0
+    for fill in (0xff, 0x7f, 0):
+        out, end = torch.full_like(y, 3.0), torch.full_like(last, 3.0)
+        got = ops.linear_attention(**d, out=out, state_out=end, scratch_buf=torch.full(
+            (front,), fill, dtype=torch.uint8, device=DEV))
+        assert got[0] is out and got[1] is end
+        assert torch.equal(out, y) and torch.equal(end, last)
+        again = ops.linear_attention_backward(dy, **d, dstate_out=last, scratch_buf=torch.full(
+            (back,), fill, dtype=torch.uint8, device=DEV))
+        assert all(torch.equal(g, w) for g, w in zip(again, grads))
+    with pytest.raises(ops._lib.LibscanError):
+        ops.linear_attention(**d, scratch_buf=torch.empty(front - 1, dtype=torch.uint8, device=DEV))
+
+
 # ---------------------------------------------------------------- single tokens
 
 @pytest.mark.parametrize("size", [(1, 1, 1, 1, 1), (3, 4, 2, 64, 64), (2, 3, 3, 128, 128),
@@ -441,7 +463,7 @@ def test_refusals():
             (dict(k=d["k"].half()), TypeError, "k"), (dict(v=None), TypeError, "v"),
             (dict(log_decay=d["log_decay"].half()), TypeError, "log_decay"),
             (dict(log_decay=d["log_decay"][:, :3]), ValueError, "log_decay"),
-            (dict(q=d["q"].transpose(2, 3)), ValueError, ""),
+            (dict(q=d["q"].transpose(2, 3)), ValueError, "q|k"),
             (dict(state=torch.zeros(2, 4, 6, 8, device=DEV)), ValueError, "state"),
             (dict(lengths=torch.zeros(3, dtype=torch.int32, device=DEV)), ValueError, "lengths"),
             (dict(lengths=torch.zeros(2, dtype=torch.int64, device=DEV)), TypeError, "lengths"),
