@@ -124,10 +124,12 @@ __global__ void __launch_bounds__(kGateThreads) k_gate_sum(const float* in, floa
 }
 
 // The states before every piece from what each adds, in place: a workgroup to 256
-// elements of a row and head; piece i of element x is states[i * each + x].
+// elements of a row and head; piece i of element x is states[i * each + x].  A piece's
+// product of decays, x 2^y (WholePiece), may be beyond fp32 where the state that it meets is 0
+// or small: the state is scaled by the exponent, which leaves 0 what it is.
 struct Carry {
     float* states;
-    const float* whole;
+    const WholePiece* whole;
     const float* first;  // nullable
     float* last;         // nullable
 };
@@ -144,10 +146,11 @@ __global__ void __launch_bounds__(256) k_carry(Carries all, int pieces, int64_t 
     const int64_t x = blockIdx.x % groups * 256 + threadIdx.x;
     if (x >= each) return;
     float* at = c.states + bh * pieces * each + x;
-    const float* whole = c.whole + bh * pieces;
+    const WholePiece* whole = c.whole + bh * pieces;
     float run = c.first ? c.first[bh * each + x] : 0.0f;
     for (int first = 0; first < pieces; first += AHEAD) {
-        float more[AHEAD], decay[AHEAD];
+        float more[AHEAD];
+        WholePiece decay[AHEAD];
 #pragma unroll
         for (int i = 0; i < AHEAD; ++i)
             if (first + i < pieces) more[i] = at[(first + i) * each], decay[i] = whole[first + i];
@@ -155,7 +158,7 @@ __global__ void __launch_bounds__(256) k_carry(Carries all, int pieces, int64_t 
         for (int i = 0; i < AHEAD; ++i) {
             if (first + i >= pieces) break;
             at[(first + i) * each] = run;
-            run = __builtin_fmaf(decay[i], run, more[i]);
+            run = __builtin_amdgcn_ldexpf(decay[i].factor * run, decay[i].exponent) + more[i];
         }
     }
     if (c.last) c.last[bh * each + x] = run;
@@ -320,7 +323,7 @@ struct Cut {
     Cut(const libscan_attend& p, int together, Room& room) : n(pieces(p, together)) {
         const int64_t all = n.count > 1 ? p.batch * p.heads * n.count : 0;
         states = room.floats(all * p.dk * p.dv);
-        whole = room.floats(all);
+        whole = room.floats(all * (int64_t)(sizeof(WholePiece) / 4));
     }
 };
 struct FrontPlan {
@@ -358,7 +361,7 @@ hipError_t cut_rows(const libscan_attend& p, Walks& walks, const Cut* const (&cu
         Walk &s = states.w[i], &w = walks.w[i];
         s.first = {};
         s.last = {(float*)(mem + cuts[i]->states), p.dv, 1};
-        s.whole = (float*)(mem + cuts[i]->whole);
+        s.whole = (WholePiece*)(mem + cuts[i]->whole);
         carries.c[i] = {s.last.p, s.whole, w.first.p, w.last.p};
         w.first = s.last;
         w.last = {};

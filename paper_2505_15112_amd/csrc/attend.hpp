@@ -27,6 +27,13 @@ struct WalkState {
     int64_t row, col;
 };
 
+// The product of a piece's decays, factor * 2^exponent with a factor of 0.5 to 1: over
+// hundreds of tokens it may be beyond fp32 both ways.
+struct WholePiece {
+    float factor;
+    int exponent;
+};
+
 struct Walk {
     int batch, steps, heads, dk, dv;
     bool reverse;
@@ -42,7 +49,7 @@ struct Walk {
     // (one for each row, head and piece) begin with, nullable; and the last ones: the
     // row's, if pieces == 1, or in a run for the states alone what each piece adds.
     WalkState first, last;
-    float* whole;  // in such a run, for each row, head and piece: the product of its decays
+    WholePiece* whole;  // in such a run, for each row, head and piece: the product of its decays
     // Output: batch x steps x heads x dv, dense; fp32 where `wide`.  With `dots`
     // (batch x steps x heads for each block of columns), the sums of the output
     // times e, before it is rounded; it is then formed to fp32's precision.
@@ -51,6 +58,9 @@ struct Walk {
     WalkSide e;
     float* dots;
 };
+
+// A logarithm past -1024 to base 2 is one of 0: what decays by it is gone.
+__device__ __forceinline__ bool clears(float g) { return g < -709.79f; }
 
 __device__ __forceinline__ int walk_len(const Walk& w, int b) {
     if (!w.lengths) return w.steps;

@@ -449,7 +449,8 @@ struct Kernel {
                     s.in[lane] = exp2_fast((float)sum) * w.outer;
                     s.left[lane] = exp2_fast((float)(last - sum)) * w.inner;
                 }
-                total += last;
+                // a cleared state stays so, however much the piece's other decays grow
+                total += __any(clears(decay)) ? -1e30 : last;
                 if (lane == 0) s.whole = exp2_fast((float)last);
             }
             __syncthreads();
@@ -540,7 +541,12 @@ struct Kernel {
         }
         if (w.last.p && (!OUT || w.pieces == 1) && column < w.dv)
             store_state(state, w.last.p + number * w.dk * w.dv, w, w.last, column, g);
-        if (!OUT && block == 0 && tid == 0) w.whole[number] = exp2_fast((float)total);
+        if (!OUT && block == 0 && tid == 0) {
+            // no product of 2^8192 leaves a state in fp32; a NaN goes into the factor
+            const double up = __builtin_ceil(total), most = 8192.0;
+            w.whole[number] = {exp2_fast((float)(total - up)),
+                               (int)__builtin_fmax(__builtin_fmin(up, most), -most)};
+        }
     }
 };
 
