@@ -136,8 +136,10 @@ int check_logits(const libscan_logits* p) {
 int check_attend(const libscan_attend* p) {
     if (!p || !known(p->type)) return LIBSCAN_EINVAL;
     if (p->dk < 1 || p->dv < 1 || p->heads < 0 || p->groups < 1) return LIBSCAN_EINVAL;
-    if (p->dk > 256 || p->dv > 256 || p->heads > (1 << 16)) return LIBSCAN_ERANGE;
-    const int r = check_sizes(p->batch, p->steps, p->heads * (p->dk > p->dv ? p->dk : p->dv));
+    // without heads there are groups all the same, and their gradients
+    const int64_t most = p->heads ? p->heads : p->groups;
+    if (p->dk > 256 || p->dv > 256 || most > (1 << 16)) return LIBSCAN_ERANGE;
+    const int r = check_sizes(p->batch, p->steps, most * (p->dk > p->dv ? p->dk : p->dv));
     if (r != LIBSCAN_OK) return r;
     if (p->heads % p->groups) return LIBSCAN_EINVAL;
     // at most two workgroups to a row's head (more only where there are few)
@@ -372,7 +374,7 @@ int linear_attention_backward(const libscan_attend* p, const void* dy, int64_t d
     Span in[kAttendInputs + 2];
     Span(&first)[kAttendInputs] = (Span(&)[kAttendInputs])in;
     if (!attend_inputs(p, first)) return LIBSCAN_EINVAL;
-    if (b * t * h && (!dy || !dq || !dk || !dv)) return LIBSCAN_EINVAL;
+    if ((b * t * h && (!dy || !dv)) || (shared && (!dq || !dk))) return LIBSCAN_EINVAL;
     if ((p->fixed ? h : b * t * h) && !dlog_decay) return LIBSCAN_EINVAL;
     const size_t need = ls::attend_back_scratch_bytes(*p);
     in[kAttendInputs] = strided(dy, es, b, dy_batch, t, dy_step, h, dy_head, p->dv);

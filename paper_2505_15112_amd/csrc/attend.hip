@@ -405,7 +405,7 @@ hipError_t launch_attend_back(const libscan_attend& p, const void* dy, int64_t d
     const BackPlan plan(p);
     char* mem = (char*)scratch;
     const auto floats = [&](int64_t at) { return (float*)(mem + at); };
-    const bool shared = p.groups < p.heads;
+    const bool shared = p.groups != p.heads;  // without heads, the groups' sums are over none
     const WalkSide side_dy = {dy, dy_batch, dy_step, dy_head, 1};
     const int dots = walk_blocks((int)p.dv, (int)p.dk);
     float* last = dstate_out ? floats(plan.last) : nullptr;
