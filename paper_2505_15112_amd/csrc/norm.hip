@@ -162,20 +162,22 @@ struct Grad {
 // The gradients likewise: the teams of a workgroup take rows of one group of channels,
 // the next row's elements on their way while one is worked on, and add up dweight
 // and dbias of their columns in registers, then over the teams in order.  Block i of a
-// group has its sums at dweight + i * apart and dbias + i * apart (nullable).  8192 x
+// group has its sums at dweight + i * apart and dbias + i * apart (nullable).  A launch takes
+// `some` groups from the first on.  8192 x
 // 4096, bf16, with dsum: 60 us for 268 MB, 4.4 TB/s.
 constexpr int kBackThreads = 1024;
 template <class T, class W, int LANES, int NV>
 __global__ void __launch_bounds__(kBackThreads)
-    k_norm_back(libscan_norm p, Grad g, T* dx, float* dweight, float* dbias, int64_t apart) {
+    k_norm_back(libscan_norm p, Grad g, T* dx, float* dweight, float* dbias, int64_t apart,
+                int first, int some) {
     constexpr int V = kVec<T>, TEAMS = kBackThreads / LANES;
     // teams within a wave are joined by shifts, those left take turns in LDS
     constexpr int TURNS = LANES < 64 ? kBackThreads / 64 : TEAMS, COLS = LANES * NV * V;
     __shared__ float s[2][kBackThreads / 64 * 2], s_sum[TURNS > 1 ? 2 : 1][TURNS > 1 ? COLS : 1];
     const int lane = threadIdx.x % LANES, team = threadIdx.x / LANES;
     const int per = (int)(p.dim / p.groups), groups = (int)p.groups;
-    const int group = blockIdx.x % groups, block = blockIdx.x / groups;
-    const int64_t rows = p.batch * p.steps, every = (int64_t)(gridDim.x / groups) * TEAMS;
+    const int group = first + blockIdx.x % some, block = blockIdx.x / some;
+    const int64_t rows = p.batch * p.steps, every = (int64_t)(gridDim.x / some) * TEAMS;
     const int c0 = group * per;
     Pack<W, V> w[NV];
     float dw[NV][V], db[NV][V];
@@ -511,7 +513,7 @@ void by_team(const Team& t, F f) {
     else f(all, std::integral_constant<int, 2>());
 }
 
-constexpr int64_t kMostBlocks = 1 << 20;  // the rest in further turns
+constexpr int64_t kMostBlocks = 1 << 20;  // the rest in further turns or launches
 uint32_t capped(int64_t blocks) { return (uint32_t)(blocks < kMostBlocks ? blocks : kMostBlocks); }
 
 // Rows of a block of k_norm_long_dw: 64 blocks, unless that is a few rows each.
@@ -574,10 +576,15 @@ hipError_t launch_norm_back(const libscan_norm& p, const void* dy, int64_t dy_ba
         if (all && t.lanes)
             by_team(t, [&](auto lanes, auto vectors) {
                 if constexpr (vectors.value == 1 || sizeof(T) == 4)
-                    k_norm_back<T, W, lanes.value, vectors.value>
-                        <<<(uint32_t)(count * p.groups), kBackThreads, 0, stream>>>(
-                            p, g, (T*)dx, whole ? dweight : part, whole ? dbias : part + p.dim,
-                            2 * p.dim);
+                    // (more than one block to a group only up to 256 groups)
+                    for (int64_t first = 0; first < p.groups; first += kMostBlocks) {
+                        const int64_t left = p.groups - first;
+                        const int some = (int)(left < kMostBlocks ? left : kMostBlocks);
+                        k_norm_back<T, W, lanes.value, vectors.value>
+                            <<<(uint32_t)(count * some), kBackThreads, 0, stream>>>(
+                                p, g, (T*)dx, whole ? dweight : part, whole ? dbias : part + p.dim,
+                                2 * p.dim, (int)first, some);
+                    }
             });
         if (all && !t.lanes) {
             k_norm_long_dx<T, W><<<capped(all), kThreads, 0, stream>>>(p, g, (T*)dx);
