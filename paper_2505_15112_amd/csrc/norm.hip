@@ -225,18 +225,20 @@ __global__ void __launch_bounds__(kBackThreads)
         const float mean = now.stats.x, rstd = now.stats.y;
         float m[2] = {0.0f, 0.0f};
 #pragma unroll
-        for (int i = 0; i < NV; ++i)
+        for (int i = 0; i < NV; ++i) {
+            const int left = per - (i * LANES + lane) * V;
 #pragma unroll
             for (int e = 0; e < V; ++e) {
-                // behind the group's end dy is 0
+                // behind the group's end dy is 0, but (0 - mean) rstd may be an infinity
                 const float d = to_f32(now.dy[i].v[e]);
-                const float hat = (to_f32(now.x[i].v[e]) - mean) * rstd;
+                const float hat = e < left ? (to_f32(now.x[i].v[e]) - mean) * rstd : 0.0f;
                 const float u = d * to_f32(w[i].v[e]);
                 m[0] += u;
                 m[1] = __builtin_fmaf(u, hat, m[1]);
                 dw[i][e] = __builtin_fmaf(d, hat, dw[i][e]);
                 db[i][e] += d;
             }
+        }
         team_sums<LANES>(m, s[turn]);
         const float m0 = m[0] / per, m1 = m[1] / per;
         if (on) {
