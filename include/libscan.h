@@ -559,9 +559,10 @@ int linear_attention(const libscan_attend* p, void* y, float* state_out, void* s
 /* Gradients for dy (batch x steps x heads x dv, strides dy_batch, dy_step, dy_head)
  * and dstate_out (nullable, batch x heads x dk x dv fp32: the gradient of the last
  * state), from the same *p: dq, dk (of the groups), dv, of `type`; dlog_decay (of
- * log_decay's shape: 0 where the decay is -infinity) and dstate (nullable: batch x
- * heads x dk x dv), fp32.  Sums run in a fixed order.  A token's dlog_decay is formed
- * of q dq - k dk of the tokens from it on: an infinity or a NaN there reaches it. */
+ * log_decay's shape: 0 where the decay is -infinity, or below -709.79, which clears the
+ * state likewise) and dstate (nullable: batch x heads x dk x dv), fp32.  Sums run in a
+ * fixed order.  A token's dlog_decay is formed of q dq - k dk of the tokens from it on, up
+ * to the next one that clears the state: an infinity or a NaN there reaches it. */
 int linear_attention_backward(const libscan_attend* p, const void* dy, int64_t dy_batch,
                               int64_t dy_step, int64_t dy_head, const float* dstate_out, void* dq,
                               void* dk, void* dv, float* dlog_decay, float* dstate, void* scratch,

@@ -25,35 +25,48 @@ __global__ void __launch_bounds__(256) k_join_heads(const float* dq_in, const fl
     }
 }
 
-// Sums over the workgroup's threads, in 64 bits: v becomes the sum over the threads
-// before this one (no difference of sums: a NaN of its own or behind it is not in it);
-// returns that of all.
+// A sum in 64 bits, over what comes behind the last place that starts it anew.
+struct Run {
+    double sum;
+    int anew;  // there is such a place
+};
+__device__ __forceinline__ Run then(const Run& a, const Run& b) {
+    return b.anew ? b : Run{a.sum + b.sum, a.anew};
+}
+
+// Runs over the workgroup's threads: v becomes the run over the threads before this one (no
+// difference of sums: a NaN of its own or behind it is not in it); returns that of all.
 constexpr int kGateThreads = 256, kGateWaves = kGateThreads / 64;
-__device__ double block_scan(double& v, double* s) {
+__device__ Run block_scan(Run& v, Run* s) {
     const int lane = threadIdx.x % 64, wave = threadIdx.x / 64;
 #pragma unroll
     for (int m = 1; m < 64; m <<= 1) {
-        const double up = __shfl_up(v, m);
-        if (lane >= m) v += up;
+        const Run up{__shfl_up(v.sum, m), __shfl_up(v.anew, m)};
+        if (lane >= m) v = then(up, v);
     }
     if (lane == 63) s[wave] = v;
-    v = __shfl_up(v, 1);
-    if (lane == 0) v = 0.0;
+    v = {__shfl_up(v.sum, 1), __shfl_up(v.anew, 1)};
+    if (lane == 0) v = {};
     __syncthreads();
-    double all = 0.0;
+    Run all{};
 #pragma unroll
     for (int i = 0; i < kGateWaves; ++i) {
-        if (i == wave) v += all;
-        all += s[i];
+        if (i == wave) v = then(all, v);
+        all = then(all, s[i]);
     }
     __syncthreads();
     return all;
 }
+__device__ double block_sum(double v, Run* s) {
+    Run run{v, 0};
+    return block_scan(run, s).sum;
+}
 
 // The decays' gradients: dg[t] = sum over s >= t of (q.dq - k.dk)[s], and the part
 // of the last state, <dS, S>; and dS_0 = e^g[0] G[0], in place (a row without tokens
-// keeps dS).  A workgroup to a row and head; eight tokens to a thread (64 rows of 2048
-// tokens: 11 us; with one token to a thread 20).
+// keeps dS).  A token whose decay clears the state has a gradient of 0, and those before
+// it have no part in the sums behind it, which start anew there.  A workgroup to a row and head; eight
+// tokens to a thread (64 rows of 2048 tokens: 11 us; with one token to a thread 20).
 struct Gates {
     const float* dq_dots;
     const float* dk_dots;
@@ -66,44 +79,46 @@ struct Gates {
 };
 __global__ void __launch_bounds__(kGateThreads) k_gates(Walk w, Gates a) {
     constexpr int PER = 8;
-    __shared__ double s[kGateWaves];
+    __shared__ Run s[kGateWaves];
     const int h = blockIdx.x % w.heads, b = blockIdx.x / w.heads, tid = threadIdx.x;
     const int len = walk_len(w, b);
     const int64_t all = (int64_t)w.batch * w.steps * w.heads, own = blockIdx.x * a.state;
     const float* g = w.g + b * w.g_batch + h;
-    double carry = 0.0;
+    Run carry{};
     if (a.dstate_out) {
+        double v = 0.0;
 #pragma unroll 8
         for (int64_t i = tid; i < a.state; i += kGateThreads)
-            carry += (double)a.dstate_out[own + i] * a.last[own + i];
-        double before = carry;
-        carry = block_scan(before, s);
+            v += (double)a.dstate_out[own + i] * a.last[own + i];
+        carry.sum = block_sum(v, s);
     }
     for (int end = w.steps; end > 0; end -= kGateThreads * PER) {
         const int t0 = end - 1 - tid * PER;  // thread 0 has the last tokens
         const int64_t at = ((int64_t)b * w.steps + t0) * w.heads + h;
-        double v[PER], sum = 0.0;
+        Run v[PER], sum{};
 #pragma unroll
         for (int i = 0; i < PER; ++i) {
-            v[i] = 0.0;
-            if (t0 - i >= 0 && t0 - i < len)
+            v[i] = {};
+            if (t0 - i < 0 || t0 - i >= len) continue;
+            v[i].anew = clears(g[(t0 - i) * w.g_step]);
+            if (!v[i].anew)
                 for (int k = 0; k < a.blocks; ++k)
-                    v[i] += (double)a.dq_dots[k * all + at - (int64_t)i * w.heads] -
-                            a.dk_dots[k * all + at - (int64_t)i * w.heads];
+                    v[i].sum += (double)a.dq_dots[k * all + at - (int64_t)i * w.heads] -
+                                a.dk_dots[k * all + at - (int64_t)i * w.heads];
         }
 #pragma unroll
-        for (int i = 0; i < PER; ++i) v[i] = sum += v[i];
-        const double more = block_scan(sum, s);
+        for (int i = 0; i < PER; ++i) {
+            v[i] = sum = then(sum, v[i]);
+        }
+        const Run more = block_scan(sum, s);
+        const Run before = then(carry, sum);
 #pragma unroll
         for (int i = 0; i < PER; ++i) {
             const int t = t0 - i;
             if (t < 0) break;
-            // a decay of -infinity leaves nothing to change
-            a.out[at - (int64_t)i * w.heads] =
-                t < len && g[t * w.g_step] != -__builtin_inff()
-                    ? (float)(carry + sum + v[i]) : 0.0f;
+            a.out[at - (int64_t)i * w.heads] = t < len ? (float)then(before, v[i]).sum : 0.0f;
         }
-        carry += more;
+        carry = then(carry, more);
     }
     if (a.dstate && len > 0) {
         const float decay = exp2_fast(g[0] * kLog2e);
@@ -115,11 +130,11 @@ __global__ void __launch_bounds__(kGateThreads) k_gates(Walk w, Gates a) {
 // One decay for all tokens of a head: the sum of their gradients.
 __global__ void __launch_bounds__(kGateThreads) k_gate_sum(const float* in, float* out,
                                                            int64_t tokens, int heads) {
-    __shared__ double s[kGateWaves];
+    __shared__ Run s[kGateWaves];
     double v = 0.0;
 #pragma unroll 8
     for (int64_t i = threadIdx.x; i < tokens; i += kGateThreads) v += in[i * heads + blockIdx.x];
-    v = block_scan(v, s);
+    v = block_sum(v, s);
     if (threadIdx.x == 0) out[blockIdx.x] = (float)v;
 }
 
