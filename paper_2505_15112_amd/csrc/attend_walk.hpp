@@ -106,6 +106,18 @@ struct Tile {
             f.t[t] = *reinterpret_cast<const bf8*>(&v[t][row][col]);
         return f;
     }
+    // The values of four elements along a row.
+    __device__ __forceinline__ f4 four(int row, int col) const {
+        f4 sum{};
+#pragma unroll
+        for (int t = TERMS - 1; t >= 0; --t) {
+            typedef __bf16 bf4 __attribute__((ext_vector_type(4)));
+            const bf4 x = *reinterpret_cast<const bf4*>(&v[t][row][col]);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) sum[e] += (float)x[e];
+        }
+        return sum;
+    }
     // Eight elements down a column, rows row + 8 (l / 16) and on, of 16 columns: `col` is
     // where this lane's four (those of all lanes l % 4) lie, and lane l gets
     // element l % 4 of the four that lane (l % 16) / 4 names.
@@ -239,8 +251,11 @@ __device__ __forceinline__ float high_part(double c) {
 constexpr int kChunk = 32;
 
 // TP terms of scores and states, LIM for the products that make outputs, DK the
-// width of q and k rounded up, WAVES of 16 columns of v each.  OUT: with outputs; else the pieces' states alone.  DOTS: with the sums of the
-// outputs times e.
+// width of q and k rounded up, WAVES of 16 columns of v each.  OUT: with outputs; else the
+// pieces' states alone.  DOTS: with the sums of the outputs times e.  What a token gives
+// its own output, whatever the decays are, is not in these: dq's and dk's sums differ by what
+// other tokens give, of which rapid decays leave little.  So it is added to the outputs last,
+// in fp32.
 //
 // A walk of 4 x 2048 tokens and 16 heads of 128 x 128, bf16, in eight pieces takes 45 us for
 // 168 MB, 32 at the rate of a copy: the vector units are busy 45 % of the time (a third of
@@ -259,6 +274,7 @@ struct Kernel {
         Tile<TP, OUT ? CH : 1, CH, 8> p;  // the scores
         float2 c[CH];            // the running sums in two parts, see high_part
         float in[CH], left[CH];  // e^c outer; e^(c[last] - c) inner
+        float own[DOTS ? CH : 1];  // the scores of tokens with themselves
         float whole;
 
         // A wave's part of a token's dot product, in the padding of k's row.
@@ -287,6 +303,10 @@ struct Kernel {
             const float2 cj = s.c[j + e];
             const float d = exp2_fast((ci.x - cj.x) + (ci.y - cj.y)) * factor;
             v[e] = j + e <= i ? acc[e] * d : 0.0f;
+            if (DOTS && j + e == i) {
+                s.own[i] = v[e];
+                v[e] = 0.0f;
+            }
         }
         unsigned u[TP][2];
         split<TP, 4>(v, u);
@@ -310,7 +330,7 @@ struct Kernel {
 #pragma unroll
         for (int row = 0; row < 2; ++row) {
             mma<LIM>(o[row], clean, s.p.along(16 * row + n, 8 * g));
-            for (int j = 0; j <= 16 * row + n; ++j) {
+            for (int j = 0; j < 16 * row + n + !DOTS; ++j) {
                 float p = 0.0f;
 #pragma unroll
                 for (int t = TP - 1; t >= 0; --t) p += (float)s.p.v[t][16 * row + n][j];
@@ -497,6 +517,11 @@ struct Kernel {
 #pragma unroll
                             for (int y = 0; y < 4; ++y)
                                 if (y < count) dot = __builtin_fmaf(o[row][y], to_f32(e.v[y]), dot);
+                            const float own = s.own[16 * row + n];
+                            const f4 x = s.v.four(16 * row + n, wave * 16 + 4 * g);
+#pragma unroll
+                            for (int y = 0; y < 4; ++y)
+                                o[row][y] = __builtin_fmaf(own, x[y], o[row][y]);
                         }
                         if (w.wide) {
                             Pack<float, 4> r;

@@ -21,9 +21,54 @@ pytestmark = pytest.mark.gpu
 DEV = "cuda"
 
 
+def pairs(a, dy, b, h, absolute=False):
+    """W of row b's head h, on the GPU in 64 bits."""
+    per = a["v"].shape[2] // a["q"].shape[2]
+    f = torch.abs if absolute else (lambda t: t)
+    q, k = (f(a[x][b, :, h // per].to(DEV).double()) for x in ("q", "k"))
+    v, d = f(a["v"][b, :, h].to(DEV).double()), f(dy[b, :, h].to(DEV).double())
+    g = a["log_decay"]
+    c = (g[b, :, h] if g.dim() > 1 else g[h].expand(len(q))).to(DEV).double().cumsum(0)
+    over = (c[:, None] - c[None]).masked_fill(
+        torch.ones(len(q), len(q), dtype=torch.bool, device=DEV).triu(1), -float("inf"))
+    return torch.exp(over) * (q @ k.t().contiguous()) * (d @ v.t().contiguous()) / q.shape[1] ** 0.5
+
+
+def crossing(w):
+    """For each t the sum of w[i,j] over j < t <= i."""
+    before = torch.cat((torch.zeros_like(w[:, :1]), w.cumsum(1)[:, :-1]), 1)  # over j < t
+    return before.flip(0).cumsum(0).flip(0).diagonal()
+
+
 def gradient(a, dy, **more):
     announce("linear_attention_backward", tuple(a["q"].shape), tuple(a["v"].shape), a["q"].dtype)
     return ops.linear_attention_backward(dy.to(DEV), **dev(a), **more)[3]
+
+
+@pytest.mark.parametrize("kind", [F32, F16, BF16])
+@pytest.mark.parametrize("heads", [2, 600])
+def test_decays_that_leave_little(kind, heads):
+    """Decays between e^-8 and e^-16 over 2100 tokens; rows in pieces and whole (600 heads,
+    of which the first and last are looked at)."""
+    a, dy = inputs(1, 2100, heads, heads, 64, 64, kind=kind)
+    a["log_decay"] = -8.0 - 8.0 * torch.rand(*a["log_decay"].shape,
+                                             generator=torch.Generator().manual_seed(7))
+    got = gradient(a, dy)
+    for h in (0, heads - 1):
+        want = crossing(pairs(a, dy, 0, h))
+        assert (got[0, :, h] - want).norm() <= 1e-4 * want.norm(), h
+
+
+@pytest.mark.parametrize("kind", [F32, BF16])
+def test_one_decay_for_all_tokens(kind):
+    """Heads' decays of e^-8 and e^-16: the sums of the tokens' gradients."""
+    a, dy = inputs(2, 700, 2, 1, 64, 64, kind=kind, fixed=True)
+    a["log_decay"] = torch.tensor([-8.0, -16.0])
+    got = gradient(a, dy)
+    for h in range(2):
+        tokens = torch.stack([crossing(pairs(a, dy, b, h)) for b in range(2)])
+        # a sum of 1400 of them: the tokens' errors as they are, at worst all of one sign
+        assert (got[h] - tokens.sum()).abs() <= 1e-4 * tokens.norm() * 1400 ** 0.5
 
 
 @pytest.mark.parametrize("kind", [F32, F16, BF16])
