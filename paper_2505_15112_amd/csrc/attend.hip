@@ -62,68 +62,77 @@ __device__ double block_sum(double v, Run* s) {
     return block_scan(run, s).sum;
 }
 
-// The decays' gradients: dg[t] = sum over s >= t of (q.dq - k.dk)[s], and the part
-// of the last state, <dS, S>; and dS_0 = e^g[0] G[0], in place (a row without tokens
-// keeps dS).  A token whose decay clears the state has a gradient of 0, and those before
-// it have no part in the sums behind it, which start anew there.  A workgroup to a row and head; eight
-// tokens to a thread (64 rows of 2048 tokens: 11 us; with one token to a thread 20).
+// The decays' gradients: dg[t] = <G[t], e^g[t] S[t-1]> at the tokens whose states are there
+// (kMark), and <dS, S> behind a row's last token; before them dg[t] = dg[t+1] + (q.dq -
+// k.dk)[t].  And dS_0 = e^g[0] G[0], in place (a row without tokens keeps dS).  A token
+// whose decay clears the state has a gradient of 0, and those before it have no part in the
+// sums behind it, which start anew there.  A workgroup to kMark tokens of a row and head.
 struct Gates {
     const float* dq_dots;
     const float* dk_dots;
-    int blocks;               // of dots
+    int blocks;            // of dots
+    const float* s_marks;  // S, and G
+    const float* g_marks;
     const float* dstate_out;  // and the last state, where it is given
     const float* last;
-    int64_t state;  // elements of a state
-    float* dstate;  // nullable
+    int64_t state, mark;  // elements of a state, and of one of the marks
+    float* dstate;        // nullable
     float* out;
 };
-__global__ void __launch_bounds__(kGateThreads) k_gates(Walk w, Gates a) {
-    constexpr int PER = 8;
-    __shared__ Run s[kGateWaves];
-    const int h = blockIdx.x % w.heads, b = blockIdx.x / w.heads, tid = threadIdx.x;
-    const int len = walk_len(w, b);
-    const int64_t all = (int64_t)w.batch * w.steps * w.heads, own = blockIdx.x * a.state;
-    const float* g = w.g + b * w.g_batch + h;
-    Run carry{};
-    if (a.dstate_out) {
-        double v = 0.0;
+__device__ double inner_product(const float* a, const float* b, int64_t n, Run* s) {
+    double v = 0.0;
 #pragma unroll 8
-        for (int64_t i = tid; i < a.state; i += kGateThreads)
-            v += (double)a.dstate_out[own + i] * a.last[own + i];
-        carry.sum = block_sum(v, s);
-    }
-    for (int end = w.steps; end > 0; end -= kGateThreads * PER) {
+    for (int64_t i = threadIdx.x; i < n; i += kGateThreads) v += (double)a[i] * b[i];
+    return block_sum(v, s);
+}
+__global__ void __launch_bounds__(kGateThreads) k_gates(Walk w, Gates a) {
+    constexpr int PER = kMark / kGateThreads;
+    __shared__ Run s[kGateWaves];
+    const int tid = threadIdx.x, marks = walk_marks(w.steps);
+    const int64_t tokens = (int64_t)w.batch * w.steps * w.heads;
+    const int64_t count = (int64_t)w.batch * w.heads * (marks + 1);
+    for (int64_t at = blockIdx.x; at < count; at += gridDim.x) {
+        const int part = (int)(at % (marks + 1));
+        const int64_t bh = at / (marks + 1);
+        const int h = (int)(bh % w.heads), b = (int)(bh / w.heads);
+        const int len = walk_len(w, b), end = part * kMark + kMark;
+        const float* g = w.g + b * w.g_batch + h;
+        Run after{};
+        if (end < len) {
+            const float decay = g[end * w.g_step];
+            const int64_t mark = (bh * marks + part) * a.mark;
+            const double all = inner_product(a.g_marks + mark, a.s_marks + mark, a.mark, s);
+            if (!clears(decay)) after.sum = all * exp2_fast(decay * kLog2e);
+        } else if (a.dstate_out && end - kMark < len) {
+            after.sum = inner_product(a.dstate_out + bh * a.state, a.last + bh * a.state, a.state, s);
+        }
         const int t0 = end - 1 - tid * PER;  // thread 0 has the last tokens
-        const int64_t at = ((int64_t)b * w.steps + t0) * w.heads + h;
+        const int64_t to = ((int64_t)b * w.steps + t0) * w.heads + h;
         Run v[PER], sum{};
 #pragma unroll
         for (int i = 0; i < PER; ++i) {
             v[i] = {};
-            if (t0 - i < 0 || t0 - i >= len) continue;
-            v[i].anew = clears(g[(t0 - i) * w.g_step]);
-            if (!v[i].anew)
-                for (int k = 0; k < a.blocks; ++k)
-                    v[i].sum += (double)a.dq_dots[k * all + at - (int64_t)i * w.heads] -
-                                a.dk_dots[k * all + at - (int64_t)i * w.heads];
-        }
-#pragma unroll
-        for (int i = 0; i < PER; ++i) {
+            if (t0 - i < len) {
+                v[i].anew = clears(g[(t0 - i) * w.g_step]);
+                if (!v[i].anew)
+                    for (int k = 0; k < a.blocks; ++k)
+                        v[i].sum += (double)a.dq_dots[k * tokens + to - (int64_t)i * w.heads] -
+                                    a.dk_dots[k * tokens + to - (int64_t)i * w.heads];
+            }
             v[i] = sum = then(sum, v[i]);
         }
-        const Run more = block_scan(sum, s);
-        const Run before = then(carry, sum);
+        block_scan(sum, s);
+        const Run before = then(after, sum);
 #pragma unroll
-        for (int i = 0; i < PER; ++i) {
-            const int t = t0 - i;
-            if (t < 0) break;
-            a.out[at - (int64_t)i * w.heads] = t < len ? (float)then(before, v[i]).sum : 0.0f;
-        }
-        carry = then(carry, more);
-    }
-    if (a.dstate && len > 0) {
-        const float decay = exp2_fast(g[0] * kLog2e);
+        for (int i = 0; i < PER; ++i)
+            if (t0 - i < w.steps)
+                a.out[to - (int64_t)i * w.heads] =
+                    t0 - i < len ? (float)then(before, v[i]).sum : 0.0f;
+        if (a.dstate && part == 0 && len > 0) {
+            const float decay = exp2_fast(g[0] * kLog2e);
 #pragma unroll 8
-        for (int64_t i = tid; i < a.state; i += kGateThreads) a.dstate[own + i] *= decay;
+            for (int64_t i = tid; i < a.state; i += kGateThreads) a.dstate[bh * a.state + i] *= decay;
+        }
     }
 }
 
@@ -275,7 +284,6 @@ Walk base(const libscan_attend& p) {
     w.g_batch = p.fixed ? 0 : p.decay_batch;
     w.g_step = p.fixed ? 0 : p.decay_step;
     w.lengths = p.lengths;
-    w.pieces = 1, w.piece = w.steps;
     w.inner = w.outer = 1.0f;
     return w;
 }
@@ -318,7 +326,7 @@ Pieces pieces(const libscan_attend& p, int together) {
                             together * p.batch * p.heads * count * p.dk * p.dv * 8 / 4.6e6 / 5 + 1;
         if (cost < best) best = cost, each = size;
     }
-    if (each >= chunks) return {1, (int)p.steps};
+    if (each >= chunks) return {1, (int)(chunks * chunk)};
     return {(int)((chunks + each - 1) / each), (int)(each * chunk)};
 }
 
@@ -349,15 +357,19 @@ struct FrontPlan {
 struct BackPlan {
     Room room;
     Cut cut, back;  // of S, and of its gradient
-    int64_t dq_dots, dk_dots, gates, last, dq, dk;
+    int64_t dq_dots, dk_dots, mark, s_marks, g_marks, gates, last, dq, dk;
     BackPlan(const libscan_attend& p) : cut(p, 2, room), back(p, 2, room) {
         const int64_t tokens = p.batch * p.steps * p.heads;
         const int64_t blocks = walk_blocks((int)p.dv, (int)p.dk);
         const bool shared = p.groups < p.heads;
         dq_dots = room.floats(tokens * blocks);
         dk_dots = room.floats(tokens * blocks);
+        const int64_t state = p.batch * p.heads * p.dk * p.dv;
+        mark = p.dk * walk_width((int)p.dv);
+        s_marks = room.floats(p.batch * p.heads * walk_marks((int)p.steps) * mark);
+        g_marks = room.floats(p.batch * p.heads * walk_marks((int)p.steps) * mark);
         gates = room.floats(p.fixed ? tokens : 0);
-        last = room.floats(p.batch * p.heads * p.dk * p.dv);
+        last = room.floats(state);
         dq = room.floats(shared ? tokens * p.dk : 0);
         dk = room.floats(shared ? tokens * p.dk : 0);
     }
@@ -455,28 +467,31 @@ hipError_t launch_attend_back(const libscan_attend& p, const void* dy, int64_t d
     wq.out = shared ? floats(plan.dq) : dq;
     wq.e = side_q(p);
     wq.dots = floats(plan.dq_dots);
+    wq.marks = floats(plan.s_marks);
     wk.q = side_v(p), wk.k = side_dy, wk.v = side_q(p);
     wk.first = {g.first.p, 1, p.dv};
     wk.last = {};
     wk.out = shared ? floats(plan.dk) : dk;
     wk.e = side_k(p);
     wk.dots = floats(plan.dk_dots);
+    wk.marks = floats(plan.g_marks);
     wq.wide = wk.wide = shared;
     if ((e = run(p.type, two, false, stream)) != hipSuccess) return e;
 
-    const uint32_t rows = (uint32_t)(p.batch * p.heads);
-    if (rows) {
-        const Gates a{floats(plan.dq_dots), floats(plan.dk_dots), dots, dstate_out, last,
-                      p.dk * p.dv, p.steps ? dstate : nullptr,
+    const int64_t parts = p.steps ? p.batch * p.heads * (walk_marks((int)p.steps) + 1) : 0;
+    const int64_t most = 1 << 20;  // workgroups; the rest in further turns
+    if (parts) {
+        const Gates a{floats(plan.dq_dots), floats(plan.dk_dots), dots, floats(plan.s_marks),
+                      floats(plan.g_marks), dstate_out, last, p.dk * p.dv, plan.mark, dstate,
                       p.fixed ? floats(plan.gates) : dlog_decay};
-        k_gates<<<rows, kGateThreads, 0, stream>>>(g, a);
+        k_gates<<<(uint32_t)(parts < most ? parts : most), kGateThreads, 0, stream>>>(g, a);
     }
     if (p.fixed && p.heads)
         k_gate_sum<<<(uint32_t)p.heads, kGateThreads, 0, stream>>>(
             floats(plan.gates), dlog_decay, p.batch * p.steps, (int)p.heads);
     const int64_t count = p.batch * p.steps * p.groups * p.dk;
     if (shared && count) {
-        const int64_t blocks = (count + 255) / 256, most = 1 << 20;
+        const int64_t blocks = (count + 255) / 256;
         const dim3 grid((uint32_t)(blocks < most ? blocks : most), 2);
         const auto join = [&](auto zero) {
             using T = decltype(zero);

@@ -34,6 +34,17 @@ struct WholePiece {
     int exponent;
 };
 
+// Tokens of a chunk: as many as one matrix instruction sums over.  64 make the states'
+// part of the work half as large, but leave room for one workgroup on a CU, not two (4 x
+// 2048 x 16 x 128 x 128, bf16: 50 us a walk against 45).
+constexpr int kChunk = 32;
+
+// A walk with dots leaves its states at the tokens whose numbers are multiples of kMark, S
+// before and G at each, for the decays' gradients: their sums then run over kMark tokens.
+// 512: 128 KB for S and G of 128 x 128, beside 900 KB of a head's operands and gradients.
+constexpr int kMark = 512;
+__host__ __device__ constexpr int walk_marks(int steps) { return steps > 0 ? (steps - 1) / kMark : 0; }
+
 struct Walk {
     int batch, steps, heads, dk, dv;
     bool reverse;
@@ -42,8 +53,8 @@ struct Walk {
     int64_t g_batch, g_step;
     float inner, outer;  // factors of k v^T, and of the output
     const int32_t* lengths;
-    // Every row's steps are cut into `pieces` of `piece` places, a workgroup to each
-    // (and to a block of columns of v).
+    // Every row's places are cut into `pieces` of `piece` (a multiple of kChunk), a workgroup
+    // to each (and to a block of columns of v).
     int pieces, piece;
     // The states that the rows (pieces == 1: one for each row and head) or their pieces
     // (one for each row, head and piece) begin with, nullable; and the last ones: the
@@ -58,6 +69,7 @@ struct Walk {
     bool wide;
     WalkSide e;
     float* dots;
+    float* marks;  // with dots: walk_marks(steps) of each row and head, dv x walk_width(dk) each
 };
 
 // A logarithm past -1024 to base 2 is one of 0: what decays by it is gone.
@@ -69,18 +81,22 @@ __device__ __forceinline__ int walk_len(const Walk& w, int b) {
     return n < 0 ? 0 : n < w.steps ? n : w.steps;
 }
 
-// The token at a place of the walk, and that place's decay.  Places at and behind
-// `len` are the tokens there, whose outputs are 0.
+// In reverse a row's first places may have no tokens, so that chunks lie at the same
+// tokens both ways.
+__device__ __forceinline__ int walk_skip(const Walk& w, int len) {
+    return w.reverse ? (kChunk - len % kChunk) % kChunk : 0;
+}
+// The token at a place of the walk, and that place's decay.
 __device__ __forceinline__ int walk_token(const Walk& w, int place, int len) {
-    return w.reverse && place < len ? len - 1 - place : place;
+    return w.reverse ? len + walk_skip(w, len) - 1 - place : place;
 }
 __device__ __forceinline__ float walk_decay(const Walk& w, int b, int h, int place, int len) {
-    if (place >= len || (w.reverse && place == 0)) return 0.0f;
-    const int t = w.reverse ? len - place : place;
-    return w.g[b * w.g_batch + t * w.g_step + h];
+    const int t = walk_token(w, place, len) + w.reverse;
+    return t >= len ? 0.0f : w.g[b * w.g_batch + t * w.g_step + h];
 }
 
-// Columns of v that a workgroup has.
+// The width that q and k have in a workgroup, filled up by zeros, and the columns of v.
+inline int walk_width(int dk) { return dk > 128 ? 256 : dk > 64 ? 128 : 64; }
 inline int walk_columns(int dk, int dv) { return dv > 64 ? 128 : 64; }
 inline int walk_blocks(int dk, int dv) {
     const int columns = walk_columns(dk, dv);

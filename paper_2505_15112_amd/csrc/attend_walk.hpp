@@ -153,10 +153,10 @@ struct Fetch {
         width = elements;
         at = p + threadIdx.x / PER_ROW * step + threadIdx.x % PER_ROW * V;
     }
-    // The next chunk, of which the first `rows` places have tokens; 0 elsewhere.
-    __device__ __forceinline__ void load(int rows) {
+    // The next chunk, whose places from `skip` to `rows` have tokens; 0 elsewhere.
+    __device__ __forceinline__ void load(int skip, int rows) {
         const bool mine = ALL % THREADS == 0 || threadIdx.x < ALL;
-        if (rows >= ROWS && width >= WIDTH) {
+        if (skip <= 0 && rows >= ROWS && width >= WIDTH) {
 #pragma unroll
             for (int i = 0; i < N; ++i)
                 if (mine) r[i] = *reinterpret_cast<const Vec*>(at + i * BETWEEN * forward);
@@ -165,7 +165,8 @@ struct Fetch {
 #pragma unroll
             for (int i = 0; i < N; ++i) {
                 Vec v{};
-                if (mine && row + i * BETWEEN < rows && col < width) {
+                const int place = row + i * BETWEEN;
+                if (mine && place >= skip && place < rows && col < width) {
                     const T* from = at + i * BETWEEN * forward;
                     if (col + V <= width) {
                         v = *reinterpret_cast<const Vec*>(from);
@@ -244,11 +245,6 @@ __device__ __forceinline__ double running_sum(float g) {
 __device__ __forceinline__ float high_part(double c) {
     return (float)(__builtin_rint(c * 256.0) * (1.0 / 256.0));
 }
-
-// Tokens of a chunk: as many as one matrix instruction sums over.  64 make the states'
-// part of the work half as large, but leave room for one workgroup on a CU, not two (4 x
-// 2048 x 16 x 128 x 128, bf16: 50 us a walk against 45).
-constexpr int kChunk = 32;
 
 // TP terms of scores and states, LIM for the products that make outputs, DK the
 // width of q and k rounded up, WAVES of 16 columns of v each.  OUT: with outputs; else the
@@ -388,15 +384,14 @@ struct Kernel {
         const int h = at % w.heads;
         at /= w.heads;
         const int piece = at % w.pieces, b = at / w.pieces, bh = b * w.heads + h;
-        const int len = walk_len(w, b), c0 = block * COLS;
-        const int start = piece * w.piece;
-        const int end = start + w.piece < w.steps ? start + w.piece : w.steps;
-        const int live = len < end ? len : end;  // places of this piece that have tokens
+        const int len = walk_len(w, b), skip = walk_skip(w, len), c0 = block * COLS;
+        const int start = piece * w.piece, end = start + w.piece;
+        const int live = len + skip < end ? len + skip : end;  // where the piece's tokens end
         const int64_t number = (int64_t)bh * w.pieces + piece;
         const int column = c0 + wave * 16 + n;  // of the state
 
         // The first place's token, and the way from token to token.
-        const int way = w.reverse ? -1 : 1, first = w.reverse ? len - 1 - start : start;
+        const int way = w.reverse ? -1 : 1, first = walk_token(w, start, len);
         const auto side = [&](const WalkSide& x, int t) {
             return (const T*)x.p + b * x.batch + (h / x.share) * x.head + t * x.step;
         };
@@ -404,9 +399,9 @@ struct Kernel {
         Fetch<T, CH, COLS, THREADS> fv;
         float decay = 0.0f;
         const auto fetch = [&](int base) {
-            fk.load(live - base);
-            fv.load(live - base);
-            if constexpr (OUT) fq.load(live - base);
+            fk.load(skip - base, live - base);
+            fv.load(skip - base, live - base);
+            if constexpr (OUT) fq.load(skip - base, live - base);
             if (wave == 0)
                 decay = lane < CH && base + lane < live ? walk_decay(w, b, h, base + lane, len) : 0.0f;
         };
@@ -423,9 +418,9 @@ struct Kernel {
             load_state(state, w.first.p + number * w.dk * w.dv, w, w.first, column, g);
 
         if constexpr (OUT) {
-            // places without a token, and the scores' tiles above the diagonal
+            // what lies behind the row's end, and the scores' tiles above the diagonal
             const int cols = w.dv - c0 < COLS ? w.dv - c0 : COLS;
-            for (int i = (live > start ? live : start) + wave; i < end; i += WAVES) {
+            for (int i = (len > start ? len : start) + wave; i < end && i < w.steps; i += WAVES) {
                 const int64_t o = (((int64_t)b * w.steps + i) * w.heads + h) * w.dv + c0;
                 for (int c = lane; c < cols; c += 64) {
                     if (w.wide)
@@ -439,7 +434,7 @@ struct Kernel {
         }
 
         const auto put_dots = [&](int base) {
-            if (tid >= CH || base + tid >= live) return;
+            if (tid >= CH || base + tid < skip || base + tid >= live) return;
             float sum = 0.0f;
 #pragma unroll
             for (int i = 0; i < WAVES; ++i) sum += s.dot(i, tid);
@@ -456,6 +451,19 @@ struct Kernel {
 
         double total = 0.0;
         for (int base = start; base < live; base += CH) {
+            if constexpr (DOTS) {
+                // tokens in front of the chunk, or up to its end in reverse
+                const int before = w.reverse ? len + skip - base : base;
+                if (before % kMark == 0 && before > 0 && before < len && column < w.dv) {
+                    const int64_t mark = (int64_t)bh * walk_marks(w.steps) + before / kMark - 1;
+                    float* p = w.marks + (mark * w.dv + column) * DK + 8 * g;
+#pragma unroll
+                    for (int x = 0; x < PAIRS; ++x)
+#pragma unroll
+                        for (int y = 0; y < 2; ++y)
+                            *reinterpret_cast<f4*>(p + 32 * x + 4 * y) = state[x][y];
+                }
+            }
             __syncthreads();  // the last chunk's tiles are read
             if (DOTS && base > start) put_dots(base - CH);
             fk.store(s.k);
@@ -510,7 +518,8 @@ struct Kernel {
                 for (int row = 0; row < 2; ++row) {
                     float dot = 0.0f;
                     const int64_t here = to + 16 * row * row_step;
-                    if (base + 16 * row + n < live && count > 0) {
+                    const int place = base + 16 * row + n;
+                    if (place >= skip && place < live && count > 0) {
                         if constexpr (DOTS) {
                             Pack<T, 4> e;
                             e.load(pe + 16 * row * way * w.e.step, count);
@@ -616,8 +625,9 @@ hipError_t launch_walk(const Walks& walks, bool states, hipStream_t stream) {
         return wide ? walk::launch<T, dk.value, 8>(walks, states, stream)
                     : walk::launch<T, dk.value, 4>(walks, states, stream);
     };
-    if (w.dk > 128) return by_width(std::integral_constant<int, 256>());
-    if (w.dk > 64) return by_width(std::integral_constant<int, 128>());
+    const int width = walk_width(w.dk);
+    if (width == 256) return by_width(std::integral_constant<int, 256>());
+    if (width == 128) return by_width(std::integral_constant<int, 128>());
     return by_width(std::integral_constant<int, 64>());
 }
 

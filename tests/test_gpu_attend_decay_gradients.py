@@ -15,7 +15,7 @@ import torch
 from attend_ref import BF16, F16, F32
 from gpu_util import announce
 from paper_2505_15112_amd import ops
-from test_gpu_attend import dev, inputs
+from test_gpu_attend import check_backward, check_forward, dev, inputs
 
 pytestmark = pytest.mark.gpu
 DEV = "cuda"
@@ -71,6 +71,20 @@ def test_one_decay_for_all_tokens(kind):
         assert (got[h] - tokens.sum()).abs() <= 1e-4 * tokens.norm() * 1400 ** 0.5
 
 
+@pytest.mark.parametrize("heads", [2, 600])
+def test_strong_decays_before_weak_ones(heads):
+    """Decays of e^-12, and behind them of e^-0.01: the first tokens' gradients hold no
+    roundings of the later ones'.  The last 512 tokens of strong decays may."""
+    a, dy = inputs(1, 2100, heads, heads, 64, 64)
+    a["log_decay"][:, :1300] = -12.0
+    a["log_decay"][:, 1300:] = -0.01
+    got = gradient(a, dy)
+    for h in (0, heads - 1):
+        want = crossing(pairs(a, dy, 0, h))
+        for part in (slice(0, 788), slice(1300, None)):
+            assert (got[0, part, h] - want[part]).norm() <= 1e-4 * want[part].norm(), (h, part)
+
+
 @pytest.mark.parametrize("kind", [F32, F16, BF16])
 @pytest.mark.parametrize("steps", [90, 1300])
 @pytest.mark.parametrize("clear", [-float("inf"), torch.finfo(torch.float32).min])
@@ -93,3 +107,24 @@ def test_rows_of_two_sequences(kind, steps, clear):
             err = (got[0, :cut, h] - want[0, :, h]).norm()
             assert err <= 2e-4 * want[0, :, h].norm(), h
         assert not got[0, cut].any()
+
+
+@pytest.mark.parametrize("steps,dims", [(512, (24, 40)), (513, (24, 40)), (1025, (130, 70)),
+                                        (1600, (24, 40))])
+def test_rows_around_the_boundaries_of_the_sums(steps, dims):
+    """Ragged rows, first states and gradients of last ones, lengths at and around
+    multiples of 512, against the definition."""
+    a, dy = inputs(3, steps, 2, 1, *dims, kind=BF16, state=True, lengths=[steps, 512, 33],
+                   rate=0.05)
+    so = torch.randn(*a["state"].shape, generator=torch.Generator().manual_seed(3))
+    check_backward(a, dy, so)
+
+
+@pytest.mark.parametrize("kind", [F16, BF16])
+@pytest.mark.parametrize("dims", [(64, 64), (128, 100)])
+def test_long_rows_against_the_definition(kind, dims):
+    """Rows of 2049 tokens, cut into pieces, forward and gradients."""
+    a, dy = inputs(1, 2049, 2, 1, *dims, kind=kind, state=True, rate=0.02)
+    check_forward(a)
+    check_backward(a, dy, torch.randn(*a["state"].shape,
+                                      generator=torch.Generator().manual_seed(3)))
