@@ -80,9 +80,16 @@ struct Gates {
     float* out;
 };
 __device__ double inner_product(const float* a, const float* b, int64_t n, Run* s) {
+    typedef f4 Vec __attribute__((aligned(4)));
     double v = 0.0;
 #pragma unroll 8
-    for (int64_t i = threadIdx.x; i < n; i += kGateThreads) v += (double)a[i] * b[i];
+    for (int64_t i = threadIdx.x; i < n / 4; i += kGateThreads) {
+        const f4 x = ((const Vec*)a)[i], y = ((const Vec*)b)[i];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v += (double)x[e] * y[e];
+    }
+    const int64_t i = n / 4 * 4 + threadIdx.x;
+    if (i < n) v += (double)a[i] * b[i];
     return block_sum(v, s);
 }
 __global__ void __launch_bounds__(kGateThreads) k_gates(Walk w, Gates a) {
@@ -129,9 +136,13 @@ __global__ void __launch_bounds__(kGateThreads) k_gates(Walk w, Gates a) {
                 a.out[to - (int64_t)i * w.heads] =
                     t0 - i < len ? (float)then(before, v[i]).sum : 0.0f;
         if (a.dstate && part == 0 && len > 0) {
+            typedef f4 Vec __attribute__((aligned(4)));
             const float decay = exp2_fast(g[0] * kLog2e);
+            float* state = a.dstate + bh * a.state;
 #pragma unroll 8
-            for (int64_t i = tid; i < a.state; i += kGateThreads) a.dstate[bh * a.state + i] *= decay;
+            for (int64_t i = tid; i < a.state / 4; i += kGateThreads) ((Vec*)state)[i] *= decay;
+            const int64_t i = a.state / 4 * 4 + tid;
+            if (i < a.state) state[i] *= decay;
         }
     }
 }
@@ -150,7 +161,7 @@ __global__ void __launch_bounds__(kGateThreads) k_gate_sum(const float* in, floa
 // The states before every piece from what each adds, in place: a workgroup to 256
 // elements of a row and head; piece i of element x is states[i * each + x].  A piece's
 // product of decays, x 2^y (WholePiece), may be beyond fp32 where the state that it meets is 0
-// or small: the state is scaled by the exponent, which leaves 0 what it is.
+// or small: the state is scaled by the exponent first, which leaves 0 what it is.
 struct Carry {
     float* states;
     const WholePiece* whole;
@@ -160,7 +171,7 @@ struct Carry {
 struct Carries {
     Carry c[2];
 };
-// AHEAD loads on their way; the chain itself is a multiply-add each.  16 are for the few rows
+// AHEAD loads on their way; the chain itself is a scaling and a multiply-add each.  16 are for the few rows
 // that are cut into many pieces (52 pieces of 8 rows' 64 x 128: 15 to 7 us); where there
 // are enough threads without them they cost (64 rows' 8 pieces of 128 x 128: 14 to 18).
 template <int AHEAD>
@@ -182,7 +193,8 @@ __global__ void __launch_bounds__(256) k_carry(Carries all, int pieces, int64_t 
         for (int i = 0; i < AHEAD; ++i) {
             if (first + i >= pieces) break;
             at[(first + i) * each] = run;
-            run = __builtin_amdgcn_ldexpf(decay[i].factor * run, decay[i].exponent) + more[i];
+            run = __builtin_fmaf(decay[i].factor,
+                                 __builtin_amdgcn_ldexpf(run, decay[i].exponent), more[i]);
         }
     }
     if (c.last) c.last[bh * each + x] = run;

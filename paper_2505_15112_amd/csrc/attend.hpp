@@ -27,7 +27,7 @@ struct WalkState {
     int64_t row, col;
 };
 
-// The product of a piece's decays, factor * 2^exponent with a factor of 0.5 to 1: over
+// The product of a piece's decays, factor * 2^exponent with a factor of 1 to 2: over
 // hundreds of tokens it may be beyond fp32 both ways.
 struct WholePiece {
     float factor;

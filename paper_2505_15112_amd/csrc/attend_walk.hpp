@@ -577,9 +577,9 @@ struct Kernel {
             store_state(state, w.last.p + number * w.dk * w.dv, w, w.last, column, g);
         if (!OUT && block == 0 && tid == 0) {
             // no product of 2^8192 leaves a state in fp32; a NaN goes into the factor
-            const double up = __builtin_ceil(total), most = 8192.0;
-            w.whole[number] = {exp2_fast((float)(total - up)),
-                               (int)__builtin_fmax(__builtin_fmin(up, most), -most)};
+            const double down = __builtin_floor(total), most = 8192.0;
+            w.whole[number] = {exp2_fast((float)(total - down)),
+                               (int)__builtin_fmax(__builtin_fmin(down, most), -most)};
         }
     }
 };
