@@ -63,8 +63,7 @@ struct Walk {
     WholePiece* whole;  // in such a run, for each row, head and piece: the product of its decays
     // Output: batch x steps x heads x dv, dense; fp32 where `wide`.  With `dots`
     // (batch x steps x heads for each block of columns), the sums of the output
-    // times e, before it is rounded and without the part that is the token's own; it
-    // is then formed to fp32's precision.
+    // times e, before it is rounded and without the part that is the token's own.
     void* out;
     bool wide;
     WalkSide e;

@@ -12,8 +12,12 @@
 // of more bits is split into terms of 8 bits each, all but the last by truncation
 // (what is left is exact, and nothing overflows): fp16 inputs into two and fp32
 // inputs into three, which hold them exactly.  Term i of one operand meets term j of
-// the other where i + j < LIM.  bfloat16's exponents are fp32's, so neither scores nor
-// states overflow or lose their small values, as they would in fp16.
+// the other where i + j < 3.  bfloat16's exponents are fp32's, so neither scores nor
+// states overflow or lose their small values, as they would in fp16.  Scores and states are
+// three terms whatever the type of the outputs, whose last rounding is the only one to
+// fewer bits than fp32's.  (Two terms, 2^-17 off, take 96 to 99 % of the time, 85 % where one
+// chain of chunks is all, but leave bfloat16 outputs 1.3e-4 of their 2-norm off those of
+// 32-bit products, by last roundings that went the other way; three leave 4e-5.)
 #pragma once
 
 #include <type_traits>
@@ -78,10 +82,11 @@ struct Frag {
 
 // c += a b.  Lane l has row (a) or column (b) l % 16 at the eight places from 8 (l /
 // 16) of the 32 summed over, and of the result column l % 16, rows from 4 (l / 16).
-template <int LIM, int NA, int NB>
+constexpr int kTerms32 = 3;  // of an fp32 value
+template <int NA, int NB>
 __device__ __forceinline__ void mma(f4& c, const Frag<NA>& a, const Frag<NB>& b) {
 #pragma unroll
-    for (int s = LIM - 1; s >= 0; --s)  // small parts first
+    for (int s = kTerms32 - 1; s >= 0; --s)  // small parts first
 #pragma unroll
         for (int i = 0; i < NA; ++i)
 #pragma unroll
@@ -246,8 +251,7 @@ __device__ __forceinline__ float high_part(double c) {
     return (float)(__builtin_rint(c * 256.0) * (1.0 / 256.0));
 }
 
-// TP terms of scores and states, LIM for the products that make outputs, DK the
-// width of q and k rounded up, WAVES of 16 columns of v each.  OUT: with outputs; else the
+// DK: the width of q and k rounded up, WAVES of 16 columns of v each.  OUT: with outputs; else the
 // pieces' states alone.  DOTS: with the sums of the outputs times e.  What a token gives
 // its own output, whatever the decays are, is not in these: dq's and dk's sums differ by what
 // other tokens give, of which rapid decays leave little.  So it is added to the outputs last,
@@ -257,10 +261,10 @@ __device__ __forceinline__ float high_part(double c) {
 // 168 MB, 32 at the rate of a copy: the vector units are busy 45 % of the time (a third of
 // their work is splitting the state into terms and scaling it), LDS 35 %, the matrix units
 // 24 %, and waves wait for barriers and LDS half of theirs.
-template <class T, int TP, int LIM, int DK, int WAVES_, bool OUT, bool DOTS>
+template <class T, int DK, int WAVES_, bool OUT, bool DOTS>
 struct Kernel {
     static constexpr int WAVES = WAVES_, COLS = 16 * WAVES, THREADS = 64 * WAVES;
-    static constexpr int TERMS = kTerms<T>;
+    static constexpr int TERMS = kTerms<T>, TP = kTerms32;
     static constexpr bool WITH_DOTS = DOTS;
     static constexpr int CH = kChunk, PAIRS = DK / 32;
     struct Shared {
@@ -289,7 +293,7 @@ struct Kernel {
         f4 acc{};
 #pragma unroll
         for (int p = 0; p < PAIRS; ++p)
-            mma<LIM>(acc, s.k.along(16 * col + n, 32 * p + 8 * g),
+            mma(acc, s.k.along(16 * col + n, 32 * p + 8 * g),
                      s.q.along(16 * row + n, 32 * p + 8 * g));
         const int i = 16 * row + n, j = 16 * col + 4 * g;
         const float2 ci = s.c[i];
@@ -325,7 +329,7 @@ struct Kernel {
         }
 #pragma unroll
         for (int row = 0; row < 2; ++row) {
-            mma<LIM>(o[row], clean, s.p.along(16 * row + n, 8 * g));
+            mma(o[row], clean, s.p.along(16 * row + n, 8 * g));
             for (int j = 0; j < 16 * row + n + !DOTS; ++j) {
                 float p = 0.0f;
 #pragma unroll
@@ -444,8 +448,12 @@ struct Kernel {
 
         // The lane's outputs: 4 columns of token n of every tile of 16.
         const int c = c0 + wave * 16 + 4 * g, count = w.dv - c;
-        const int64_t row_step = (int64_t)way * w.heads * w.dv;
-        int64_t to = (((int64_t)b * w.steps + first) * w.heads + h) * w.dv + c + n * row_step;
+        const int row_step = way * w.heads * w.dv;  // at most 2^24
+        int64_t to = (((int64_t)b * w.steps + first) * w.heads + h) * w.dv + c0;
+        // the lane's place by itself is a register less; with dots, where scalar registers
+        // are short, added to the rest
+        int lane_to = c - c0 + n * row_step;
+        if constexpr (DOTS) to += lane_to, lane_to = 0;
         const T* pe = nullptr;
         if constexpr (DOTS) pe = side(w.e, first) + c + n * way * w.e.step;
 
@@ -497,7 +505,7 @@ struct Kernel {
                     f.from(r);
 #pragma unroll
                     for (int row = 0; row < 2; ++row)
-                        mma<LIM>(o[row], f, s.q.along(16 * row + n, 32 * p + 8 * g));
+                        mma(o[row], f, s.q.along(16 * row + n, 32 * p + 8 * g));
                 }
 #pragma unroll
                 for (int row = 0; row < 2; ++row) o[row] *= s.in[16 * row + n];
@@ -510,14 +518,14 @@ struct Kernel {
                 if (fine) {
 #pragma unroll
                     for (int row = 0; row < 2; ++row)
-                        mma<LIM>(o[row], v, s.p.along(16 * row + n, 8 * g));
+                        mma(o[row], v, s.p.along(16 * row + n, 8 * g));
                 } else {
                     careful(s, o, v, wave, lane);
                 }
 #pragma unroll
                 for (int row = 0; row < 2; ++row) {
                     float dot = 0.0f;
-                    const int64_t here = to + 16 * row * row_step;
+                    const int here = lane_to + 16 * row * row_step;
                     const int place = base + 16 * row + n;
                     if (place >= skip && place < live && count > 0) {
                         if constexpr (DOTS) {
@@ -536,12 +544,12 @@ struct Kernel {
                             Pack<float, 4> r;
 #pragma unroll
                             for (int y = 0; y < 4; ++y) r.v[y] = o[row][y];
-                            r.store((float*)w.out + here, count);
+                            r.store((float*)w.out + to + here, count);
                         } else {
                             Pack<T, 4> r;
 #pragma unroll
                             for (int y = 0; y < 4; ++y) r.v[y] = from_f32<T>(o[row][y]);
-                            r.store((T*)w.out + here, count);
+                            r.store((T*)w.out + to + here, count);
                         }
                     }
                     if constexpr (DOTS) {
@@ -558,7 +566,7 @@ struct Kernel {
             const float whole = s.whole;
 #pragma unroll
             for (int p = 0; p < PAIRS; ++p) state[p][0] *= whole, state[p][1] *= whole;
-            Frag<3> vw;
+            Frag<TP> vw;
             float r[8];
 #pragma unroll
             for (int e = 0; e < 8; ++e) r[e] = v.value(e) * s.left[8 * g + e];
@@ -567,7 +575,7 @@ struct Kernel {
             for (int p = 0; p < PAIRS; ++p)
 #pragma unroll
                 for (int y = 0; y < 2; ++y)
-                    mma<3>(state[p][y], s.k.down(0, 32 * p + 8 * (lane % 4) + 4 * y, lane), vw);
+                    mma(state[p][y], s.k.down(0, 32 * p + 8 * (lane % 4) + 4 * y, lane), vw);
         }
         if (DOTS && live > start) {
             __syncthreads();
@@ -601,17 +609,16 @@ __global__ void __launch_bounds__(K::THREADS, kPerSimd<K>) k_walk(Walks walks) {
 template <class T, int DK, int WAVES>
 hipError_t launch(const Walks& walks, bool states, hipStream_t stream) {
     const Walk& w = walks.w[0];
-    constexpr int COLS = 16 * WAVES, THREADS = 64 * WAVES, NARROW = kTerms<T> == 3 ? 3 : 2;
+    constexpr int COLS = 16 * WAVES, THREADS = 64 * WAVES;
     const int64_t blocks = (int64_t)w.batch * w.heads * w.pieces * ((w.dv + COLS - 1) / COLS);
     if (blocks == 0) return hipSuccess;
     const dim3 grid((uint32_t)blocks, walks.count);
     if (states)
-        k_walk<Kernel<T, 1, 3, DK, WAVES, false, false>><<<grid, THREADS, 0, stream>>>(walks);
+        k_walk<Kernel<T, DK, WAVES, false, false>><<<grid, THREADS, 0, stream>>>(walks);
     else if (!w.dots)
-        k_walk<Kernel<T, NARROW, NARROW, DK, WAVES, true, false>>
-            <<<grid, THREADS, 0, stream>>>(walks);
+        k_walk<Kernel<T, DK, WAVES, true, false>><<<grid, THREADS, 0, stream>>>(walks);
     else
-        k_walk<Kernel<T, 3, 3, DK, WAVES, true, true>><<<grid, THREADS, 0, stream>>>(walks);
+        k_walk<Kernel<T, DK, WAVES, true, true>><<<grid, THREADS, 0, stream>>>(walks);
     return hipGetLastError();
 }
 
