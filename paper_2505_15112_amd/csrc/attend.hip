@@ -320,7 +320,7 @@ struct Pieces {
 // `together`: walks of one launch.
 Pieces pieces(const libscan_attend& p, int together) {
     const int64_t chunk = 64, chunks = (p.steps + chunk - 1) / chunk;
-    const int64_t groups = together * p.batch * p.heads * walk_blocks((int)p.dk, (int)p.dv);
+    const int64_t groups = together * p.batch * p.heads * walk_blocks((int)p.dv);
     const auto time = [](int64_t count, double full, double half) {
         const int64_t left = count % 512;
         return count / 512 * full + (left > 256 ? full : left ? half : 0.0);
@@ -372,7 +372,7 @@ struct BackPlan {
     int64_t dq_dots, dk_dots, mark, s_marks, g_marks, gates, last, dq, dk;
     BackPlan(const libscan_attend& p) : cut(p, 2, room), back(p, 2, room) {
         const int64_t tokens = p.batch * p.steps * p.heads;
-        const int64_t blocks = walk_blocks((int)p.dv, (int)p.dk);
+        const int64_t blocks = walk_blocks((int)p.dk);
         const bool shared = p.groups < p.heads;
         dq_dots = room.floats(tokens * blocks);
         dk_dots = room.floats(tokens * blocks);
@@ -446,7 +446,7 @@ hipError_t launch_attend_back(const libscan_attend& p, const void* dy, int64_t d
     const auto floats = [&](int64_t at) { return (float*)(mem + at); };
     const bool shared = p.groups != p.heads;  // without heads, the groups' sums are over none
     const WalkSide side_dy = {dy, dy_batch, dy_step, dy_head, 1};
-    const int dots = walk_blocks((int)p.dv, (int)p.dk);
+    const int dots = walk_blocks((int)p.dk);
     float* last = dstate_out ? floats(plan.last) : nullptr;
     hipError_t e;
 

@@ -96,9 +96,9 @@ __device__ __forceinline__ float walk_decay(const Walk& w, int b, int h, int pla
 
 // The width that q and k have in a workgroup, filled up by zeros, and the columns of v.
 inline int walk_width(int dk) { return dk > 128 ? 256 : dk > 64 ? 128 : 64; }
-inline int walk_columns(int dk, int dv) { return dv > 64 ? 128 : 64; }
-inline int walk_blocks(int dk, int dv) {
-    const int columns = walk_columns(dk, dv);
+inline int walk_columns(int dv) { return dv > 64 ? 128 : 64; }
+inline int walk_blocks(int dv) {
+    const int columns = walk_columns(dv);
     return (dv + columns - 1) / columns;
 }
 

@@ -627,7 +627,7 @@ hipError_t launch(const Walks& walks, bool states, hipStream_t stream) {
 template <class T>
 hipError_t launch_walk(const Walks& walks, bool states, hipStream_t stream) {
     const Walk& w = walks.w[0];
-    const bool wide = walk_columns(w.dk, w.dv) == 128;
+    const bool wide = walk_columns(w.dv) == 128;
     const auto by_width = [&](auto dk) {
         return wide ? walk::launch<T, dk.value, 8>(walks, states, stream)
                     : walk::launch<T, dk.value, 4>(walks, states, stream);
