@@ -527,9 +527,10 @@ int selective_scan_step(const libscan_ssm* p, float* states, int64_t n_states,
  * q, k: batch x steps x groups x dk; v, y: batch x steps x heads x dv, with unit
  * stride over the last dimension.  log_decay: fp32, batch x steps x heads with
  * unit stride over heads, or (fixed != 0) heads, one for all tokens; 0 keeps the
- * state, -infinity clears it; values above 0 let it grow, and products of decays over
- * 32 tokens have to stay within fp32.  state (nullable: zeros): batch x heads x dk x dv,
- * dense fp32.  1 <= dk, dv <= 256, heads a multiple of groups.  An infinity or a NaN
+ * state, -infinity clears it (infinities and NaNs in it stay, as 0 times them is a
+ * NaN); values above 0 let it grow, and products of decays over 32 tokens have to
+ * stay within fp32.  state (nullable: zeros): batch x heads x dk x dv, dense fp32.
+ * 1 <= dk, dv <= 256, heads and groups up to 65536, heads a multiple of groups.  An infinity or a NaN
  * in an operand makes the outputs that it reaches infinite or NaN (which of the two is
  * not said), and no others: of v, one column of its head; of any, no earlier token. */
 typedef struct {
@@ -562,7 +563,10 @@ int linear_attention(const libscan_attend* p, void* y, float* state_out, void* s
  * log_decay's shape: 0 where the decay is -infinity, or below -709.79, which clears the
  * state likewise) and dstate (nullable: batch x heads x dk x dv), fp32.  Sums run in a
  * fixed order.  A token's dlog_decay is formed of q dq - k dk of the tokens from it on, up
- * to the next one that clears the state: an infinity or a NaN there reaches it. */
+ * to the next one that clears the state or whose number is a multiple of 512: an infinity or
+ * a NaN there reaches it, and so do the roundings of such sums (fp32's, of what pairs
+ * of different tokens give), which the gradient may be far smaller than where one decay is
+ * much stronger than those around it. */
 int linear_attention_backward(const libscan_attend* p, const void* dy, int64_t dy_batch,
                               int64_t dy_step, int64_t dy_head, const float* dstate_out, void* dq,
                               void* dk, void* dv, float* dlog_decay, float* dstate, void* scratch,

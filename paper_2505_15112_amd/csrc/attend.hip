@@ -66,7 +66,8 @@ __device__ double block_sum(double v, Run* s) {
 // (kMark), and <dS, S> behind a row's last token; before them dg[t] = dg[t+1] + (q.dq -
 // k.dk)[t].  And dS_0 = e^g[0] G[0], in place (a row without tokens keeps dS).  A token
 // whose decay clears the state has a gradient of 0, and those before it have no part in the
-// sums behind it, which start anew there.  A workgroup to kMark tokens of a row and head.
+// sums behind it, which start anew there.  A workgroup to kMark tokens of a row and head: 64
+// rows of 2048 tokens, 128 x 128, 11 us for 30 MB.
 struct Gates {
     const float* dq_dots;
     const float* dk_dots;
@@ -172,7 +173,7 @@ struct Carries {
     Carry c[2];
 };
 // AHEAD loads on their way; the chain itself is a scaling and a multiply-add each.  16 are for the few rows
-// that are cut into many pieces (52 pieces of 8 rows' 64 x 128: 15 to 7 us); where there
+// that are cut into many pieces (52 pieces of 8 rows' 64 x 128: 15 to 8 us); where there
 // are enough threads without them they cost (64 rows' 8 pieces of 128 x 128: 14 to 18).
 template <int AHEAD>
 __global__ void __launch_bounds__(256) k_carry(Carries all, int pieces, int64_t each) {
@@ -312,8 +313,9 @@ WalkSide side_v(const libscan_attend& p) { return {p.v, p.v_batch, p.v_step, p.v
 // longer carry, which reads and writes every piece's state.  The times that are weighed
 // up are those of 128 x 128 states in bf16, in units of 5 us: 512 workgroups (two to a CU) walk
 // n chunks of 64 tokens in 2 n + 1.5 and run for their states in 0.8 n + 1.4, 256 in 1.2 n
-// + 1.5 and 0.45 n + 1.3; the carry moves 4.6 TB/s; two launches take 1.  fp32's chunks
-// take more than twice as long, in six products for one or two.
+// + 1.5 and 0.45 n + 1.3; the carry moves 4.6 TB/s; two launches take 1.  (Measured with
+// scores and states in two terms; with three the walks take 3 to 15 % more.)  fp32's chunks
+// take more than twice as long, in six products for three.
 struct Pieces {
     int count, places;
 };

@@ -257,10 +257,10 @@ __device__ __forceinline__ float high_part(double c) {
 // other tokens give, of which rapid decays leave little.  So it is added to the outputs last,
 // in fp32.
 //
-// A walk of 4 x 2048 tokens and 16 heads of 128 x 128, bf16, in eight pieces takes 45 us for
-// 168 MB, 32 at the rate of a copy: the vector units are busy 45 % of the time (a third of
-// their work is splitting the state into terms and scaling it), LDS 35 %, the matrix units
-// 24 %, and waves wait for barriers and LDS half of theirs.
+// A walk of 4 x 2048 tokens and 16 heads of 128 x 128, bf16, in eight pieces takes 51 us for
+// 168 MB, 32 at the rate of a copy: the vector units are busy 51 % of the time (a third of
+// their work is splitting the state into terms and scaling it), LDS 34 %, the matrix units
+// 26 %, and waves wait for barriers and LDS half of theirs.
 template <class T, int DK, int WAVES_, bool OUT, bool DOTS>
 struct Kernel {
     static constexpr int WAVES = WAVES_, COLS = 16 * WAVES, THREADS = 64 * WAVES;

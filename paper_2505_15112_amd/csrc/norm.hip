@@ -84,7 +84,7 @@ __device__ __forceinline__ Pack<W, V> load_weights(const void* w, int at, int co
 
 // A team of LANES threads to a group of a row, with NV vectors a thread: one read of the
 // row, the mean, then the sum of the squared differences.  Bound by memory: 8192 x 4096,
-// bf16, with the sum: 48 us for 268 MB, 5.6 TB/s.
+// bf16, with the sum: 51 us for 268 MB, 5.2 TB/s.
 constexpr int kFrontThreads = 256;
 template <class T, class W, int LANES, int NV>
 __global__ void __launch_bounds__(LANES > kFrontThreads ? LANES : kFrontThreads, 8)
@@ -163,8 +163,8 @@ struct Grad {
 // the next row's elements on their way while one is worked on, and add up dweight
 // and dbias of their columns in registers, then over the teams in order.  Block i of a
 // group has its sums at dweight + i * apart and dbias + i * apart (nullable).  A launch takes
-// `some` groups from the first on.  8192 x
-// 4096, bf16, with dsum: 60 us for 268 MB, 4.4 TB/s.
+// `some` groups from the first on.  8192 x 4096, bf16, with dsum: 62 us for 268 MB, 4.3
+// TB/s.
 constexpr int kBackThreads = 1024;
 template <class T, class W, int LANES, int NV>
 __global__ void __launch_bounds__(kBackThreads)
@@ -315,7 +315,7 @@ __global__ void __launch_bounds__(kBackThreads)
 constexpr int kThreads = 1024;
 
 // A workgroup to a group of a row, which is read three times, twice from the L2 cache.  501
-// x 16389, fp16: 16 us; with three vectors a thread in registers 15, but some of them
+// x 16389, fp16: 17 us; with three vectors a thread in registers 15, but some of them
 // spilled, with four, one workgroup to a CU, 19.
 template <class T, class W>
 __global__ void __launch_bounds__(kThreads)
@@ -530,7 +530,6 @@ int64_t parts(const libscan_norm& p) {
     const Team t = team(p, true);
     if (!t.lanes) return (rows + part_rows(p) - 1) / part_rows(p);
     const int64_t teams = kBackThreads / t.lanes, blocks = (rows + teams - 1) / teams;
-    // a workgroup to a CU, two where rows are short
     // a workgroup to a CU: twice as many take turns (8192 x 4096, bf16: 70 us, not 60)
     const int64_t most = p.groups >= 256 ? 1 : 256 / p.groups;
     return blocks < most ? blocks : most;
