@@ -128,3 +128,51 @@ def test_long_rows_against_the_definition(kind, dims):
     check_forward(a)
     check_backward(a, dy, torch.randn(*a["state"].shape,
                                       generator=torch.Generator().manual_seed(3)))
+
+
+def test_more_rows_than_workgroups_of_a_launch():
+    """2^20 + 5 rows of two tokens, whose only pair is that of tokens 0 and 1."""
+    rows, d = (1 << 20) + 5, 4
+    g = torch.Generator(device=DEV).manual_seed(3)
+    q, k, v, dy = (torch.randn(rows, 2, 1, d, device=DEV, generator=g) for _ in range(4))
+    decay = -torch.rand(rows, 2, 1, device=DEV, generator=g)
+    announce("linear_attention_backward", rows)
+    got = ops.linear_attention_backward(dy, q, k, v, decay)[3][:, :, 0]
+    qk, dv = ((x[:, 1, 0].double() * y[:, 0, 0].double()) for x, y in ((q, k), (dy, v)))
+    a = torch.exp(decay[:, 1, 0].double()) / d ** 0.5
+    want, mag = a * qk.sum(1) * dv.sum(1), a * qk.abs().sum(1) * dv.abs().sum(1)
+    # two dots of four terms through some eight roundings each, and their difference (token 1's
+    # k dq is 0)
+    assert ((got[:, 1] - want).abs() <= 32 * 2.0**-24 * mag + 2.0**-126).all()
+    assert (got[:, 0].abs() <= 32 * 2.0**-24 * mag + 2.0**-126).all()
+
+
+def test_a_captured_graph_of_long_rows_replays():
+    """Rows of several 512 tokens, ragged, replayed over new inputs with eager work between."""
+    size, lengths = (3, 1300, 2, 1, 64, 48), [1300, 1024, 70]
+    a, dy = inputs(*size, kind=BF16, state=True, lengths=lengths, rate=0.1)
+    d, dy = dev(a), dy.to(DEV)
+
+    def work():
+        y, last = ops.linear_attention(**d, with_state=True)
+        return (y, last, *ops.linear_attention_backward(dy, **d, dstate_out=last))
+
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        first = work()
+    torch.cuda.current_stream().wait_stream(side)
+    assert all(torch.equal(x, w) for x, w in zip(first, work()))
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        out = work()
+    for seed in range(3):
+        b, dy2 = inputs(*size, kind=BF16, state=True, lengths=lengths, rate=0.1, seed=20 + seed)
+        for k in ("q", "k", "v", "log_decay", "state"):
+            d[k].copy_(b[k])
+        dy.copy_(dy2)
+        want = work()
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(x, w) for x, w in zip(out, want))
